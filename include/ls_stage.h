@@ -268,6 +268,112 @@ ls_status ls_stage_check_decode(const ls_stage* stage, int batch, int max_ctx);
 ls_status ls_stage_decode_static(ls_stage* stage, const void* in, int batch, int max_ctx,
                                  const ls_kv* kv, void* out, float* logits_out, void* hip_stream);
 
+/* ---- several continuations of a sequence over one cache --------------------------------
+ *
+ * Trees of drafted tokens (speculative decoding) and beams.  These calls need no stage handle: they work on a cache
+ * of any span of layers, one layer's for the attention, with the conventions above.  Buffers are device memory unless "host"
+ * is said, 4-byte aligned at least (bf16 rows: 2); caches, rows and outputs on 16 bytes take the faster kernels.
+ */
+
+/* Shape of the attention heads and of the cache they work on. */
+typedef struct {
+  uint32_t dtype;      /* LS_DTYPE_F32 or LS_DTYPE_BF16: queries, keys, values, caches                    */
+  uint32_t n_q_heads;  /* query head h reads kv head h / (n_q_heads / n_kv_heads)                         */
+  uint32_t n_kv_heads; /* divides n_q_heads                                                               */
+  uint32_t head_dim;   /* even, at most 256                                                               */
+  uint32_t max_batch;  /* sequences the cache is laid out for                                             */
+  uint32_t max_seq;    /* positions the cache is laid out for                                             */
+} ls_heads;
+
+/* Most nodes of a tree; most beams of a request and candidates chosen for it. */
+#define LS_TREE_MAX 64
+#define LS_BEAMS_MAX 64
+
+/*
+ * One tree of tokens for each sequence of a call, node after node.  Node 0 is the root, the token that follows the
+ * sequence's cached positions (the one a generation step would be given); a parent stands in front of its children.  Sequence
+ * b has nodes [cu_nodes[b], cu_nodes[b+1]), none to LS_TREE_MAX of them; one without nodes takes no part in the call.
+ *   parents        device int32 [nodes]: index of a node's parent within its own tree; the root's is not read.  A parent
+ *                  that does not stand in front of its child counts as none: the child then follows the cache itself.
+ *   cu_nodes       device int32 [batch+1], cu_nodes[0] = 0.   cu_nodes_host: host copy (validation and launch sizing).
+ */
+typedef struct {
+  const int32_t* parents;
+  const int32_t* cu_nodes;
+  const int32_t* cu_nodes_host;
+} ls_tree;
+
+/* Device bytes of scratch with which every ls_tree_attention call of this shape cuts long contexts into as many chunks as
+ * pay; 0 if it needs none or the shape is invalid. */
+size_t ls_tree_attention_scratch_bytes(const ls_heads* heads);
+
+/*
+ * Attention of one layer for the trees' nodes.  Node i of sequence b stands at position seq_lens[b] + depth(i), its key and
+ * value are written to cache slot seq_lens[b] + i, and it attends to the cached positions 0..seq_lens[b]-1 and to the slots
+ * of its path from the root, itself included.  seq_lens is not changed: the nodes become positions with ls_tree_keep.
+ *   qkv       [nodes, (n_q_heads + 2 n_kv_heads) * head_dim]: query heads, key heads, value heads side by side
+ *   rope      fp32 [max_seq][head_dim/2][2], cos and sin by which pair (2i, 2i+1) of queries and keys turns at a position
+ *             (the table that a stage's workspace starts with), or NULL: rows come turned
+ *   layer     one layer's cache, k and v [max_batch][n_kv_heads][max_seq][head_dim], and seq_lens
+ *   out       [nodes, n_q_heads * head_dim]
+ *   max_ctx   host-side upper bound of seq_lens[b]; max_ctx + the smallest tree beyond max_seq is LS_ERR_KV_OVERFLOW.  An
+ *             understated bound costs speed, never keys.
+ *   scratch   16-byte aligned, or NULL: holds partial results of contexts that several workgroups share; less than
+ *             ls_tree_attention_scratch_bytes, or none, costs speed.  Nothing in it outlasts the call.
+ * Scores, softmax and sums are fp32.  A sequence whose tree finds no room behind seq_lens[b] on the device keeps its cache, and its
+ * output rows are zeros.
+ */
+ls_status ls_tree_attention(const ls_heads* heads, const ls_tree* tree, int batch, int max_ctx, const void* qkv, const float* rope,
+                            const ls_kv* layer, void* out, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/*
+ * Which drafts a model agrees with: tokens[i] are the nodes' tokens, said[i] what the model says behind node i (its greedy token).
+ * The root is accepted, another node if its parent is and its token is what the model says behind that.  Of the
+ * deepest accepted nodes the one of the lowest index and its path are kept.  Per sequence b (outputs [batch] unless noted):
+ *   kept       uint64, bit i: node i is kept
+ *   count      nodes kept, the root among them
+ *   emitted    [batch][LS_TREE_MAX] the tokens gained: said[i] along the path, count of them, then -1
+ *   following  the last of them, the next tree's root; -1 for a sequence without nodes, whose kept and count are 0
+ */
+ls_status ls_tree_accept(const ls_tree* tree, int batch, const int32_t* tokens, const int32_t* said, uint64_t* kept, int32_t* count,
+                         int32_t* emitted, int32_t* following, void* hip_stream);
+
+/*
+ * Make the kept nodes positions: in every layer of the cache (k, v [layers][max_batch][n_kv_heads][max_seq][head_dim]) the rows
+ * of sequence b's kept nodes move, in index order, to the slots from seq_lens[b] on, and seq_lens[b] grows by their number.
+ * `kept` may come from ls_tree_accept or from the caller's own rule; bits beyond a tree are not read.  Slots behind the kept
+ * ones are left as they are.  A sequence without nodes, or without room for its tree, is left alone.  Only tree->cu_nodes and
+ * cu_nodes_host are read.  Stages of a pipeline call it each on their own cache.
+ */
+ls_status ls_tree_keep(const ls_heads* heads, int layers, const ls_tree* tree, int batch, const uint64_t* kept, const ls_kv* kv, void* hip_stream);
+
+/*
+ * The k best continuations of each of `groups` requests with `beams` beams (both 1..LS_BEAMS_MAX): row g * beams + b is beam b
+ * of request g, candidate (b, token) scores scores[row] + logits[row][token] - log(sum(exp(logits[row]))).  Best first; equal
+ * scores go by the lower b * vocab + token.  Scores are compared in 64 bits (the sums of exponentials are of fp32
+ * terms) and rounded to fp32 on output.  A beam of score -inf has no candidates but at -inf, and so has one whose logits make the sum
+ * NaN or infinite; where candidates above -inf do not suffice those come in the order of their index.
+ *   logits [groups * beams, vocab] fp32, as ls_stage_prefill and ls_stage_decode write them;  scores [groups * beams]
+ *   ended  optional int32 [groups * beams]: a beam with a nonzero entry has ended; its one candidate is token eos at its own
+ *          score, and its logits are not used
+ *   rows, tokens, scores_out  [groups, k]: the candidate's row, token and score
+ *   scratch of ls_beam_select_scratch_bytes (0: invalid sizes), 16-byte aligned; nothing in it outlasts the call
+ */
+size_t ls_beam_select_scratch_bytes(int groups, int beams, int vocab, int k);
+ls_status ls_beam_select(const float* logits, const float* scores, const int32_t* ended, int groups, int beams, int vocab, int k, int eos,
+                         int32_t* rows, int32_t* tokens, float* scores_out, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/*
+ * Give each sequence the cache of another one of its group, all at once and in place: in every layer (k, v as in ls_tree_keep)
+ * positions first[b] <= p < seq_lens[src[b]] of sequence b become those that src[b] had, and seq_lens[b] becomes seq_lens[src[b]].
+ * The sequences [0, batch) are groups of `group` neighbours (1..LS_BEAMS_MAX, a divisor of batch).
+ *   src      int32 [batch] sequence index (the rows of ls_beam_select where k = beams); one outside b's group counts as b
+ *   first    optional int32 [batch]: positions below it are the same in b and src[b] already, as a shared prompt's are
+ *   max_ctx  host-side upper bound of seq_lens[b]; positions at and beyond it are not moved
+ */
+ls_status ls_kv_reorder(const ls_heads* heads, int layers, const int32_t* src, int batch, int group, const int32_t* first, int max_ctx,
+                        const ls_kv* kv, void* hip_stream);
+
 /* ---- measurement ---------------------------------------------------------------------*/
 
 /* With profiling on, ls_stage_load_block brackets each copy and ls_stage_prefill brackets

@@ -29,6 +29,7 @@ lib = C.CDLL(LIB_PATH)
 
 LS_ABI_VERSION = 1
 LS_STATIC_SCRATCH_BYTES = 16 << 20
+LS_TREE_MAX = LS_BEAMS_MAX = 64
 LS_DTYPE_F32, LS_DTYPE_BF16 = 0, 1
 LS_BLOCK_EMBED = -1
 LS_OP_NONE, LS_OP_NORM, LS_OP_GEMM_QKV = 0, 1, 2
@@ -50,6 +51,14 @@ class ls_cfg(C.Structure):
 
 class ls_kv(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("seq_lens", C.c_void_p)]
+
+
+class ls_heads(C.Structure):
+    _fields_ = [(n, C.c_uint32) for n in ("dtype", "n_q_heads", "n_kv_heads", "head_dim", "max_batch", "max_seq")]
+
+
+class ls_tree(C.Structure):
+    _fields_ = [("parents", C.c_void_p), ("cu_nodes", C.c_void_p), ("cu_nodes_host", C.c_void_p)]
 
 
 class ls_microbatch(C.Structure):
@@ -105,6 +114,13 @@ _SIGS = {
     "ls_probe_mfma_tflops": (C.c_double, [C.c_int, C.c_int, C.c_void_p, C.c_void_p]),
     "ls_plan_multicast_schedule": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int,
                                              C.POINTER(C.c_int)]),
+    "ls_tree_attention_scratch_bytes": (C.c_size_t, [C.POINTER(ls_heads)]),
+    "ls_tree_attention": (C.c_int, [C.POINTER(ls_heads), C.POINTER(ls_tree), C.c_int, C.c_int, _P, _P, C.POINTER(ls_kv), _P, _P, C.c_size_t, _P]),
+    "ls_tree_accept": (C.c_int, [C.POINTER(ls_tree), C.c_int, _P, _P, _P, _P, _P, _P, _P]),
+    "ls_tree_keep": (C.c_int, [C.POINTER(ls_heads), C.c_int, C.POINTER(ls_tree), C.c_int, _P, C.POINTER(ls_kv), _P]),
+    "ls_beam_select_scratch_bytes": (C.c_size_t, [C.c_int] * 4),
+    "ls_beam_select": (C.c_int, [_P, _P, _P] + [C.c_int] * 5 + [_P, _P, _P, _P, C.c_size_t, _P]),
+    "ls_kv_reorder": (C.c_int, [C.POINTER(ls_heads), C.c_int, _P, C.c_int, C.c_int, _P, C.c_int, C.POINTER(ls_kv), _P]),
     "ls_last_error": (C.c_char_p, []),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -151,6 +167,130 @@ def pack_block(cfg: ls_cfg, layer: int, tensors: Sequence[np.ndarray], out: Opti
             raise ValueError("tensor %d of block %d has %d bytes, format says %d" % (i, layer, raw.size, nb.value))
         buf[off.value : off.value + nb.value] = raw
     return buf
+
+
+# ---- several continuations of a sequence over one cache: include/ls_stage.h says what each call does ----------------------
+# They run on torch's current stream of their tensors' device and allocate their outputs and scratch there.
+def _tensor(name, t, dtype, device, numel=None):
+    """A pointer to `t`, which has to be a contiguous tensor of `dtype` on `device` (of `numel` elements)."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+        raise ValueError("%s: a %s tensor on %s is wanted" % (name, dtype, device))
+    if not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        raise ValueError("%s: %swanted contiguous, got %s" % (name, "" if numel is None else "%d elements " % numel, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _gpu(t):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("a tensor on a GPU is wanted")
+    return t.device
+
+
+def _run(device, fn, *args):
+    stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        check(fn(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            check(fn(*args, stream))
+
+
+def _cache(k, v, seq_lens, dims, n_q_heads=None):
+    """ls_heads and ls_kv of a cache [.., max_batch, n_kv_heads, max_seq, head_dim] of `dims` dimensions."""
+    device = _gpu(k)
+    if k.dim() != dims or k.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("k: a float32 or bfloat16 cache of %d dimensions is wanted" % dims)
+    b, hkv, s, hd = k.shape[-4:]
+    if tuple(v.shape) != tuple(k.shape):
+        raise ValueError("v: the shape of k is wanted")
+    kv = ls_kv(_tensor("k", k, k.dtype, device), _tensor("v", v, k.dtype, device), _tensor("seq_lens", seq_lens, torch.int32, device))
+    if seq_lens.numel() < b:
+        raise ValueError("seq_lens: %d entries are wanted" % b)
+    return ls_heads(LS_DTYPE_F32 if k.dtype == torch.float32 else LS_DTYPE_BF16, n_q_heads or hkv, hkv, hd, b, s), kv
+
+
+def _trees(parents, cu_nodes, cu_nodes_host, device):
+    """(ls_tree, sequences, nodes, what has to stay alive through the call)."""
+    host = np.ascontiguousarray(cu_nodes_host, np.int32)
+    if host.ndim != 1 or host.size < 2:
+        raise ValueError("cu_nodes_host: the trees' bounds are wanted, one more than sequences")
+    rows = max(0, int(host[-1]))
+    if parents is not None:
+        parents = _tensor("parents", parents, torch.int32, device, rows)
+    tree = ls_tree(parents, _tensor("cu_nodes", cu_nodes, torch.int32, device, host.size), host.__array_interface__["data"][0])
+    return tree, host.size - 1, rows, host
+
+
+def tree_attention(qkv, parents, cu_nodes, cu_nodes_host, rope, k, v, seq_lens, max_ctx: int, out=None):
+    """Attention of one layer for trees of drafted tokens (ls_tree_attention): the nodes' keys and values are written behind
+    the cached positions of k and v [max_batch, n_kv_heads, max_seq, head_dim].  qkv [nodes, (n_q_heads + 2 n_kv_heads) * head_dim];
+    parents, cu_nodes: int32 on the GPU, cu_nodes_host: the same bounds on the host; rope: float32 [max_seq, head_dim/2, 2]
+    or None.  Returns [nodes, n_q_heads * head_dim]."""
+    device = _gpu(qkv)
+    if k.dim() != 4 or qkv.dim() != 2 or qkv.shape[1] % k.shape[3]:
+        raise ValueError("k of 4 dimensions and qkv of 2, whose columns are heads, are wanted")
+    hq, hd = qkv.shape[1] // k.shape[3] - 2 * k.shape[1], k.shape[3]
+    if hq < 1:
+        raise ValueError("qkv: %d columns hold no query head" % qkv.shape[1])
+    heads, kv = _cache(k, v, seq_lens, 4, hq)
+    tree, batch, rows, host = _trees(parents, cu_nodes, cu_nodes_host, device)
+    q = _tensor("qkv", qkv, k.dtype, device, rows * qkv.shape[1])
+    turn = None if rope is None else _tensor("rope", rope, torch.float32, device, k.shape[2] * hd)
+    if out is None:
+        out = torch.empty(rows, hq * hd, dtype=k.dtype, device=device)
+    to = _tensor("out", out, k.dtype, device, rows * hq * hd)
+    nb = lib.ls_tree_attention_scratch_bytes(C.byref(heads))
+    scratch = torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+    _run(device, lib.ls_tree_attention, C.byref(heads), C.byref(tree), batch, max_ctx, q, turn, C.byref(kv), to,
+         scratch.data_ptr() if nb else None, nb)
+    return out
+
+
+def tree_accept(tokens, said, parents, cu_nodes, cu_nodes_host):
+    """Which drafted tokens a model agrees with (ls_tree_accept); tokens and said: int32, one for each node.  Returns kept (int64,
+    a bit for each node), count, emitted [sequences, LS_TREE_MAX] and the next roots, int32."""
+    device = _gpu(tokens)
+    tree, batch, rows, host = _trees(parents, cu_nodes, cu_nodes_host, device)
+    kept = torch.empty(batch, dtype=torch.int64, device=device)
+    count, following = (torch.empty(batch, dtype=torch.int32, device=device) for _ in range(2))
+    emitted = torch.empty(batch, LS_TREE_MAX, dtype=torch.int32, device=device)
+    _run(device, lib.ls_tree_accept, C.byref(tree), batch, _tensor("tokens", tokens, torch.int32, device, rows),
+         _tensor("said", said, torch.int32, device, rows), kept.data_ptr(), count.data_ptr(), emitted.data_ptr(), following.data_ptr())
+    return kept, count, emitted, following
+
+
+def tree_keep(kept, cu_nodes, cu_nodes_host, k, v, seq_lens):
+    """Make the kept nodes positions of k and v [layers, max_batch, n_kv_heads, max_seq, head_dim] (ls_tree_keep)."""
+    device = _gpu(k)
+    heads, kv = _cache(k, v, seq_lens, 5)
+    tree, batch, _, host = _trees(None, cu_nodes, cu_nodes_host, device)
+    _run(device, lib.ls_tree_keep, C.byref(heads), k.shape[0], C.byref(tree), batch, _tensor("kept", kept, torch.int64, device, batch), C.byref(kv))
+
+
+def beam_select(logits, scores, beams: int, k: int, ended=None, eos: int = 0):
+    """The k best continuations of each request's beams (ls_beam_select); logits [requests * beams, vocab] and scores [requests *
+    beams] float32, ended: int32 or None.  Returns rows, tokens (int32) and scores [requests, k]."""
+    device = _gpu(logits)
+    if logits.dim() != 2 or beams < 1 or logits.shape[0] % beams:
+        raise ValueError("logits: [requests * beams, vocab] is wanted")
+    n, vocab = logits.shape
+    nb = lib.ls_beam_select_scratch_bytes(n // beams, beams, vocab, k)
+    scratch = torch.empty(max(nb, 16), dtype=torch.uint8, device=device)
+    rows, tokens = (torch.empty(n // beams, max(k, 0), dtype=torch.int32, device=device) for _ in range(2))
+    best = torch.empty(n // beams, max(k, 0), dtype=torch.float32, device=device)
+    _run(device, lib.ls_beam_select, _tensor("logits", logits, torch.float32, device), _tensor("scores", scores, torch.float32, device, n),
+         None if ended is None else _tensor("ended", ended, torch.int32, device, n), n // beams, beams, vocab, k, eos,
+         rows.data_ptr(), tokens.data_ptr(), best.data_ptr(), scratch.data_ptr(), nb)
+    return rows, tokens, best
+
+
+def kv_reorder(src, group: int, k, v, seq_lens, max_ctx: int, first=None):
+    """Give each sequence the cache of sequence src[b] of its group, in place (ls_kv_reorder); k and v [layers, max_batch,
+    n_kv_heads, max_seq, head_dim], src and first: int32, one for each sequence."""
+    device = _gpu(k)
+    heads, kv = _cache(k, v, seq_lens, 5)
+    _run(device, lib.ls_kv_reorder, C.byref(heads), k.shape[0], _tensor("src", src, torch.int32, device), src.numel(), group,
+         None if first is None else _tensor("first", first, torch.int32, device, src.numel()), max_ctx, C.byref(kv))
 
 
 class Stage:

@@ -315,6 +315,23 @@ void launch_attention_generic(uint32_t dt, const void* qkv, int qkv_stride, cons
                               const void* vcache, const int32_t* row_seq, const int32_t* row_pos, int rows,
                               int hq, int hkv, int hd, int max_seq, void* out, hipStream_t st);
 
+// Attention of trees of drafted tokens over their sequences' caches, with RoPE and the cache append (tree_attn.hip): node i of
+// sequence b is row cu[b] + i of qkv [rows, (hq + 2 hkv) hd], takes cache slot seq_lens[b] + i, is turned by its depth behind
+// seq_lens[b] (cs null: not turned) and sees the cached positions and its path from the root.  out is [rows, hq hd]; rows of a
+// sequence without room for its tree hold zeros.
+struct TreeAttn {
+  const void* qkv = nullptr;
+  const float* cs = nullptr;
+  const int32_t *parents = nullptr, *cu = nullptr, *seq_lens = nullptr;
+  int batch = 0, rows = 0, max_nodes = 0, max_keys = 0;  // max_keys: upper bound of cached positions and nodes of a sequence
+  int hq = 0, hkv = 0, hd = 0, max_seq = 0;
+  void *kc = nullptr, *vc = nullptr, *out = nullptr;
+  float* scratch = nullptr;  // partial results of contexts cut into chunks, or null
+  size_t scratch_bytes = 0;
+};
+size_t tree_attn_scratch_bytes(uint32_t dt, int hq, int hkv, int hd, int max_batch, int max_seq);
+void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st);
+
 // tok[r] = index of the largest logit of row r, lowest index on ties.
 void launch_argmax(const float* logits, int rows, int vocab, int32_t* tok, hipStream_t st);
 

@@ -1,0 +1,135 @@
+// Attention of a tree of drafted tokens over a sequence's cache, with RoPE and the cache append.
+//
+// Node i of a sequence with c cached positions stands at position c + depth(i) and takes cache slot c + i.  Its query sees the c
+// cached keys and the slots of the nodes on its path from the root, itself included.
+//
+// Kernels for every shape: one rotates and appends the nodes' keys and values, one attends, a wavefront to a (row, query head).
+#include "tree.hpp"
+
+namespace ls {
+
+namespace {
+
+template <class T>
+__global__ void __launch_bounds__(256)
+k_tree_append(const T* __restrict__ qkv, const float2* __restrict__ cs, const int32_t* __restrict__ cu, const int32_t* __restrict__ parents,
+              const int32_t* __restrict__ seq_lens, int rows, int hq, int hkv, int hd, int max_seq, T* __restrict__ kc, T* __restrict__ vc) {
+  const int b = blockIdx.x, kh = blockIdx.y;
+  TreeSeq t;
+  if (!tree_seq(cu, seq_lens, b, rows, max_seq, t)) return;
+  __shared__ int depth[TREE_MAX];
+  const uint64_t path = tree_path(parents, t);
+  if (threadIdx.x < 64) depth[threadIdx.x] = __builtin_popcountll(path) - 1;
+  __syncthreads();
+  const int half = hd >> 1;
+  const size_t base = (((size_t)b * hkv + kh) * max_seq + t.ctx) * hd;
+  for (int i = threadIdx.x; i < t.n * half; i += 256) {
+    const int node = i / half, p = i - node * half;
+    const T* row = qkv + (size_t)(t.row0 + node) * (hq + 2 * hkv) * hd;
+    const T* k = row + (size_t)(hq + kh) * hd + 2 * p;
+    const T* v = row + (size_t)(hq + hkv + kh) * hd + 2 * p;
+    T* ko = kc + base + (size_t)node * hd + 2 * p;
+    T* vo = vc + base + (size_t)node * hd + 2 * p;
+    if (cs) {
+      const float2 turn = cs[(size_t)(t.ctx + depth[node]) * half + p];
+      const float u0 = to_f(k[0]), u1 = to_f(k[1]);
+      ko[0] = from_f<T>(turn0(u0, u1, turn));
+      ko[1] = from_f<T>(turn1(u0, u1, turn));
+    } else {
+      ko[0] = k[0];
+      ko[1] = k[1];
+    }
+    vo[0] = v[0];
+    vo[1] = v[1];
+  }
+}
+
+template <class T>
+__global__ void __launch_bounds__(64)
+k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int32_t* __restrict__ cu, const int32_t* __restrict__ parents,
+            const int32_t* __restrict__ seq_lens, int rows, int hq, int hkv, int hd, int max_seq, const T* __restrict__ kc,
+            const T* __restrict__ vc, T* __restrict__ out) {
+  constexpr int MAXP = 2;  // pairs of a lane: head_dim <= 256
+  const int b = blockIdx.x, node = blockIdx.y, h = blockIdx.z, lane = threadIdx.x, half = hd >> 1;
+  const int row0 = cu[b], n = cu[b + 1] - row0;
+  if (node >= n || row0 < 0 || row0 + node >= rows) return;
+  T* o = out + (size_t)(row0 + node) * hq * hd + (size_t)h * hd;
+  TreeSeq t;
+  if (!tree_seq(cu, seq_lens, b, rows, max_seq, t)) {  // no room: the rows hold zeros
+    for (int i = lane; i < hd; i += 64) o[i] = from_f<T>(0.f);
+    return;
+  }
+  const uint64_t all = tree_path(parents, t);
+  const uint64_t path = (uint64_t)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(all >> 32), node) << 32 |
+                        (unsigned)__builtin_amdgcn_readlane((int)(unsigned)all, node);
+  const int kh = h / (hq / hkv), pos = t.ctx + __builtin_popcountll(path) - 1;
+  const T* q = qkv + (size_t)(row0 + node) * (hq + 2 * hkv) * hd + (size_t)h * hd;
+  const float scale = 1.0f / sqrtf((float)hd);
+  float q0[MAXP], q1[MAXP], a0[MAXP], a1[MAXP];
+#pragma unroll
+  for (int i = 0; i < MAXP; ++i) {
+    const int p = lane + 64 * i;
+    a0[i] = a1[i] = q0[i] = q1[i] = 0.f;
+    if (p < half) {
+      const float u0 = to_f(q[2 * p]), u1 = to_f(q[2 * p + 1]);
+      const float2 turn = cs ? cs[(size_t)pos * half + p] : float2{1.f, 0.f};
+      q0[i] = (cs ? turn0(u0, u1, turn) : u0) * scale;
+      q1[i] = (cs ? turn1(u0, u1, turn) : u1) * scale;
+    }
+  }
+  const T* kb = kc + ((size_t)b * hkv + kh) * max_seq * hd;
+  const T* vb = vc + ((size_t)b * hkv + kh) * max_seq * hd;
+  float m = -INFINITY, l = 0.f;
+  for (int key = 0; key < t.ctx + t.n; ++key) {
+    if (key >= t.ctx && !(path >> (key - t.ctx) & 1)) continue;
+    const T* kr = kb + (size_t)key * hd;
+    const T* vr = vb + (size_t)key * hd;
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < MAXP; ++i) {
+      const int p = lane + 64 * i;
+      if (p < half) s = fmaf(q0[i], to_f(kr[2 * p]), fmaf(q1[i], to_f(kr[2 * p + 1]), s));
+    }
+    s = wave_sum(s);
+    const float mn = fmaxf(m, s);
+    const float corr = mn == -INFINITY ? 1.f : __expf(m - mn), w = s == -INFINITY ? 0.f : __expf(s - mn);
+    l = fmaf(l, corr, w);
+#pragma unroll
+    for (int i = 0; i < MAXP; ++i) {
+      const int p = lane + 64 * i;
+      if (p < half) {
+        a0[i] = fmaf(w, to_f(vr[2 * p]), a0[i] * corr);
+        a1[i] = fmaf(w, to_f(vr[2 * p + 1]), a1[i] * corr);
+      }
+    }
+    m = mn;
+  }
+#pragma unroll
+  for (int i = 0; i < MAXP; ++i) {
+    const int p = lane + 64 * i;
+    if (p < half) {
+      o[2 * p] = from_f<T>(a0[i] / l);
+      o[2 * p + 1] = from_f<T>(a1[i] / l);
+    }
+  }
+}
+
+template <class T>
+void launch_any(const TreeAttn& a, hipStream_t st) {
+  k_tree_append<T><<<dim3(a.batch, a.hkv), 256, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.hq, a.hkv, a.hd,
+                                                         a.max_seq, (T*)a.kc, (T*)a.vc);
+  k_tree_attn<T><<<dim3(a.batch, a.max_nodes, a.hq), 64, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.hq,
+                                                                  a.hkv, a.hd, a.max_seq, (const T*)a.kc, (const T*)a.vc, (T*)a.out);
+}
+
+}  // namespace
+
+size_t tree_attn_scratch_bytes(uint32_t, int, int, int, int, int) { return 0; }
+
+void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st) {
+  if (a.rows <= 0) return;
+  if (dt == F32) launch_any<float>(a, st);
+  else launch_any<bf16>(a, st);
+}
+
+}  // namespace ls
