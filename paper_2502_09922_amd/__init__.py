@@ -14,5 +14,6 @@ def __getattr__(name):
         import importlib
 
         binding = importlib.import_module(".binding", __name__)
-        return binding if name == "binding" else getattr(binding, name)
+        value = globals()[name] = binding if name == "binding" else getattr(binding, name)  # found without this function from now on
+        return value
     raise AttributeError(name)

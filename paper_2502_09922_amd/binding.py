@@ -116,6 +116,7 @@ _SIGS = {
                                              C.POINTER(C.c_int)]),
     "ls_tree_attention_scratch_bytes": (C.c_size_t, [C.POINTER(ls_heads)]),
     "ls_tree_attention": (C.c_int, [C.POINTER(ls_heads), C.POINTER(ls_tree), C.c_int, C.c_int, _P, _P, C.POINTER(ls_kv), _P, _P, C.c_size_t, _P]),
+    "ls_stage_tree": (C.c_int, [_P, _P, C.POINTER(ls_tree), C.c_int, C.c_int, C.POINTER(ls_kv), _P, _P, _P]),
     "ls_tree_accept": (C.c_int, [C.POINTER(ls_tree), C.c_int, _P, _P, _P, _P, _P, _P, _P]),
     "ls_tree_keep": (C.c_int, [C.POINTER(ls_heads), C.c_int, C.POINTER(ls_tree), C.c_int, _P, C.POINTER(ls_kv), _P]),
     "ls_beam_select_scratch_bytes": (C.c_size_t, [C.c_int] * 4),
@@ -421,6 +422,26 @@ class Stage:
         check(fn(
             self.handle, inp.data_ptr(), batch, max_ctx, C.byref(self.kv), out.data_ptr(),
             logits.data_ptr() if logits is not None else None, self._stream_ptr(stream)))
+        return (out, logits) if want_logits else out
+
+    def caches(self):
+        """Keys and values [layers, max_batch, n_kv_heads, max_seq, head_dim], as tree_keep and kv_reorder take them."""
+        size = (self.hi - self.lo, self.cfg.max_batch, self.cfg.n_kv_heads, self.cfg.max_seq, self.cfg.head_dim)
+        return self.k.view(self.tdtype).view(size), self.v.view(self.tdtype).view(size)
+
+    def tree(self, inp, parents, cu_nodes, cu_nodes_host, max_ctx: int, stream=None, want_logits=False):
+        """ls_stage_tree: the pass over the nodes of draft trees (see tree_attention for their arguments); inp, parents and
+        cu_nodes are on the stage's device.  tree_accept says which nodes to keep, tree_keep makes them positions of caches()."""
+        torch = self.torch
+        tree, batch, rows, host = _trees(parents, cu_nodes, cu_nodes_host, self.slab.device)
+        with torch.cuda.stream(stream):  # outputs belong to the stream that writes them
+            out = (torch.empty(rows, dtype=torch.int32, device=self.device) if self.last
+                   else torch.empty(rows, self.shape.hidden, dtype=self.tdtype, device=self.device))
+            logits = torch.empty(rows, self.shape.vocab, dtype=torch.float32, device=self.device) if (want_logits and self.last) else None
+        check(lib.ls_stage_tree(self.handle, _tensor("inp", inp, torch.int32 if self.first else self.tdtype, self.slab.device,
+                                                     rows if self.first else rows * self.shape.hidden),
+                                C.byref(tree), batch, max_ctx, C.byref(self.kv), out.data_ptr(), logits.data_ptr() if logits is not None else None,
+                                self._stream_ptr(stream)))
         return (out, logits) if want_logits else out
 
     def workspace_region(self, which: int, rows: int):

@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(NT) k_rows(const void* in, float* x, const voi
           a.last_rows[lo] = r;
           a.seq_lens[lo] = c1 - c0;
         }
-      } else {  // generation step: a sequence without room is left alone and marked -1
+      } else if (a.seq_lens) {  // generation step: a sequence without room is left alone and marked -1
         const int p = a.seq_lens[r];
         const bool ok = p >= 0 && p < a.max_seq;
         a.row_seq[r] = r;

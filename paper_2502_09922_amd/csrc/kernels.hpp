@@ -207,7 +207,7 @@ struct RowsArgs {
   const void* in = nullptr;
   const void* table = nullptr;
   int vocab = 0;
-  const int32_t* cu = nullptr;  // prompt pass: sequence bounds; nullptr: generation step
+  const int32_t* cu = nullptr;  // prompt pass: sequence bounds; nullptr: generation step, or without seq_lens no bookkeeping
   int batch = 0, max_seq = 0;
   int32_t *row_seq = nullptr, *row_pos = nullptr, *last_rows = nullptr, *seq_lens = nullptr;
   void* out = nullptr;

@@ -1,7 +1,7 @@
 // Stage runtime behind the C ABI of include/ls_stage.h: block table, event-gated loader,
 // workspace carving and the per-layer launch sequence.  Host code only; every device step
 // is a kernel launched through kernels.hpp.
-#include "../../include/ls_stage.h"
+#include "entry.hpp"
 #include "kernels.hpp"
 
 #include <algorithm>
@@ -582,9 +582,10 @@ bool own_memory(const ls_stage* s, const void* p) {
   return false;
 }
 
-// `gsc`: where GEMM kernels that split K across workgroups put their partial tiles.
+// `gsc`: where GEMM kernels that split K across workgroups put their partial tiles.  `trees`: the rows are nodes of draft trees,
+// of which every one gets logits and a next token; rows keep no maps then and seq_lens stays.
 ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_dev, int batch, int rows, int max_len,
-                  const ls_kv* kv, void* out, float* logits_out, hipStream_t st, const ls::GemmScratch& gsc) {
+                  const ls_kv* kv, void* out, float* logits_out, hipStream_t st, const ls::GemmScratch& gsc, const ls::TreeAttn* trees = nullptr) {
   using namespace ls;
   const ls_cfg& c = s->cfg;
   const uint32_t dt = c.dtype;
@@ -603,7 +604,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   int32_t* row_pos = (int32_t*)(ws + s->w.row_pos);
   int32_t* last_rows = (int32_t*)(ws + s->w.last_rows);
   const bool timed = s->profiling && prefill;
-  const bool probing = s->probe_op != LS_OP_NONE && s->probe_phase == (prefill ? 0 : 1) && !s->probe_a.empty();
+  const bool probing = !trees && s->probe_op != LS_OP_NONE && s->probe_phase == (prefill ? 0 : 1) && !s->probe_a.empty();
 
   // PROBE(op, launch): bracket the launch with an event pair if this (op, layer) is probed
 #define PROBE(op, launch)                                                        \
@@ -635,7 +636,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   const bool few_rows = dt == BF16 && rows <= (d > 4096 ? 8 : 16);
 
   // ---- decode step with the RMSNorms folded into the weight-streaming GEMMs
-  const bool fused = !prefill && dt == BF16 && d % 16 == 0 && (few_rows || !rows_supported(d)) &&
+  const bool fused = !prefill && !trees && dt == BF16 && d % 16 == 0 && (few_rows || !rows_supported(d)) &&
                      (attn_decode_supported(hq, hkv, hd) || attn_decode_gqa_supported(hq, hkv, hd)) &&
                      gemm_decode_fusable(rows, qkv_cols, d) && gemm_decode_fusable(rows, d, hq * hd) &&
                      gemm_decode_fusable(rows, F, d) && gemm_decode_fusable(rows, d, F);
@@ -719,7 +720,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   }
 
   // ---- generation steps of few rows of a small fp32 model: one launch, once every block has landed
-  if (!prefill && dt == F32 && s->step_places.xch && !probing) {
+  if (!prefill && !trees && dt == F32 && s->step_places.xch && !probing) {
     SmallStep a;
     TensorSpan sp[6];
     const Block& b0 = s->blocks[s->layer0];
@@ -784,7 +785,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   };
   // attention without a fused kernel, and that of a prompt pass, wants rotated rows and a filled cache
   const bool attn_rotates =
-      !prefill && (attn_decode_supported(hq, hkv, hd) || (dt == BF16 && attn_decode_gqa_supported(hq, hkv, hd)));
+      trees || (!prefill && (attn_decode_supported(hq, hkv, hd) || (dt == BF16 && attn_decode_gqa_supported(hq, hkv, hd))));
   const bool rope_tiles = !attn_rotates && hd % 16 == 0;  // a 16-column fragment inside one head
   const TiledPlan p_qkv = attn_rotates ? plan(TILED_STORE, qkv_cols, d) : rope_tiles ? plan(TILED_ROPE, qkv_cols, d) : TiledPlan{};
   const TiledPlan p_o = rows_one_pass && gsc.splitk ? plan(TILED_PART, d, hq * hd) : TiledPlan{};
@@ -809,7 +810,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     RowsArgs ra;
     ra.rows = rows; ra.d = d; ra.x = x; ra.in = in; ra.table = table; ra.vocab = c.vocab;
     ra.cu = prefill ? cu_dev : nullptr; ra.batch = batch; ra.max_seq = c.max_seq;
-    ra.row_seq = row_seq; ra.row_pos = row_pos; ra.last_rows = last_rows; ra.seq_lens = kv->seq_lens;
+    ra.row_seq = row_seq; ra.row_pos = row_pos; ra.last_rows = last_rows; ra.seq_lens = trees ? nullptr : kv->seq_lens;
     Block& b0 = s->blocks[s->layer0];
     if (landed(b0) && !norm_alone(b0) && !(few_pieces && folds_norm(p_qkv, qkv_cols))) {
       ra.gamma = tensor(b0, 0); ra.y = y; ra.eps = c.rms_eps;
@@ -824,7 +825,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     launch_rows(dt, s->first ? ROWS_EMBED : ROWS_HIDDEN, ra, st);
   } else {
     if (prefill) launch_row_index_prefill(cu_dev, batch, rows, row_seq, row_pos, last_rows, st);
-    else launch_row_index_decode(kv->seq_lens, batch, c.max_seq, row_seq, row_pos, last_rows, st);
+    else if (!trees) launch_row_index_decode(kv->seq_lens, batch, c.max_seq, row_seq, row_pos, last_rows, st);
     if (s->first) launch_embed(dt, table, (const int32_t*)in, x, rows, d, c.vocab, st);
     else launch_load_hidden(dt, in, x, (size_t)rows * d, st);
   }
@@ -894,10 +895,20 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     } else {
       PROBE(LS_OP_GEMM_QKV, launch_gemm(dt, EPI_STORE, y, tensor(b, 1), rows, qkv_cols, d, qkv, nullptr, st, &gsc));
     }
-    PROBE(LS_OP_ATTENTION, launch_attention_block(dt, cu_dev, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
-                                                  hq, hkv, hd, c.max_seq, attn, st,
-                                                  s->w.attn_part_bytes ? (float*)(ws + s->w.attn_part) : nullptr,
-                                                  s->w.attn_part_bytes, roped));
+    if (trees) {
+      TreeAttn a = *trees;
+      a.qkv = qkv; a.cs = cs; a.kc = kc; a.vc = vc; a.out = attn;
+      // the GEMMs' partial tiles are added up by now, their room is the larger one mostly
+      const bool tiles = s->w.splitk_bytes > s->w.attn_part_bytes;
+      a.scratch = (float*)(ws + (tiles ? s->w.splitk : s->w.attn_part));
+      a.scratch_bytes = tiles ? s->w.splitk_bytes : s->w.attn_part_bytes;
+      launch_tree_attn(dt, a, st);
+    } else {
+      PROBE(LS_OP_ATTENTION, launch_attention_block(dt, cu_dev, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
+                                                    hq, hkv, hd, c.max_seq, attn, st,
+                                                    s->w.attn_part_bytes ? (float*)(ws + s->w.attn_part) : nullptr,
+                                                    s->w.attn_part_bytes, roped));
+    }
     LS_HIP(gate(b, st, 1));
     PROBE(LS_OP_GEMM_O, residual(p_o, attn, tensor(b, 2), hq * hd, fold_gu ? nullptr : tensor(b, 3), false));
     LS_HIP(gate(b, st, 2));
@@ -926,25 +937,33 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     block_tensors(&c, hb->layer, sp, nullptr);
     const char* base = s->slab + hb->off;
     LS_HIP(gate(*hb, st));  // gate: head block has landed
-    float* logits = logits_out ? logits_out : (float*)(ws + s->w.logits);
-    const TiledPlan p_head = (dt == F32 || batch > (d > 4096 ? 8 : 16)) && ((uintptr_t)logits & 15) == 0
-                                 ? gemm_tiled_plan(dt, TILED_PART, batch, (int)c.vocab, d, false, 0, nullptr, s->w.parts_bytes)
-                                 : TiledPlan{};
-    if (rows_f32(p_head) && gemm_rows_f32_norm_supported(batch, (int)c.vocab, d)) {
-      RowsF32Fusion f;
-      f.gamma = (const float*)(base + sp[0].off); f.eps = c.rms_eps; f.row_map = last_rows;
-      launch_gemm_rows_f32(TILED_PART, x, base + sp[1].off, batch, c.vocab, d, 1, logits, st, f);
-    } else {
-      launch_rmsnorm(dt, x, base + sp[0].off, y, batch, d, c.rms_eps, last_rows, st);
-      if (p_head.splits) launch_gemm_tiled(dt, TILED_PART, p_head, y, base + sp[1].off, batch, c.vocab, d, logits, RopeAppend{}, st, parts);
-      else launch_gemm(dt, EPI_F32, y, base + sp[1].off, batch, c.vocab, d, logits, nullptr, st, &gsc);
+    // rows of the head: the sequences' last ones, or all nodes, which without logits_out go max_batch at a time, as many as the
+    // workspace has logits for
+    const int heads = trees ? rows : batch, at_once = logits_out ? heads : std::min(heads, (int)c.max_batch);
+    for (int r0 = 0; r0 < heads; r0 += at_once) {
+      const int n = std::min(at_once, heads - r0);
+      const int32_t* map = trees ? nullptr : last_rows;
+      const float* xr = x + (size_t)r0 * d;
+      float* logits = logits_out ? logits_out : (float*)(ws + s->w.logits);
+      const TiledPlan p_head = (dt == F32 || n > (d > 4096 ? 8 : 16)) && ((uintptr_t)logits & 15) == 0
+                                   ? gemm_tiled_plan(dt, TILED_PART, n, (int)c.vocab, d, false, 0, nullptr, s->w.parts_bytes)
+                                   : TiledPlan{};
+      if (rows_f32(p_head) && gemm_rows_f32_norm_supported(n, (int)c.vocab, d)) {
+        RowsF32Fusion f;
+        f.gamma = (const float*)(base + sp[0].off); f.eps = c.rms_eps; f.row_map = map;
+        launch_gemm_rows_f32(TILED_PART, xr, base + sp[1].off, n, c.vocab, d, 1, logits, st, f);
+      } else {
+        launch_rmsnorm(dt, xr, base + sp[0].off, y, n, d, c.rms_eps, map, st);
+        if (p_head.splits) launch_gemm_tiled(dt, TILED_PART, p_head, y, base + sp[1].off, n, c.vocab, d, logits, RopeAppend{}, st, parts);
+        else launch_gemm(dt, EPI_F32, y, base + sp[1].off, n, c.vocab, d, logits, nullptr, st, &gsc);
+      }
+      launch_argmax(logits, n, c.vocab, (int32_t*)out + r0, st);
     }
-    launch_argmax(logits, batch, c.vocab, (int32_t*)out, st);
   }
 
   if (!rows_one_pass) {
     if (prefill) launch_seq_lens_set(cu_dev, batch, kv->seq_lens, st);
-    else launch_seq_lens_inc(batch, c.max_seq, kv->seq_lens, st);
+    else if (!trees) launch_seq_lens_inc(batch, c.max_seq, kv->seq_lens, st);
   }
   if (timed) LS_HIP(hipEventRecord(s->pass_end, st));
   LS_HIP(hipGetLastError());
@@ -1071,6 +1090,27 @@ ls_status ls_stage_decode(ls_stage* s, const void* in, int batch, int max_ctx, c
   // max_len of a decode step: the keys a row may attend to (cached ones plus its own)
   return forward(s, false, in, nullptr, batch, batch, max_ctx + 1, kv, out, logits_out, (hipStream_t)hip_stream,
                  workspace_scratch(s));
+}
+
+ls_status ls_stage_tree(ls_stage* s, const void* in, const ls_tree* tree, int batch, int max_ctx, const ls_kv* kv, void* out, float* logits_out,
+                        void* hip_stream) {
+  static const char* who = "ls_stage_tree";
+  ls_status rc = check_state(who, s, batch);
+  if (rc != LS_OK) return rc;
+  ls::TreeAttn a;
+  int min_nodes = 0;
+  if (const char* e = ls::tree_error(tree, batch, (int)s->cfg.max_batch, true, &a.rows, &min_nodes, &a.max_nodes)) return ls::bad(who, e);
+  if (a.rows == 0) return LS_OK;
+  rc = check_pointers(who, s, in, kv, out, logits_out);
+  if (rc != LS_OK) return rc;
+  if (a.rows > (int)s->cfg.max_tokens) return fail(LS_ERR_INVALID_ARG, "%s: %d nodes, max_tokens is %u", who, a.rows, s->cfg.max_tokens);
+  if (max_ctx < 0) return fail(LS_ERR_INVALID_ARG, "%s: max_ctx %d is negative", who, max_ctx);
+  if ((long)max_ctx + min_nodes > (long)s->cfg.max_seq)
+    return fail(LS_ERR_KV_OVERFLOW, "%s: context %d + %d nodes exceed max_seq %u", who, max_ctx, min_nodes, s->cfg.max_seq);
+  a.parents = tree->parents; a.cu = tree->cu_nodes; a.seq_lens = kv->seq_lens; a.batch = batch;
+  a.max_keys = std::min(max_ctx + a.max_nodes, (int)s->cfg.max_seq);
+  a.hq = (int)s->cfg.n_q_heads; a.hkv = (int)s->cfg.n_kv_heads; a.hd = (int)s->cfg.head_dim; a.max_seq = (int)s->cfg.max_seq;
+  return forward(s, false, in, nullptr, batch, a.rows, a.max_keys, kv, out, logits_out, (hipStream_t)hip_stream, workspace_scratch(s), &a);
 }
 
 ls_status ls_stage_decode_static(ls_stage* s, const void* in, int batch, int max_ctx, const ls_kv* kv, void* out,
