@@ -303,9 +303,9 @@ typedef struct {
   const int32_t* cu_nodes_host;
 } ls_tree;
 
-/* Device bytes of scratch with which every ls_tree_attention call of this shape cuts long contexts into as many chunks as
- * pay; 0 if it needs none or the shape is invalid. */
-size_t ls_tree_attention_scratch_bytes(const ls_heads* heads);
+/* Device bytes of scratch with which an ls_tree_attention call of these arguments cuts long contexts into as many chunks as
+ * pay; 0 if it needs none or would be refused. */
+size_t ls_tree_attention_scratch_bytes(const ls_heads* heads, const ls_tree* tree, int batch, int max_ctx);
 
 /*
  * Attention of one layer for the trees' nodes.  Node i of sequence b stands at position seq_lens[b] + depth(i), its key and

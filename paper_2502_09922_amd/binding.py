@@ -114,7 +114,7 @@ _SIGS = {
     "ls_probe_mfma_tflops": (C.c_double, [C.c_int, C.c_int, C.c_void_p, C.c_void_p]),
     "ls_plan_multicast_schedule": (C.c_int, [C.c_int, C.c_int, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int,
                                              C.POINTER(C.c_int)]),
-    "ls_tree_attention_scratch_bytes": (C.c_size_t, [C.POINTER(ls_heads)]),
+    "ls_tree_attention_scratch_bytes": (C.c_size_t, [C.POINTER(ls_heads), C.POINTER(ls_tree), C.c_int, C.c_int]),
     "ls_tree_attention": (C.c_int, [C.POINTER(ls_heads), C.POINTER(ls_tree), C.c_int, C.c_int, _P, _P, C.POINTER(ls_kv), _P, _P, C.c_size_t, _P]),
     "ls_stage_tree": (C.c_int, [_P, _P, C.POINTER(ls_tree), C.c_int, C.c_int, C.POINTER(ls_kv), _P, _P, _P]),
     "ls_tree_accept": (C.c_int, [C.POINTER(ls_tree), C.c_int, _P, _P, _P, _P, _P, _P, _P]),
@@ -240,7 +240,7 @@ def tree_attention(qkv, parents, cu_nodes, cu_nodes_host, rope, k, v, seq_lens, 
     if out is None:
         out = torch.empty(rows, hq * hd, dtype=k.dtype, device=device)
     to = _tensor("out", out, k.dtype, device, rows * hq * hd)
-    nb = lib.ls_tree_attention_scratch_bytes(C.byref(heads))
+    nb = lib.ls_tree_attention_scratch_bytes(C.byref(heads), C.byref(tree), batch, max_ctx)
     scratch = torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
     _run(device, lib.ls_tree_attention, C.byref(heads), C.byref(tree), batch, max_ctx, q, turn, C.byref(kv), to,
          scratch.data_ptr() if nb else None, nb)

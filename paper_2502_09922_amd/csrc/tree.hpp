@@ -5,6 +5,14 @@
 
 namespace ls {
 
+// Chunks of the keys that workgroups of their own take, and where they leave their results.
+struct TreeChunks {
+  int n = 1, keys = 0;   // keys of a chunk: a multiple of 64
+  float* o = nullptr;    // [chunk][row * hq + head][head_dim], not normalised
+  float2* ml = nullptr;  // [chunk][row * hq + head]: maximum in score units, sum
+};
+void launch_tree_attn_bf16(const TreeAttn& a, const TreeChunks& p, hipStream_t st);  // head_dim 64 and 128
+
 constexpr int TREE_MAX = 64;  // LS_TREE_MAX: a node for each lane, a bit of a 64-bit mask for each node
 
 struct TreeSeq {

@@ -3,8 +3,10 @@
 // Node i of a sequence with c cached positions stands at position c + depth(i) and takes cache slot c + i.  Its query sees the c
 // cached keys and the slots of the nodes on its path from the root, itself included.
 //
-// Kernels for every shape: one rotates and appends the nodes' keys and values, one attends, a wavefront to a (row, query head).
+// Here the kernels for every shape (the fast ones: tree_attn_bf16.hip): one rotates and appends the nodes' keys and values, one attends, a wavefront to a (row, query head).
 #include "tree.hpp"
+
+#include <algorithm>
 
 namespace ls {
 
@@ -122,12 +124,47 @@ void launch_any(const TreeAttn& a, hipStream_t st) {
                                                                   a.hkv, a.hd, a.max_seq, (const T*)a.kc, (const T*)a.vc, (T*)a.out);
 }
 
+// Chunks of a call.  One workgroup to a (sequence, kv head, block of columns) where they fill the chip, two to a CU; fewer are
+// cut along the keys, into pieces of CHUNK_MIN keys at least.
+constexpr int WG_TARGET = 512, CHUNK_MIN = 256;
+TreeChunks chunks_for(const TreeAttn& a) {
+  TreeChunks p;
+  const int cols = a.max_nodes * (a.hq / a.hkv), wide = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  const long base = (long)a.batch * a.hkv * ((cols + wide - 1) / wide);
+  const long want = std::min((WG_TARGET + base - 1) / base, (long)(a.max_keys + CHUNK_MIN - 1) / CHUNK_MIN);
+  p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
+  p.n = (a.max_keys + p.keys - 1) / p.keys;
+  return p;
+}
+size_t chunk_bytes(const TreeAttn& a, int n) { return (size_t)n * a.rows * a.hq * (a.hd + 2) * sizeof(float); }
+
+bool fast(uint32_t dt, const TreeAttn& a) {
+  const uintptr_t at = (uintptr_t)a.qkv | (uintptr_t)a.kc | (uintptr_t)a.vc | (uintptr_t)a.out | (uintptr_t)a.cs;
+  return dt == BF16 && (a.hd == 64 || a.hd == 128) && (at & 15) == 0 && a.batch <= 65535 && (long)a.max_nodes * a.hq <= 65535;
+}
+
 }  // namespace
 
-size_t tree_attn_scratch_bytes(uint32_t, int, int, int, int, int) { return 0; }
+size_t tree_attn_scratch_bytes(uint32_t dt, const TreeAttn& a) {
+  if (!fast(dt, a)) return 0;
+  const TreeChunks p = chunks_for(a);
+  return p.n > 1 ? chunk_bytes(a, p.n) : 0;
+}
 
 void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st) {
   if (a.rows <= 0) return;
+  if (fast(dt, a)) {
+    TreeChunks p = chunks_for(a);
+    if (p.n > 1 && (!a.scratch || chunk_bytes(a, p.n) > a.scratch_bytes)) {  // as many as there is room for
+      const int fit = a.scratch ? (int)(a.scratch_bytes / chunk_bytes(a, 1)) : 0;
+      p.keys = ((a.max_keys + std::max(fit, 1) - 1) / std::max(fit, 1) + 63) / 64 * 64;
+      p.n = (a.max_keys + p.keys - 1) / p.keys;
+    }
+    p.ml = (float2*)a.scratch;
+    p.o = a.scratch ? a.scratch + ((size_t)p.n * a.rows * a.hq * 2) : nullptr;
+    launch_tree_attn_bf16(a, p, st);
+    return;
+  }
   if (dt == F32) launch_any<float>(a, st);
   else launch_any<bf16>(a, st);
 }

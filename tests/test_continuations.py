@@ -32,7 +32,7 @@ def attention(h=None, t=None, batch=3, max_ctx=36, qkv=HERE, rope=HERE, k=HERE, 
                                    dict(max_batch=0), dict(max_seq=0), dict(max_seq=(1 << 24) + 1)], ids=str)
 def test_heads(wrong):
     assert attention(heads(**wrong)) == b.LS_ERR_INVALID_ARG
-    assert b.lib.ls_tree_attention_scratch_bytes(C.byref(heads(**wrong))) == 0
+    assert b.lib.ls_tree_attention_scratch_bytes(C.byref(heads(**wrong)), C.byref(tree()), 3, 36) == 0
 
 
 @pytest.mark.parametrize("counts,start", [((5, 65, 1), 0), ((5, -1, 3), 0), ((5, 1, 1), 1)])
