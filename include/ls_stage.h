@@ -363,9 +363,10 @@ ls_status ls_tree_keep(const ls_heads* heads, int layers, const ls_tree* tree, i
 /*
  * The k best continuations of each of `groups` requests with `beams` beams (both 1..LS_BEAMS_MAX): row g * beams + b is beam b
  * of request g, candidate (b, token) scores scores[row] + logits[row][token] - log(sum(exp(logits[row]))).  Best first; equal
- * scores go by the lower b * vocab + token.  Scores are compared in 64 bits (the sums of exponentials are of fp32
- * terms) and rounded to fp32 on output.  A beam of score -inf has no candidates but at -inf, and so has one whose logits make the sum
- * NaN or infinite; where candidates above -inf do not suffice those come in the order of their index.
+ * scores go by the lower beam, then the larger logit, then the lower token.  Scores are compared in 64 bits (the sums of
+ * exponentials are of fp32 terms) and rounded to fp32 on output.  A beam whose score is not finite has no candidates but at -inf,
+ * and so has one without a finite sum, all of its logits -inf, or one of them NaN or +inf; where candidates above -inf do not
+ * suffice, those come in the order of beam and token.
  *   logits [groups * beams, vocab] fp32, as ls_stage_prefill and ls_stage_decode write them;  scores [groups * beams]
  *   ended  optional int32 [groups * beams]: a beam with a nonzero entry has ended; its one candidate is token eos at its own
  *          score, and its logits are not used

@@ -8,74 +8,274 @@ namespace {
 
 constexpr int BEAMS_MAX = LS_BEAMS_MAX;
 
-// A candidate: its score in 64 bits, its place beam * vocab + token in its request.
-struct Cand {
-  double s;
-  long at;
+// ---- selection in two launches.
+//
+// k_beam_rows reads the logits once.  A row is cut into segments of SEG tokens, a workgroup to each; a thread's EACH tokens of a segment
+// (float4s 256 apart) are a set of which it leaves the largest logit and its float4, the segment leaves its maximum and its sum of
+// exponentials.  k_beam_pick, a workgroup to a request, makes scores of them: the k best candidates of a request lie in the k
+// sets whose best ones are the best, for a candidate of another set has k better ones in front of it.  It chooses those sets and reads
+// their logits again, k x EACH of beams x vocab.
+//
+// Order: the higher score; of equal ones the lower beam, the larger logit, the lower token.  Within a beam that is the order of the
+// logits, so that a set's best is known before its row's sum is.
+//
+// Bound by the one reading: 64 x 5 rows of 50257 tokens (64 MB) @PICK@.
+constexpr int SEG = 8192, EACH = SEG / 256;
+constexpr int LIST = 2048;             // candidates in LDS: >= BEAMS_MAX * EACH
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Set {
+  float m;  // the largest logit of its tokens
+  int at;   // the first token of the float4 that has it
 };
-__device__ __forceinline__ bool before(Cand a, Cand b) { return a.s > b.s || (a.s == b.s && a.at < b.at); }
-__device__ __forceinline__ Cand better(Cand a, Cand b) { return before(a, b) ? a : b; }
+struct SegSum {
+  double l;  // sum of exp(x - m)
+  float m;
+  int pad;
+};
+struct Cand {
+  double s;  // score
+  float x;   // logit
+  int at;    // beam << 24 | token
+};
+constexpr int NONE = 0x7fffffff;  // Cand::at of no candidate
+__device__ __forceinline__ bool before(Cand a, Cand b) {
+  if (a.s != b.s) return a.s > b.s;
+  if (a.at >> 24 != b.at >> 24 || a.x == b.x) return a.at < b.at;
+  return a.x > b.x;
+}
 __device__ __forceinline__ Cand cand_xor(Cand c, int off) {
   Cand o;
   o.s = __shfl_xor(c.s, off);
+  o.x = __shfl_xor(c.x, off);
   o.at = __shfl_xor(c.at, off);
   return o;
 }
 
-// One workgroup to a request: the rows' log-sums, then the best candidate behind the last one, k times.
-__global__ void __launch_bounds__(1024)
-k_beam_select(const float* __restrict__ logits, const float* __restrict__ scores, const int32_t* __restrict__ ended, int beams, int vocab, int k,
-              int eos, int32_t* __restrict__ rows_out, int32_t* __restrict__ tokens, float* __restrict__ scores_out) {
-  constexpr int NT = 1024, NW = NT / 64;
-  __shared__ double part[NW], base[BEAMS_MAX];
-  __shared__ float top[NW], most[BEAMS_MAX];
-  __shared__ Cand best[NW];
-  const int g = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = 0; b < beams; ++b) {
-    const float* x = logits + ((size_t)g * beams + b) * vocab;
-    float m = -INFINITY;
-    for (int i = threadIdx.x; i < vocab; i += NT) m = fmaxf(m, x[i]);
-    m = exchange<32, 1>(m, Max{});
-    if (lane == 0) top[wave] = m;
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) m = fmaxf(m, top[w]);
-    double s = 0.;
-    for (int i = threadIdx.x; i < vocab; i += NT) s += (double)__expf(x[i] - m);
-    for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off);
-    if (lane == 0) part[wave] = s;
-    __syncthreads();
-    s = 0.;
-    for (int w = 0; w < NW; ++w) s += part[w];
-    if (threadIdx.x == 0) {  // the largest logit apart: next to a large one the rest would be lost
-      base[b] = (double)scores[g * beams + b] - log(s);
-      most[b] = m;
+__global__ void __launch_bounds__(256)
+k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended, int vocab, int nseg, Set* __restrict__ sets, SegSum* __restrict__ sums) {
+  typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));  // a row may start anywhere
+  const int row = blockIdx.x, seg = blockIdx.y, tid = threadIdx.x;
+  if (ended && ended[row]) return;  // its logits are not used
+  const float* x = logits + (size_t)row * vocab;
+  const int first = seg * SEG + tid * 4;
+  f32x4 v[EACH / 4];
+#pragma unroll
+  for (int j = 0; j < EACH / 4; ++j) {
+    const int at = first + j * 1024;
+    v[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    if (at + 4 <= vocab) {
+      v[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4u*>(x + at));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (at + e < vocab) v[j][e] = x[at + e];
     }
-    __syncthreads();
   }
-  Cand last{INFINITY, -1};
-  for (int j = 0; j < k; ++j) {
-    Cand mine{-INFINITY, (long)beams * vocab};
-    for (int b = 0; b < beams; ++b) {
-      const float* x = logits + ((size_t)g * beams + b) * vocab;
-      const bool end = ended && ended[g * beams + b];
-      for (int i = threadIdx.x; i < vocab; i += NT) {
-        Cand c{end ? (i == eos ? (double)scores[g * beams + b] : -INFINITY) : ((double)x[i] - (double)most[b]) + base[b], (long)b * vocab + i};
-        if (!(c.s == c.s)) c.s = -INFINITY;
-        if (before(last, c)) mine = better(mine, c);
+  float m = -INFINITY;
+  int best = first;
+#pragma unroll
+  for (int j = 0; j < EACH / 4; ++j) {
+    const float mj = fmaxf(fmaxf(v[j][0], v[j][1]), fmaxf(v[j][2], v[j][3]));
+    if (mj > m) {
+      m = mj;
+      best = first + j * 1024;
+    }
+  }
+  sets[((size_t)row * nseg + seg) * 256 + tid] = Set{m, best};
+  // sums behind the workgroup's maximum; the difference before the product, whose rounding then is each addend's own
+  __shared__ float top[4];
+  __shared__ double part[4];
+  float M = exchange<32, 1>(m, Max{});
+  if ((tid & 63) == 0) top[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  const float ref = M == -INFINITY ? 0.f : M;
+  float l = 0.f;
+#pragma unroll
+  for (int j = 0; j < EACH / 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) l += __builtin_amdgcn_exp2f((v[j][e] - ref) * LOG2E);
+  double s = l;
+#pragma unroll
+  for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off);
+  if ((tid & 63) == 0) part[tid >> 6] = s;
+  __syncthreads();
+  if (tid == 0) sums[(size_t)row * nseg + seg] = SegSum{(part[0] + part[1]) + (part[2] + part[3]), M, 0};
+}
+
+__global__ void __launch_bounds__(1024)
+k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, const int32_t* __restrict__ ended, int beams, int vocab, int k, int eos,
+            int nseg, const Set* __restrict__ sets, const SegSum* __restrict__ sums, int32_t* __restrict__ rows_out, int32_t* __restrict__ tokens,
+            float* __restrict__ scores_out) {
+  constexpr int NT = 1024;
+  enum { DEAD = 0, LIVE = 1, ENDED = 2 };
+  __shared__ double base[BEAMS_MAX];  // score - log(sum)
+  __shared__ float most[BEAMS_MAX];   // the largest logit; of an ended beam the score
+  __shared__ int state[BEAMS_MAX], chosen[BEAMS_MAX], count;
+  __shared__ Cand some[64], bound, list[LIST];
+  __shared__ int id[LIST];
+  const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const size_t row0 = (size_t)g * beams;
+  if (tid < beams) {
+    const size_t r = row0 + tid;
+    const float score = scores[r];
+    if (ended && ended[r]) {
+      state[tid] = score < INFINITY && score > -INFINITY ? ENDED : DEAD;
+      most[tid] = score;
+    } else {
+      float M = -INFINITY;
+      for (int s = 0; s < nseg; ++s) M = fmaxf(M, sums[r * nseg + s].m);
+      double l = 0.;
+      for (int s = 0; s < nseg; ++s) {
+        const SegSum p = sums[r * nseg + s];
+        l += p.m == -INFINITY ? p.l : p.l * exp((double)p.m - (double)M);
+      }
+      const double b = (double)score - log(l);
+      // all others have no candidate above -inf: nothing left of their logits, or one that makes the sum none
+      state[tid] = M < INFINITY && M > -INFINITY && b < INFINITY && b > -INFINITY ? LIVE : DEAD;
+      base[tid] = b;
+      most[tid] = M;
+    }
+  }
+  if (tid == 0) count = 0;
+  __syncthreads();
+
+  const int C = nseg * 256, N = beams * C;
+  auto score_of = [&](int beam, float x, int token) {
+    Cand c{-INFINITY, 0.f, beam << 24 | token};
+    if (state[beam] == LIVE) {
+      c.s = ((double)x - (double)most[beam]) + base[beam];  // x apart from the rest: next to a large one that would be lost
+      c.x = x;
+    } else if (state[beam] == ENDED && token == eos) {
+      c.s = most[beam];
+    }
+    return c;
+  };
+  // the best of set e.  Its token is that of a float4: sets share none, so that it orders them
+  auto best_of = [&](int e) {
+    const int beam = (int)((unsigned)e / (unsigned)C), c = e - beam * C, first = (c >> 8) * SEG + (c & 255) * 4;
+    if (first >= vocab) return Cand{-INFINITY, 0.f, NONE};
+    if (state[beam] == LIVE) {
+      const Set s = sets[(row0 + beam) * C + c];
+      return score_of(beam, s.m, s.at);
+    }
+    const bool has_eos = eos >= first && eos < (c >> 8) * SEG + SEG && (((eos - first) >> 2) & 255) == 0;
+    Cand out = score_of(beam, 0.f, first);
+    if (state[beam] == ENDED && has_eos) out = score_of(beam, 0.f, eos);
+    return out;
+  };
+
+  // ---- a bound: the k-th best of 64 parts' best sets
+  Cand mine{-INFINITY, 0.f, NONE};
+  for (int e = tid; e < N; e += NT) {
+    const Cand c = best_of(e);
+    if (before(c, mine)) mine = c;
+  }
+#pragma unroll
+  for (int off = 8; off; off >>= 1) {
+    const Cand c = cand_xor(mine, off);
+    if (before(c, mine)) mine = c;
+  }
+  if ((tid & 15) == 0) some[tid >> 4] = mine;
+  __syncthreads();
+  // how many of n candidates stand before the one at i (a copy in front of it counts as one); no more than k are counted for sure
+  auto rank_of = [&](const Cand* of, int n, int i) {
+    const Cand c = of[i];
+    int r = 0;
+    for (int j = 0; j < n; ++j) {
+      const Cand o = of[j];
+      r += before(o, c) || (j < i && !before(c, o));
+      if ((j & 31) == 31 && __builtin_amdgcn_ballot_w64(r < k) == 0) break;
+    }
+    return r;
+  };
+  if (tid < 64 && rank_of(some, 64, lane) == k - 1) bound = some[lane];
+  __syncthreads();
+
+  // ---- the sets that are no worse, and the k best of them
+  const Cand lowest = bound;
+  for (int e = tid; e < N; e += NT) {
+    const Cand c = best_of(e);
+    if (c.at != NONE && !before(lowest, c)) {
+      const int to = atomicAdd(&count, 1);
+      if (to < LIST) {
+        list[to] = c;
+        id[to] = e;
       }
     }
-    for (int off = 32; off; off >>= 1) mine = better(mine, cand_xor(mine, off));
-    if (lane == 0) best[wave] = mine;
-    __syncthreads();
-    for (int w = 0; w < NW; ++w) mine = better(mine, best[w]);
-    last = mine;
-    if (threadIdx.x == 0) {
-      const size_t to = (size_t)g * k + j;
-      rows_out[to] = g * beams + (int)(last.at / vocab);
-      tokens[to] = (int)(last.at % vocab);
-      scores_out[to] = (float)last.s;
+  }
+  __syncthreads();
+  const int found = count, sel = min(found, k);
+  if (found <= LIST) {
+    for (int i = tid; i < found; i += NT) {
+      const int r = rank_of(list, found, i);
+      if (r < sel) chosen[r] = id[i];
+      if (r == sel - 1) bound = list[i];
     }
-    __syncthreads();
+  } else {  // more than there is room for, as in many equal ones: one after the other
+    __shared__ int at[16];
+    Cand last{INFINITY, 0.f, -1};
+    for (int j = 0; j < sel; ++j) {
+      mine = Cand{-INFINITY, 0.f, NONE};
+      int set = -1;
+      for (int e = tid; e < N; e += NT) {
+        const Cand c = best_of(e);
+        if (before(last, c) && before(c, mine)) {
+          mine = c;
+          set = e;
+        }
+      }
+      for (int off = 32; off; off >>= 1) {
+        const Cand c = cand_xor(mine, off);
+        const int o = __shfl_xor(set, off);
+        if (before(c, mine)) {
+          mine = c;
+          set = o;
+        }
+      }
+      if (lane == 0) {
+        some[tid >> 6] = mine;
+        at[tid >> 6] = set;
+      }
+      __syncthreads();
+      for (int w = 0; w < NT / 64; ++w)
+        if (!before(mine, some[w])) {
+          mine = some[w];
+          set = at[w];
+        }
+      last = mine;
+      if (tid == 0) {
+        chosen[j] = set;
+        bound = mine;
+      }
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+  if (tid == 0) count = 0;
+  __syncthreads();
+
+  // ---- the tokens of the chosen sets: the k-th best set's best one bounds the k-th best token
+  Cand least = bound;
+  least.at |= 3;  // the last token of its float4 that may be it
+  for (int i = tid; i < sel * EACH; i += NT) {
+    const int e = chosen[i / EACH], q = i % EACH;
+    const int beam = (int)((unsigned)e / (unsigned)C), c = e - beam * C, token = (c >> 8) * SEG + (c & 255) * 4 + (q >> 2) * 1024 + (q & 3);
+    if (token >= vocab) continue;
+    const Cand d = score_of(beam, state[beam] == LIVE ? logits[(row0 + beam) * vocab + token] : 0.f, token);
+    if (sel < k || !before(least, d)) list[atomicAdd(&count, 1)] = d;
+  }
+  __syncthreads();
+  const int n = count;
+  for (int i = tid; i < n; i += NT) {
+    const int r = rank_of(list, n, i);
+    if (r < k) {
+      const size_t to = (size_t)g * k + r;
+      rows_out[to] = (int)row0 + (list[i].at >> 24);
+      tokens[to] = list[i].at & 0xffffff;
+      scores_out[to] = (float)list[i].s;
+    }
   }
 }
 
@@ -156,7 +356,10 @@ bool select_ok(int groups, int beams, int vocab, int k) {
 
 extern "C" {
 
-size_t ls_beam_select_scratch_bytes(int groups, int beams, int vocab, int k) { return select_ok(groups, beams, vocab, k) ? 256 : 0; }
+size_t ls_beam_select_scratch_bytes(int groups, int beams, int vocab, int k) {
+  if (!select_ok(groups, beams, vocab, k)) return 0;
+  return (size_t)groups * beams * ((vocab + ls::SEG - 1) / ls::SEG) * (256 * sizeof(ls::Set) + sizeof(ls::SegSum));
+}
 
 ls_status ls_beam_select(const float* logits, const float* scores, const int32_t* ended, int groups, int beams, int vocab, int k, int eos,
                          int32_t* rows, int32_t* tokens, float* scores_out, void* scratch, size_t scratch_bytes, void* hip_stream) {
@@ -170,7 +373,12 @@ ls_status ls_beam_select(const float* logits, const float* scores, const int32_t
     ls::set_last_error("%s: scratch too small", who);
     return LS_ERR_OOM;
   }
-  ls::k_beam_select<<<groups, 1024, 0, (hipStream_t)hip_stream>>>(logits, scores, ended, beams, vocab, k, eos, rows, tokens, scores_out);
+  const int nseg = (vocab + ls::SEG - 1) / ls::SEG, n = groups * beams;
+  ls::SegSum* sums = (ls::SegSum*)scratch;
+  ls::Set* sets = (ls::Set*)(sums + (size_t)n * nseg);
+  hipStream_t st = (hipStream_t)hip_stream;
+  ls::k_beam_rows<<<dim3(n, nseg), 256, 0, st>>>(logits, ended, vocab, nseg, sets, sums);
+  ls::k_beam_pick<<<groups, 1024, 0, st>>>(logits, scores, ended, beams, vocab, k, eos, nseg, sets, sums, rows, tokens, scores_out);
   return launched(who);
 }
 

@@ -114,3 +114,12 @@ def test_reorder(heads, dtype, group):
             wl[b] = lens[s]
         # positions behind max_ctx may move or not
         assert torch.equal(gk.cpu()[..., :45, :], wk[..., :45, :]) and torch.equal(gv.cpu()[..., :45, :], wv[..., :45, :]) and torch.equal(gl.cpu(), wl)
+
+
+@pytest.mark.parametrize("beams,vocab,k", [(1, 40000, 64), (8, 9001, 40), (64, 300, 64), (64, 4000, 50)])
+def test_the_best_lie_side_by_side(beams, vocab, k):
+    """Logits that fall along the vocabulary, and all alike: the best candidates, or as good ones, are many in few places."""
+    fall = -torch.arange(vocab).float() / 1000
+    check(fall.repeat(beams, 1), -torch.arange(beams).float() / 1e5, beams, k)
+    check(torch.zeros(beams, vocab), torch.zeros(beams), beams, k)
+    check(torch.full((beams, vocab), -math.inf), torch.zeros(beams), beams, k)
