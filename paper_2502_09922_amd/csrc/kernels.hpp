@@ -329,7 +329,7 @@ struct TreeAttn {
   float* scratch = nullptr;  // partial results of contexts cut into chunks, or null
   size_t scratch_bytes = 0;
 };
-size_t tree_attn_scratch_bytes(uint32_t dt, const TreeAttn& a);  // for as many chunks as pay
+size_t tree_attn_scratch_bytes(const TreeAttn& a);  // for as many chunks as pay
 void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st);
 
 // tok[r] = index of the largest logit of row r, lowest index on ties.

@@ -135,7 +135,7 @@ size_t ls_tree_attention_scratch_bytes(const ls_heads* h, const ls_tree* tree, i
   if (max_ctx < 0 || a.rows == 0 || (long)max_ctx + min_nodes > (long)h->max_seq) return 0;
   a.batch = batch; a.max_keys = std::min(max_ctx + a.max_nodes, (int)h->max_seq);
   a.hq = (int)h->n_q_heads; a.hkv = (int)h->n_kv_heads; a.hd = (int)h->head_dim; a.max_seq = (int)h->max_seq;
-  return ls::tree_attn_scratch_bytes(h->dtype, a);
+  return ls::tree_attn_scratch_bytes(a);
 }
 
 ls_status ls_tree_attention(const ls_heads* h, const ls_tree* tree, int batch, int max_ctx, const void* qkv, const float* rope, const ls_kv* layer,

@@ -11,7 +11,7 @@ struct TreeChunks {
   float* o = nullptr;    // [chunk][row * hq + head][head_dim], not normalised
   float2* ml = nullptr;  // [chunk][row * hq + head]: maximum in score units, sum
 };
-void launch_tree_attn_bf16(const TreeAttn& a, const TreeChunks& p, hipStream_t st);  // head_dim 64 and 128
+void launch_tree_attn_mfma(uint32_t dt, const TreeAttn& a, const TreeChunks& p, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
 
 constexpr int TREE_MAX = 64;  // LS_TREE_MAX: a node for each lane, a bit of a 64-bit mask for each node
 

@@ -3,7 +3,7 @@
 // Node i of a sequence with c cached positions stands at position c + depth(i) and takes cache slot c + i.  Its query sees the c
 // cached keys and the slots of the nodes on its path from the root, itself included.
 //
-// Here the kernels for every shape (the fast ones: tree_attn_bf16.hip): one rotates and appends the nodes' keys and values, one attends, a wavefront to a (row, query head).
+// Here the kernels for every shape (the fast ones: tree_attn_mfma.hip): one rotates and appends the nodes' keys and values, one attends, a wavefront to a (row, query head).
 #include "tree.hpp"
 
 #include <algorithm>
@@ -138,22 +138,22 @@ TreeChunks chunks_for(const TreeAttn& a) {
 }
 size_t chunk_bytes(const TreeAttn& a, int n) { return (size_t)n * a.rows * a.hq * (a.hd + 2) * sizeof(float); }
 
-bool fast(uint32_t dt, const TreeAttn& a) {
+bool fast(const TreeAttn& a) {
   const uintptr_t at = (uintptr_t)a.qkv | (uintptr_t)a.kc | (uintptr_t)a.vc | (uintptr_t)a.out | (uintptr_t)a.cs;
-  return dt == BF16 && (a.hd == 64 || a.hd == 128) && (at & 15) == 0 && a.batch <= 65535 && (long)a.max_nodes * a.hq <= 65535;
+  return (a.hd == 64 || a.hd == 128) && (at & 15) == 0 && a.batch <= 65535 && (long)a.max_nodes * a.hq <= 65535;
 }
 
 }  // namespace
 
-size_t tree_attn_scratch_bytes(uint32_t dt, const TreeAttn& a) {
-  if (!fast(dt, a)) return 0;
+size_t tree_attn_scratch_bytes(const TreeAttn& a) {
+  if (!fast(a)) return 0;
   const TreeChunks p = chunks_for(a);
   return p.n > 1 ? chunk_bytes(a, p.n) : 0;
 }
 
 void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st) {
   if (a.rows <= 0) return;
-  if (fast(dt, a)) {
+  if (fast(a)) {
     TreeChunks p = chunks_for(a);
     if (p.n > 1 && (!a.scratch || chunk_bytes(a, p.n) > a.scratch_bytes)) {  // as many as there is room for
       const int fit = a.scratch ? (int)(a.scratch_bytes / chunk_bytes(a, 1)) : 0;
@@ -162,7 +162,7 @@ void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st) {
     }
     p.ml = (float2*)a.scratch;
     p.o = a.scratch ? a.scratch + ((size_t)p.n * a.rows * a.hq * 2) : nullptr;
-    launch_tree_attn_bf16(a, p, st);
+    launch_tree_attn_mfma(dt, a, p, st);
     return;
   }
   if (dt == F32) launch_any<float>(a, st);

@@ -1,18 +1,21 @@
-// bf16 attention of draft trees on the matrix cores (head_dim 64 and 128).
+// Attention of draft trees on the matrix cores (head_dim 64 and 128).
 //
 // Nodes x query heads of a kv head are the columns of both products, all of which see the cached keys:
-//   S^T[key][column] = K Q^T        v_mfma_f32_16x16x32_bf16, A = 16 key rows, B = 16 columns
-//   O^T[dim][column] += V^T P^T     A = V^T by transposing LDS reads of the row-major tile, B = P^T
+//   S^T[key][column] = K Q^T        A = 16 key rows, B = 16 columns
+//   O^T[dim][column] += V^T P^T     A = V^T, B = P^T
 // A lane of a result holds column lane % 16 and rows 4 (lane / 16) + e: one column's running maximum and sum are per-lane values
-// and exchanges with lanes +-16 and +-32, and the eight weights a lane has for 32 keys are a B operand whose k index runs over
-// keys {4g..4g+3, 16+4g..16+4g+3}, g = lane / 16.
-//
-// Queries are turned in fp32 and enter as a sum of two bf16 (16 bits and more of them): rounded once they would move every score by
-// 2^-9 of its size, which costs more than the rounding of the output.  Weights are rounded to bf16 for the second product (their
-// sum is of the unrounded ones), as the prompt kernel does.
+// and exchanges with lanes +-16 and +-32, and the weights that a lane has are a B operand as they are.
+//   bf16: v_mfma_f32_16x16x32_bf16, steps of 32 keys.  The k index of the second product runs over keys {4g..4g+3, 16+4g..16+4g+3},
+// g = lane / 16; V^T comes out of transposing LDS reads of the row-major tile.  Queries are turned in fp32 and enter as a sum of two
+// bf16 (16 bits and more of them): rounded once they would move every score by 2^-9 of its size, which costs more than the
+// rounding of the output.  Weights are rounded to bf16 for the second product (their sum is of the unrounded ones), as the prompt
+// kernel does.
+//   fp32: v_mfma_f32_16x16x4_f32, steps of 16 keys.  The k index is lane / 16; a 16-byte read of a key's or a value's row serves four
+// products, of dims 16 j + 4 g + e of a key, and of rows 64 j + 4 (lane % 16) + e of V^T, which are the dims that a result's
+// lane holds 4 apart.
 //
 // A workgroup is a (sequence, kv head, block of columns, chunk of keys).  Of its four wavefronts CW share keys, each with columns
-// of its own, and 4 / CW split the chunk's keys.  Up to 16 columns each walks keys of its own, 32 at a time through registers into LDS of
+// of its own, and 4 / CW split the chunk's keys.  Up to 16 columns each walks keys of its own, a step at a time through registers into LDS of
 // its own, no barriers (CW = 1); wavefronts that share keys fill double-buffered tiles together.  The splits' results are joined
 // through LDS, chunks' by a second kernel, both in order.
 //
@@ -22,6 +25,7 @@
 #include "tree.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ls {
 
@@ -33,41 +37,76 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // 16-byte chunks of a row of a tile are permuted by its key, so that 16 rows' equal chunks (keys) and 4 rows' 32 bytes (values,
 // transposing) lie in different banks.
-template <int HD> __device__ __forceinline__ int key_swizzle(int key) { return HD == 128 ? key & 15 : ((key & 3) << 1) | ((key >> 2) & 1); }
-template <int HD> __device__ __forceinline__ int value_swizzle(int key) { return HD == 128 ? (key & 7) << 1 : ((key & 3) << 1) | ((key >> 2) & 1); }
+template <class T, int HD> __device__ __forceinline__ int key_swizzle(int key) { return HD == 128 || sizeof(T) == 4 ? key & 15 : ((key & 3) << 1) | ((key >> 2) & 1); }
+template <class T, int HD> __device__ __forceinline__ int value_swizzle(int key) {
+  return sizeof(T) == 4 ? 0 : HD == 128 ? (key & 7) << 1 : ((key & 3) << 1) | ((key >> 2) & 1);
+}
 
 // Values that are no numbers become zeros; whether there were any.
+template <class T>
 __device__ __forceinline__ bool drop_nonfinite(u32x4& v) {
   bool any = false;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool lo = (v[i] & 0x7F80u) == 0x7F80u, hi = (v[i] & 0x7F800000u) == 0x7F800000u;
-    any |= lo || hi;
-    v[i] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+    if constexpr (sizeof(T) == 4) {
+      const bool bad = (v[i] & 0x7F800000u) == 0x7F800000u;
+      any |= bad;
+      v[i] = bad ? 0u : v[i];
+    } else {
+      const bool lo = (v[i] & 0x7F80u) == 0x7F80u, hi = (v[i] & 0x7F800000u) == 0x7F800000u;
+      any |= lo || hi;
+      v[i] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+    }
   }
   return any;
 }
 
+// A 16-byte piece of a row from dim `at` on, turned by its position's table row.
+__device__ __forceinline__ u32x4 turned(u32x4 v, const float* turn, bf16) {
+  const bf16x8 u = __builtin_bit_cast(bf16x8, v);
+  const f32x4 ta = reinterpret_cast<const f32x4*>(turn)[0], tb = reinterpret_cast<const f32x4*>(turn)[1];
+  bf16x8 w;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const float2 c2 = p < 2 ? float2{ta[2 * p], ta[2 * p + 1]} : float2{tb[2 * p - 4], tb[2 * p - 3]};
+    w[2 * p] = (bf16)turn0((float)u[2 * p], (float)u[2 * p + 1], c2);
+    w[2 * p + 1] = (bf16)turn1((float)u[2 * p], (float)u[2 * p + 1], c2);
+  }
+  return __builtin_bit_cast(u32x4, w);
+}
+__device__ __forceinline__ u32x4 turned(u32x4 v, const float* turn, float) {
+  const f32x4 u = __builtin_bit_cast(f32x4, v), c = *reinterpret_cast<const f32x4*>(turn);
+  f32x4 w;
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    w[2 * p] = turn0(u[2 * p], u[2 * p + 1], float2{c[2 * p], c[2 * p + 1]});
+    w[2 * p + 1] = turn1(u[2 * p], u[2 * p + 1], float2{c[2 * p], c[2 * p + 1]});
+  }
+  return __builtin_bit_cast(u32x4, w);
+}
+
 constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns' equal dims in different banks
 
-// Steps of 32 keys in a tile: two where tiles are shared by all and the registers suffice.
-template <int HD, int CT, int CW> constexpr int steps_of() { return CW == 4 && (CT == 1 || HD == 64) ? 2 : 1; }
+template <class T> constexpr int STEP_KEYS = sizeof(T) == 2 ? 32 : 16;
+// Steps in a tile: two where tiles are shared by all and the registers suffice.
+template <class T, int HD, int CT, int CW> constexpr int steps_of() { return CW == 4 && (CT == 1 || HD == 64) ? 2 : 1; }
 
-template <int HD, int CT, int CW>
+template <class T, int HD, int CT, int CW>
 __global__ void __launch_bounds__(256, 2)
-k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ parents, const bf16* __restrict__ qkv,
-            const float* __restrict__ cs, bf16* __restrict__ kc, bf16* __restrict__ vc, bf16* __restrict__ out, int rows, int hq, int hkv, int max_seq,
+k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ parents, const T* __restrict__ qkv,
+            const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, T* __restrict__ out, int rows, int hq, int hkv, int max_seq,
             int nchunk, int chunk_tiles, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   constexpr int KW = 4 / CW;             // wavefronts that split the keys
-  constexpr int SUB = steps_of<HD, CT, CW>();
-  constexpr int TK = 32 * SUB;
-  constexpr int ROWB = HD * 2;
-  constexpr int CPR = HD / 8;            // 16-byte chunks of a row
+  constexpr int SK = STEP_KEYS<T>, SUB = steps_of<T, HD, CT, CW>();
+  constexpr int TK = SK * SUB;
+  constexpr int ROWB = HD * sizeof(T), EPC = 16 / sizeof(T);
+  constexpr int CPR = HD / EPC;          // 16-byte chunks of a row
   constexpr int RPI = 64 / CPR;          // rows that a wavefront's load covers
   constexpr int NL = TK / RPI / CW;      // loads of a wavefront for a tile's keys, as many for its values
   constexpr int TILE = TK * ROWB;
   constexpr int COLS = 16 * CT * CW;     // of a workgroup
-  constexpr int KS = HD / 32, DT = HD / 16;
+  constexpr int DT = HD / 16;
+  typedef T T4 __attribute__((ext_vector_type(4)));
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   const int G = hq / hkv;
@@ -81,7 +120,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     if (z == 0 && cb == 0)
       for (int i = threadIdx.x; i < t.n * G * HD; i += 256) {
         const int c = i / HD;
-        out[((size_t)(t.row0 + c / G) * hq + kh * G + c % G) * HD + i % HD] = (bf16)0.f;
+        out[((size_t)(t.row0 + c / G) * hq + kh * G + c % G) * HD + i % HD] = from_f<T>(0.f);
       }
     return;
   }
@@ -96,9 +135,9 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   const int t_begin = min(t_lo + split * per, t_hi), t_end = min(t_begin + per, t_hi);
 
   const size_t head0 = ((size_t)b * hkv + kh) * max_seq * HD;
-  bf16 *kb = kc + head0, *vb = vc + head0;
+  T *kb = kc + head0, *vb = vc + head0;
   const int stride = (hq + 2 * hkv) * HD;
-  const bf16* rows0 = qkv + (size_t)t.row0 * stride;
+  const T* rows0 = qkv + (size_t)t.row0 * stride;
   const int lrow = lane / CPR, lchunk = lane % CPR;
   const int first_row = share * NL * RPI;  // of a tile, that this wavefront brings
 
@@ -108,8 +147,8 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     const char *kt = (const char*)(kb + (size_t)row0 * HD), *vt = (const char*)(vb + (size_t)row0 * HD);
     auto fetch = [&](int i, int from) {
       const int r = first_row + i * RPI + lrow;
-      const u32x4* kp = reinterpret_cast<const u32x4*>(kt + from * ROWB + (unsigned)((lchunk ^ key_swizzle<HD>(r)) << 4));
-      const u32x4* vp = reinterpret_cast<const u32x4*>(vt + from * ROWB + (unsigned)((lchunk ^ value_swizzle<HD>(r)) << 4));
+      const u32x4* kp = reinterpret_cast<const u32x4*>(kt + from * ROWB + (unsigned)((lchunk ^ key_swizzle<T, HD>(r)) << 4));
+      const u32x4* vp = reinterpret_cast<const u32x4*>(vt + from * ROWB + (unsigned)((lchunk ^ value_swizzle<T, HD>(r)) << 4));
       kreg[i] = CW == 1 ? __builtin_nontemporal_load(kp) : *kp;
       vreg[i] = CW == 1 ? __builtin_nontemporal_load(vp) : *vp;
     };
@@ -133,24 +172,12 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       const int i = i0 + (CW == 1 ? lane : (int)threadIdx.x), key = n_lo + i / CPR, ch = i % CPR, node = min(key - t.ctx, t.n - 1);
       const int d = __shfl(depth, node);
       if (i < items) {
-        const bf16* row = rows0 + (size_t)node * stride + ch * 8;
+        const T* row = rows0 + (size_t)node * stride + ch * EPC;
         u32x4 k = *reinterpret_cast<const u32x4*>(row + (size_t)(hq + kh) * HD);
         const u32x4 v = *reinterpret_cast<const u32x4*>(row + (size_t)(hq + hkv + kh) * HD);
-        if (cs) {
-          const bf16x8 u = __builtin_bit_cast(bf16x8, k);
-          const f32x4* turn = reinterpret_cast<const f32x4*>(cs + (size_t)(t.ctx + d) * HD + ch * 8);
-          const f32x4 ta = turn[0], tb = turn[1];
-          bf16x8 w;
-#pragma unroll
-          for (int p = 0; p < 4; ++p) {
-            const float2 c2 = p < 2 ? float2{ta[2 * p], ta[2 * p + 1]} : float2{tb[2 * p - 4], tb[2 * p - 3]};
-            w[2 * p] = (bf16)turn0((float)u[2 * p], (float)u[2 * p + 1], c2);
-            w[2 * p + 1] = (bf16)turn1((float)u[2 * p], (float)u[2 * p + 1], c2);
-          }
-          k = __builtin_bit_cast(u32x4, w);
-        }
-        *reinterpret_cast<u32x4*>(kb + (size_t)key * HD + ch * 8) = k;
-        *reinterpret_cast<u32x4*>(vb + (size_t)key * HD + ch * 8) = v;
+        if (cs) k = turned(k, cs + (size_t)(t.ctx + d) * HD + ch * EPC, T{});
+        *reinterpret_cast<u32x4*>(kb + (size_t)key * HD + ch * EPC) = k;
+        *reinterpret_cast<u32x4*>(vb + (size_t)key * HD + ch * EPC) = v;
       }
     }
     if constexpr (CW == 1) {
@@ -160,9 +187,11 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     }
   }
 
-  // ---- this wavefront's columns: queries as two bf16 parts, the nodes they see
+  // ---- this wavefront's columns: queries, bf16 as two parts, and the nodes they see
   const int col0 = cb * COLS + share * 16 * CT + lr;
-  bf16x8 qh[CT][KS], ql[CT][KS];
+  constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a key's row
+  typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Q;
+  Q qh[CT][KS], ql[CT][sizeof(T) == 2 ? KS : 1];
   uint64_t sees[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
@@ -171,30 +200,36 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     const int node = in ? col / G : 0;
     sees[c] = (uint64_t)(unsigned)__shfl((int)(unsigned)(path >> 32), node) << 32 | (unsigned)__shfl((int)(unsigned)path, node);
     const int pos = t.ctx + __builtin_popcountll(sees[c]) - 1;
-    const bf16* q = rows0 + (size_t)node * stride + (size_t)(kh * G + (in ? col % G : 0)) * HD;
+    const T* q = rows0 + (size_t)node * stride + (size_t)(kh * G + (in ? col % G : 0)) * HD;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
-      const int d0 = kk * 32 + lg * 8;
-      const bf16x8 raw = *reinterpret_cast<const bf16x8*>(q + d0);
-      float turn[8];
-      if (cs) {
-        const f32x4* cp = reinterpret_cast<const f32x4*>(cs + (size_t)pos * HD + d0);
-        *reinterpret_cast<f32x4*>(turn) = cp[0];
-        *reinterpret_cast<f32x4*>(turn + 4) = cp[1];
-      }
-#pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        float u0 = (float)raw[2 * p], u1 = (float)raw[2 * p + 1];
+      if constexpr (sizeof(T) == 4) {
+        const int d0 = kk * 16 + lg * 4;
+        u32x4 raw = *reinterpret_cast<const u32x4*>(q + d0);
+        if (cs) raw = turned(raw, cs + (size_t)pos * HD + d0, T{});
+        qh[c][kk] = __builtin_bit_cast(f32x4, raw);
+      } else {
+        const int d0 = kk * 32 + lg * 8;
+        const bf16x8 raw = *reinterpret_cast<const bf16x8*>(q + d0);
+        f32x4 ta{}, tb{};
         if (cs) {
-          const float2 c2{turn[2 * p], turn[2 * p + 1]};
-          const float w0 = turn0(u0, u1, c2), w1 = turn1(u0, u1, c2);
-          u0 = w0;
-          u1 = w1;
+          ta = reinterpret_cast<const f32x4*>(cs + (size_t)pos * HD + d0)[0];
+          tb = reinterpret_cast<const f32x4*>(cs + (size_t)pos * HD + d0)[1];
         }
-        qh[c][kk][2 * p] = (bf16)u0;
-        qh[c][kk][2 * p + 1] = (bf16)u1;
-        ql[c][kk][2 * p] = (bf16)(u0 - (float)qh[c][kk][2 * p]);
-        ql[c][kk][2 * p + 1] = (bf16)(u1 - (float)qh[c][kk][2 * p + 1]);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          float u0 = (float)raw[2 * p], u1 = (float)raw[2 * p + 1];
+          if (cs) {
+            const float2 c2 = p < 2 ? float2{ta[2 * p], ta[2 * p + 1]} : float2{tb[2 * p - 4], tb[2 * p - 3]};
+            const float w0 = turn0(u0, u1, c2), w1 = turn1(u0, u1, c2);
+            u0 = w0;
+            u1 = w1;
+          }
+          qh[c][kk][2 * p] = (bf16)u0;
+          qh[c][kk][2 * p + 1] = (bf16)u1;
+          ql[c][kk][2 * p] = (bf16)(u0 - (float)qh[c][kk][2 * p]);
+          ql[c][kk][2 * p + 1] = (bf16)(u1 - (float)qh[c][kk][2 * p + 1]);
+        }
       }
     }
   }
@@ -209,37 +244,51 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     for (int d = 0; d < DT; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const float scale = 1.4426950408889634f / sqrtf((float)HD);  // score -> exponent of 2
+  // four neighbouring dims that a lane holds of a column: i of DT such, from dim_of(i) on
+  auto dim_of = [&](int i) { return sizeof(T) == 2 ? i * 16 + 4 * lg : (i >> 2) * 64 + 16 * lg + 4 * (i & 3); };
+  auto out_at = [&](int c, int i, int e) -> float& {
+    float* at = reinterpret_cast<float*>(&o[c][0]);
+    return sizeof(T) == 2 ? at[i * 4 + e] : at[((i & ~3) + e) * 4 + (i & 3)];
+  };
+  auto piece = [&](int c, int i) { return f32x4{out_at(c, i, 0), out_at(c, i, 1), out_at(c, i, 2), out_at(c, i, 3)}; };
 
-  // ---- 32 keys of a tile in LDS
+  // ---- a step of a tile in LDS
+  constexpr int HALVES = SK / 16;
   auto attend = [&](const unsigned char* ks, const unsigned char* vs, int sub, int key0, bool odd) {
-    f32x4 s[CT][2];
+    f32x4 s[CT][HALVES];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int kl = sub * 32 + h * 16 + lr;
+    for (int h = 0; h < HALVES; ++h) {
+      const int kl = sub * SK + h * 16 + lr;
 #pragma unroll
       for (int c = 0; c < CT; ++c) s[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
-        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<HD>(kl)) << 4));
+        const Q kf = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-          s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, ql[c][kk], s[c][h], 0, 0, 0);
-          s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qh[c][kk], s[c][h], 0, 0, 0);
+          if constexpr (sizeof(T) == 2) {
+            s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, ql[c][kk], s[c][h], 0, 0, 0);
+            s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qh[c][kk], s[c][h], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[c][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qh[c][kk][e], s[c][h], 0, 0, 0);
+          }
         }
       }
     }
-    bf16x8 pf[CT];
     const int behind = key0 - t.ctx;  // of the cached positions
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      if (behind > -32) {  // slots of nodes
+      if (behind > -SK) {  // slots of nodes
         const unsigned seen = behind >= 64 ? 0u : behind >= 0 ? (unsigned)(sees[c] >> behind) : (unsigned)(sees[c] << -behind) | ((1u << -behind) - 1u);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[c][h][e] = seen >> (h * 16 + 4 * lg + e) & 1u ? s[c][h][e] : -INFINITY;
       }
-      float mx = fmaxf(fmaxf(fmaxf(s[c][0][0], s[c][0][1]), fmaxf(s[c][0][2], s[c][0][3])), fmaxf(fmaxf(s[c][1][0], s[c][1][1]), fmaxf(s[c][1][2], s[c][1][3])));
+      float mx = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) mx = fmaxf(mx, fmaxf(fmaxf(s[c][h][0], s[c][h][1]), fmaxf(s[c][h][2], s[c][h][3])));
       mx = exchange<16, 32>(mx, Max{});
       const float m_new = fmaxf(m_run[c], mx), m_ref = m_new == -INFINITY ? 0.f : m_new;
       if (__builtin_amdgcn_ballot_w64(m_new > m_run[c]) != 0) {
@@ -254,43 +303,60 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       const float mc = m_ref * scale;
       float sum = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < HALVES; ++h)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(s[c][h][e], scale, -mc));
-          sum += p;
-          pf[c][h * 4 + e] = (bf16)p;
+          s[c][h][e] = __builtin_amdgcn_exp2f(fmaf(s[c][h][e], scale, -mc));
+          sum += s[c][h][e];
         }
       l_run[c] += sum;
     }
-    const int k0 = sub * 32 + 4 * lg + (lr >> 2), k1 = k0 + 16;
-    const int within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 pf[CT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      const int ch = d * 2 + ((lr & 3) >> 1);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<HD>(k0)) << 4) + within));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k1 * ROWB + ((ch ^ value_swizzle<HD>(k1)) << 4) + within));
-      const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int c = 0; c < CT; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[c], o[c][d], 0, 0, 0);
+        for (int i = 0; i < 8; ++i) pf[c][i] = (bf16)s[c][i >> 2][i & 3];
+      const int k0 = sub * SK + 4 * lg + (lr >> 2), k1 = k0 + 16;
+      const int within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const int ch = d * 2 + ((lr & 3) >> 1);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<T, HD>(k0)) << 4) + within));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k1 * ROWB + ((ch ^ value_swizzle<T, HD>(k1)) << 4) + within));
+        const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int c = 0; c < CT; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[c], o[c][d], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const f32x4 vt = *reinterpret_cast<const f32x4*>(vs + (sub * SK + 4 * lg + e) * ROWB + (j * 16 + lr) * 16);
+#pragma unroll
+          for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[c][j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[d], s[c][0][e], o[c][j * 4 + d], 0, 0, 0);
+        }
     }
     if (odd) {  // nodes' values that are no numbers lie in the tile as zeros: only the columns that see the nodes take them
-      for (int j = max(0, -behind); j < 32 && behind + j < t.n; ++j) {
-        const bf16* v = rows0 + (size_t)(behind + j) * stride + (size_t)(hq + hkv + kh) * HD + 4 * lg;
+      for (int j = max(0, -behind); j < SK && behind + j < t.n; ++j) {
+        const T* v = rows0 + (size_t)(behind + j) * stride + (size_t)(hq + hkv + kh) * HD;
         const int from = ((j >> 2) & 3) * 16 + lr;
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
           float p = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) p = (j >> 4) * 4 + (j & 3) == i ? (float)pf[c][i] : p;
+          for (int i = 0; i < 4 * HALVES; ++i) p = (j >> 4) * 4 + (j & 3) == i ? s[c][i >> 2][i & 3] : p;
           p = __shfl(p, from);
           if (!(sees[c] >> (behind + j) & 1)) continue;
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const bf16x4 x = *reinterpret_cast<const bf16x4*>(v + d * 16);
+          for (int i = 0; i < DT; ++i) {
+            const T4 x = *reinterpret_cast<const T4*>(v + dim_of(i));
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (!(fabsf((float)x[e]) < INFINITY)) o[c][d][e] += p * (float)x[e];
+              if (!(fabsf(to_f(x[e])) < INFINITY)) out_at(c, i, e) += p * to_f(x[e]);
             __builtin_amdgcn_sched_barrier(0);  // rare: no registers for it
           }
         }
@@ -304,7 +370,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     if ((tile + 1) * TK > t.ctx) {
 #pragma unroll
       for (int i = 0; i < NL; ++i)
-        if (tile * TK + first_row + i * RPI + lrow >= t.ctx) odd |= drop_nonfinite(vreg[i]);
+        if (tile * TK + first_row + i * RPI + lrow >= t.ctx) odd |= drop_nonfinite<T>(vreg[i]);
     }
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
@@ -336,7 +402,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
         for (int w = 0; w < CW; ++w) odd |= odd_flags[buf][split * CW + w];
 #pragma unroll 1
         for (int sub = 0; sub < SUB; ++sub)
-          if (i * TK + sub * 32 < keys) attend(ks, vs, sub, i * TK + sub * 32, odd != 0);
+          if (i * TK + sub * SK < keys) attend(ks, vs, sub, i * TK + sub * SK, odd != 0);
       }
       if (i + 1 < t_end) {
         unsigned char* to = tiles + (buf ^ 1) * (2 * TILE);
@@ -360,7 +426,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
         sm_l[split][at] = l;
       }
 #pragma unroll
-      for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(sm_o + (split * COLS + at) * (HD + SM_PAD) + d * 16 + 4 * lg) = o[c][d];
+      for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(sm_o + (split * COLS + at) * (HD + SM_PAD) + dim_of(i)) = piece(c, i);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < COLS * (HD / 4); i += 256) {
@@ -381,10 +447,10 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       }
       const size_t row = row_of(col);
       if (whole) {
-        bf16x4 v;
+        T4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (bf16)(num[e] / den);
-        *reinterpret_cast<bf16x4*>(out + row * HD + d) = v;
+        for (int e = 0; e < 4; ++e) v[e] = from_f<T>(num[e] / den);
+        *reinterpret_cast<T4*>(out + row * HD + d) = v;
       } else {
         *reinterpret_cast<f32x4*>(part_o + (pieces + row) * HD + d) = num;
         if (d == 0) part_ml[pieces + row] = float2{m, den};
@@ -400,15 +466,16 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       if (whole) {
         const float inv = 1.0f / l;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          bf16x4 v;
+        for (int i = 0; i < DT; ++i) {
+          const f32x4 p = piece(c, i);
+          T4 v;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = (bf16)(o[c][d][e] * inv);
-          *reinterpret_cast<bf16x4*>(out + row * HD + d * 16 + 4 * lg) = v;
+          for (int e = 0; e < 4; ++e) v[e] = from_f<T>(p[e] * inv);
+          *reinterpret_cast<T4*>(out + row * HD + dim_of(i)) = v;
         }
       } else {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(part_o + (pieces + row) * HD + d * 16 + 4 * lg) = o[c][d];
+        for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(part_o + (pieces + row) * HD + dim_of(i)) = piece(c, i);
         if (lg == 0) part_ml[pieces + row] = float2{m_run[c], l};
       }
     }
@@ -416,10 +483,11 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 }
 
 // Rows of sequences of several chunks: the chunks' results in chunk order, four dims to a thread.
-template <int HD>
+template <class T, int HD>
 __global__ void __launch_bounds__(256)
 k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, int rows, int hq, int max_seq, int nchunk, int chunk_keys,
-             const float* __restrict__ part_o, const float2* __restrict__ part_ml, bf16* __restrict__ out) {
+             const float* __restrict__ part_o, const float2* __restrict__ part_ml, T* __restrict__ out) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
   constexpr int TPR = HD / 4;
   const int node = blockIdx.x, b = blockIdx.y, h = blockIdx.z * (256 / TPR) + threadIdx.x / TPR, d = threadIdx.x % TPR * 4;
   TreeSeq t;
@@ -442,41 +510,46 @@ k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_len
     for (int e = 0; e < 4; ++e) num[e] += v[e] * wt;
     den += ml.y * wt;
   }
-  bf16x4 v;
+  T4 v;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = (bf16)(num[e] / den);
-  *reinterpret_cast<bf16x4*>(out + row * HD + d) = v;
+  for (int e = 0; e < 4; ++e) v[e] = from_f<T>(num[e] / den);
+  *reinterpret_cast<T4*>(out + row * HD + d) = v;
 }
 
-template <int HD, int CT, int CW>
+template <class T, int HD, int CT, int CW>
 void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
-  constexpr int COLS = 16 * CT * CW, KW = 4 / CW, TK = 32 * steps_of<HD, CT, CW>();
-  constexpr int TILES = KW * (CW == 1 ? 1 : 2) * 2 * TK * HD * 2, JOIN = KW > 1 ? KW * COLS * (HD + SM_PAD) * 4 : 0, SMEM = TILES > JOIN ? TILES : JOIN;
+  constexpr int COLS = 16 * CT * CW, KW = 4 / CW, TK = STEP_KEYS<T> * steps_of<T, HD, CT, CW>();
+  constexpr int TILES = KW * (CW == 1 ? 1 : 2) * 2 * TK * HD * (int)sizeof(T), JOIN = KW > 1 ? KW * COLS * (HD + SM_PAD) * 4 : 0;
+  constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
   static std::atomic<uint64_t> lds_allowed{0};
-  allow_dynamic_lds((const void*)k_tree_mfma<HD, CT, CW>, SMEM, lds_allowed);
+  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CT, CW>, SMEM, lds_allowed);
   const int blocks = (a.max_nodes * (a.hq / a.hkv) + COLS - 1) / COLS;
-  k_tree_mfma<HD, CT, CW><<<dim3(p.n, a.hkv * blocks, a.batch), 256, SMEM, st>>>(
-      a.cu, a.seq_lens, a.parents, (const bf16*)a.qkv, a.cs, (bf16*)a.kc, (bf16*)a.vc, (bf16*)a.out, a.rows, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK,
-      p.o, p.ml);
+  k_tree_mfma<T, HD, CT, CW><<<dim3(p.n, a.hkv * blocks, a.batch), 256, SMEM, st>>>(
+      a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, p.o, p.ml);
   if (p.n > 1)
-    k_tree_merge<HD><<<dim3(a.max_nodes, a.batch, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(a.cu, a.seq_lens, a.rows, a.hq, a.max_seq, p.n, p.keys,
-                                                                                                   p.o, p.ml, (bf16*)a.out);
+    k_tree_merge<T, HD><<<dim3(a.max_nodes, a.batch, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(
+        a.cu, a.seq_lens, a.rows, a.hq, a.max_seq, p.n, p.keys, p.o, p.ml, (T*)a.out);
 }
 
-template <int HD>
+template <class T, int HD>
 void launch_hd(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
   const int cols = a.max_nodes * (a.hq / a.hkv);
-  if (cols <= 16) launch<HD, 1, 1>(a, p, st);
-  else if (cols <= 32) launch<HD, 1, 2>(a, p, st);
-  else if (cols <= 64) launch<HD, 1, 4>(a, p, st);
-  else launch<HD, 2, 4>(a, p, st);
+  if (cols <= 16) launch<T, HD, 1, 1>(a, p, st);
+  else if (cols <= 32) launch<T, HD, 1, 2>(a, p, st);
+  else if (cols <= 64) launch<T, HD, 1, 4>(a, p, st);
+  else launch<T, HD, 2, 4>(a, p, st);
 }
 
 }  // namespace
 
-void launch_tree_attn_bf16(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
-  if (a.hd == 128) launch_hd<128>(a, p, st);
-  else launch_hd<64>(a, p, st);
+void launch_tree_attn_mfma(uint32_t dt, const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
+  if (dt == F32) {
+    if (a.hd == 128) launch_hd<float, 128>(a, p, st);
+    else launch_hd<float, 64>(a, p, st);
+  } else {
+    if (a.hd == 128) launch_hd<bf16, 128>(a, p, st);
+    else launch_hd<bf16, 64>(a, p, st);
+  }
 }
 
 }  // namespace ls
