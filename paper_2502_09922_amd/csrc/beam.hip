@@ -21,6 +21,7 @@ constexpr int BEAMS_MAX = LS_BEAMS_MAX;
 //
 // Bound by the one reading: 64 x 5 rows of 50257 tokens (64 MB) @PICK@.
 constexpr int SEG = 8192, EACH = SEG / 256;
+constexpr int HELD = 12288;            // sets in LDS: what 5 beams of 64k tokens leave, or 12 of 32k
 constexpr int LIST = 2048;             // candidates in LDS: >= BEAMS_MAX * EACH
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -65,7 +66,7 @@ k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended,
     const int at = first + j * 1024;
     v[j] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     if (at + 4 <= vocab) {
-      v[j] = __builtin_nontemporal_load(reinterpret_cast<const f32x4u*>(x + at));
+      v[j] = *reinterpret_cast<const f32x4u*>(x + at);
     } else {
 #pragma unroll
       for (int e = 0; e < 3; ++e)
@@ -106,7 +107,7 @@ k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended,
 
 __global__ void __launch_bounds__(1024)
 k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, const int32_t* __restrict__ ended, int beams, int vocab, int k, int eos,
-            int nseg, const Set* __restrict__ sets, const SegSum* __restrict__ sums, int32_t* __restrict__ rows_out, int32_t* __restrict__ tokens,
+            int nseg, unsigned nseg_inv, const Set* __restrict__ sets, const SegSum* __restrict__ sums, int32_t* __restrict__ rows_out, int32_t* __restrict__ tokens,
             float* __restrict__ scores_out) {
   constexpr int NT = 1024;
   enum { DEAD = 0, LIVE = 1, ENDED = 2 };
@@ -115,33 +116,65 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
   __shared__ int state[BEAMS_MAX], chosen[BEAMS_MAX], count;
   __shared__ Cand some[64], bound, list[LIST];
   __shared__ int id[LIST];
+  __shared__ int rank[LIST];
+  struct Rough {  // a beam in 32 bits
+    float most, base, score;
+    int eos_set;  // of an ended beam
+  };
+  __shared__ Rough rough[BEAMS_MAX];
+  __shared__ __attribute__((aligned(16))) float part[64];
+  __shared__ float rough_bound;
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const size_t row0 = (size_t)g * beams;
-  if (tid < beams) {
-    const size_t r = row0 + tid;
+  const int C = nseg * 256, N = beams * C;
+  const Set* mine_sets = sets + row0 * C;
+  // Sets go through LDS, HELD at a time: all on their way at once, and then short loops.  (The loops unrolled: 18.4 us for 64 x 5 beams
+  // instead of 15.1.)
+  __shared__ Set held[HELD];
+  auto load = [&](int e0) {
+    Set v[HELD / NT];
+#pragma unroll
+    for (int u = 0; u < HELD / NT; ++u)
+      if (e0 + u * NT < N) v[u] = mine_sets[min(e0 + u * NT + tid, N - 1)];
+#pragma unroll
+    for (int u = 0; u < HELD / NT; ++u)
+      if (e0 + u * NT < N) held[u * NT + tid] = v[u];
+  };
+  load(0);
+  {  // sixteen threads to a beam
+    const int beam = tid >> 4;
+    const bool in = beam < beams;
+    const size_t r = row0 + (in ? beam : 0);
+    const bool end = ended && ended[r];
     const float score = scores[r];
-    if (ended && ended[r]) {
-      state[tid] = score < INFINITY && score > -INFINITY ? ENDED : DEAD;
-      most[tid] = score;
-    } else {
-      float M = -INFINITY;
-      for (int s = 0; s < nseg; ++s) M = fmaxf(M, sums[r * nseg + s].m);
-      double l = 0.;
-      for (int s = 0; s < nseg; ++s) {
-        const SegSum p = sums[r * nseg + s];
-        l += p.m == -INFINITY ? p.l : p.l * exp((double)p.m - (double)M);
-      }
+    float M = -INFINITY;
+    for (int s = tid & 15; s < nseg; s += 16) M = fmaxf(M, sums[r * nseg + s].m);
+    M = exchange<8, 1>(M, Max{});
+    double l = 0.;
+    for (int s = tid & 15; s < nseg; s += 16) {
+      const SegSum p = sums[r * nseg + s];
+      l += p.m == -INFINITY ? p.l : p.l * exp((double)p.m - (double)M);
+    }
+#pragma unroll
+    for (int off = 8; off; off >>= 1) l += __shfl_xor(l, off);
+    if (in && (tid & 15) == 0) {
       const double b = (double)score - log(l);
-      // all others have no candidate above -inf: nothing left of their logits, or one that makes the sum none
-      state[tid] = M < INFINITY && M > -INFINITY && b < INFINITY && b > -INFINITY ? LIVE : DEAD;
-      base[tid] = b;
-      most[tid] = M;
+      // dead: nothing left of the logits, or one that makes the sum none; such have no candidate above -inf
+      if (end) state[beam] = score < INFINITY && score > -INFINITY ? ENDED : DEAD;
+      else state[beam] = M < INFINITY && M > -INFINITY && b < INFINITY && b > -INFINITY ? LIVE : DEAD;
+      base[beam] = b;
+      most[beam] = end ? score : M;
+      const bool live = state[beam] == LIVE, over = state[beam] == ENDED;
+      rough[beam] = Rough{live ? M : 0.f, live ? (float)b : -INFINITY, score, over ? beam * C + eos / SEG * 256 + (eos / 4 & 255) : -1};
     }
   }
-  if (tid == 0) count = 0;
+  if (tid == 0) {
+    count = 0;
+    rough_bound = -INFINITY;
+  }
+  if (tid < 64) rank[tid] = 0;
   __syncthreads();
 
-  const int C = nseg * 256, N = beams * C;
   auto score_of = [&](int beam, float x, int token) {
     Cand c{-INFINITY, 0.f, beam << 24 | token};
     if (state[beam] == LIVE) {
@@ -153,63 +186,119 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
     return c;
   };
   // the best of set e.  Its token is that of a float4: sets share none, so that it orders them
-  auto best_of = [&](int e) {
-    const int beam = (int)((unsigned)e / (unsigned)C), c = e - beam * C, first = (c >> 8) * SEG + (c & 255) * 4;
+  auto best_of = [&](int e, Set s) {
+    const int beam = (int)__umulhi((unsigned)(e >> 8) * 2u, nseg_inv), c = e - beam * C, first = (c >> 8) * SEG + (c & 255) * 4;
     if (first >= vocab) return Cand{-INFINITY, 0.f, NONE};
-    if (state[beam] == LIVE) {
-      const Set s = sets[(row0 + beam) * C + c];
-      return score_of(beam, s.m, s.at);
-    }
+    if (state[beam] == LIVE) return score_of(beam, s.m, s.at);
     const bool has_eos = eos >= first && eos < (c >> 8) * SEG + SEG && (((eos - first) >> 2) & 255) == 0;
-    Cand out = score_of(beam, 0.f, first);
-    if (state[beam] == ENDED && has_eos) out = score_of(beam, 0.f, eos);
-    return out;
+    return score_of(beam, 0.f, state[beam] == ENDED && has_eos ? eos : first);
   };
-
-  // ---- a bound: the k-th best of 64 parts' best sets
-  Cand mine{-INFINITY, 0.f, NONE};
-  for (int e = tid; e < N; e += NT) {
-    const Cand c = best_of(e);
-    if (before(c, mine)) mine = c;
-  }
-#pragma unroll
-  for (int off = 8; off; off >>= 1) {
-    const Cand c = cand_xor(mine, off);
-    if (before(c, mine)) mine = c;
-  }
-  if ((tid & 15) == 0) some[tid >> 4] = mine;
-  __syncthreads();
-  // how many of n candidates stand before the one at i (a copy in front of it counts as one); no more than k are counted for sure
-  auto rank_of = [&](const Cand* of, int n, int i) {
-    const Cand c = of[i];
-    int r = 0;
-    for (int j = 0; j < n; ++j) {
-      const Cand o = of[j];
-      r += before(o, c) || (j < i && !before(c, o));
-      if ((j & 31) == 31 && __builtin_amdgcn_ballot_w64(r < k) == 0) break;
+  // f(set, what it left) for all of this thread's: it reads what it has written itself
+  auto each = [&](auto f) {
+    for (int e0 = 0; e0 < N; e0 += HELD) {
+      if (N > HELD) load(e0);
+#pragma unroll 1
+      for (int e = tid; e < min(HELD, N - e0); e += NT) f(e0 + e, held[e]);
     }
-    return r;
   };
-  if (tid < 64 && rank_of(some, 64, lane) == k - 1) bound = some[lane];
-  __syncthreads();
+  // rank[i] += how many of n candidates stand before the one at i, a copy in front of it included; a sixteenth of them to a wavefront
+  auto add_ranks = [&](const Cand* of, int n) {
+    for (int i = lane; i < n; i += 64) {
+      const Cand c = of[i];
+      int r = 0;
+      for (int j = tid >> 6; j < n; j += NT / 64) {
+        const Cand o = of[j];
+        r += o.s > c.s;
+        if (o.s == c.s && i != j) r += before(o, c) || (j < i && !before(c, o));
+      }
+      if (r) atomicAdd(&rank[i], r);
+    }
+  };
 
-  // ---- the sets that are no worse, and the k best of them
-  const Cand lowest = bound;
-  for (int e = tid; e < N; e += NT) {
-    const Cand c = best_of(e);
-    if (c.at != NONE && !before(lowest, c)) {
-      const int to = atomicAdd(&count, 1);
-      if (to < LIST) {
-        list[to] = c;
-        id[to] = e;
+  auto push = [&](int e, Cand c) {
+    const int to = atomicAdd(&count, 1);
+    if (to < LIST) {
+      list[to] = c;
+      id[to] = e;
+      rank[to] = 0;
+    }
+  };
+  // ---- a bound: the k-th best of 64 parts' best sets; then the sets that are no worse.  In 32 bits with room for their rounding, 2^-24
+  // of the logit, the base (twice) and the sum each
+  auto rounded = [&](int e, float m, float way) {  // 64 neighbouring sets are one beam's
+    const Rough b = rough[__umulhi((unsigned)(__builtin_amdgcn_readfirstlane(e) >> 8) * 2u, nseg_inv)];
+    const float f = (m - b.most) + b.base;
+    return e == b.eos_set ? b.score : f + way * 0x1p-21f * (fabsf(f) + fabsf(b.base));  // of a dead beam NaN
+  };
+  // g(i, e) for this thread's sets, the i-th of those held, e of all
+  auto rough_each = [&](int e0, auto g) {
+    const int n = min(HELD, N - e0);
+#pragma unroll 1
+    for (int i = tid; i < n; i += NT) g(i, e0 + i);
+  };
+  float top = -INFINITY;
+  for (int e0 = 0; e0 < N; e0 += HELD) {
+    if (N > HELD) load(e0);
+    rough_each(e0, [&](int i, int e) { top = fmaxf(top, rounded(e, held[i].m, -1.f)); });
+  }
+  top = exchange<8, 1>(top, Max{});
+  if ((tid & 15) == 0) part[tid >> 4] = top;
+  __syncthreads();
+  {  // each wavefront compares all with four of them
+    const float c = part[lane];
+    const f32x4 o = reinterpret_cast<const f32x4*>(part)[tid >> 6];
+    int r = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r += o[j] > c || (o[j] == c && (tid >> 6) * 4 + j < lane);
+    if (r) atomicAdd(&rank[lane], r);
+  }
+  __syncthreads();
+  if (tid < 64) {
+    if (rank[tid] == k - 1) rough_bound = part[tid];
+    rank[tid] = 0;
+  }
+  __syncthreads();
+  const float least_top = rough_bound;
+  if (least_top > -INFINITY) {
+    for (int e0 = 0; e0 < N; e0 += HELD) {
+      if (N > HELD) load(e0);
+      unsigned good = 0;  // of this thread's HELD / NT
+      rough_each(e0, [&](int i, int e) { good |= (unsigned)(rounded(e, held[i].m, 1.f) >= least_top) << (i / NT); });
+      for (; good; good &= good - 1) {
+        const int i = __builtin_ctz(good) * NT + tid;
+        push(e0 + i, best_of(e0 + i, held[i]));
       }
     }
+  } else {  // fewer parts than k with any candidate above -inf: the order of those at -inf counts
+    Cand mine{-INFINITY, 0.f, NONE};
+    each([&](int e, Set s) {
+      const Cand c = best_of(e, s);
+      if (before(c, mine)) mine = c;
+    });
+#pragma unroll
+    for (int off = 8; off; off >>= 1) {
+      const Cand c = cand_xor(mine, off);
+      if (before(c, mine)) mine = c;
+    }
+    if ((tid & 15) == 0) some[tid >> 4] = mine;
+    __syncthreads();
+    add_ranks(some, 64);
+    __syncthreads();
+    if (tid < 64 && rank[tid] == k - 1) bound = some[tid];
+    __syncthreads();
+    const Cand lowest = bound;
+    each([&](int e, Set s) {
+      const Cand c = best_of(e, s);
+      if (c.at != NONE && !before(lowest, c)) push(e, c);
+    });
   }
   __syncthreads();
   const int found = count, sel = min(found, k);
   if (found <= LIST) {
+    add_ranks(list, found);
+    __syncthreads();
     for (int i = tid; i < found; i += NT) {
-      const int r = rank_of(list, found, i);
+      const int r = rank[i];
       if (r < sel) chosen[r] = id[i];
       if (r == sel - 1) bound = list[i];
     }
@@ -217,15 +306,15 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
     __shared__ int at[16];
     Cand last{INFINITY, 0.f, -1};
     for (int j = 0; j < sel; ++j) {
-      mine = Cand{-INFINITY, 0.f, NONE};
+      Cand mine{-INFINITY, 0.f, NONE};
       int set = -1;
-      for (int e = tid; e < N; e += NT) {
-        const Cand c = best_of(e);
+      each([&](int e, Set s) {
+        const Cand c = best_of(e, s);
         if (before(last, c) && before(c, mine)) {
           mine = c;
           set = e;
         }
-      }
+      });
       for (int off = 32; off; off >>= 1) {
         const Cand c = cand_xor(mine, off);
         const int o = __shfl_xor(set, off);
@@ -261,15 +350,21 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
   least.at |= 3;  // the last token of its float4 that may be it
   for (int i = tid; i < sel * EACH; i += NT) {
     const int e = chosen[i / EACH], q = i % EACH;
-    const int beam = (int)((unsigned)e / (unsigned)C), c = e - beam * C, token = (c >> 8) * SEG + (c & 255) * 4 + (q >> 2) * 1024 + (q & 3);
+    const int beam = (int)__umulhi((unsigned)(e >> 8) * 2u, nseg_inv), c = e - beam * C, token = (c >> 8) * SEG + (c & 255) * 4 + (q >> 2) * 1024 + (q & 3);
     if (token >= vocab) continue;
     const Cand d = score_of(beam, state[beam] == LIVE ? logits[(row0 + beam) * vocab + token] : 0.f, token);
-    if (sel < k || !before(least, d)) list[atomicAdd(&count, 1)] = d;
+    if (sel < k || !before(least, d)) {
+      const int to = atomicAdd(&count, 1);
+      list[to] = d;
+      rank[to] = 0;
+    }
   }
   __syncthreads();
   const int n = count;
+  add_ranks(list, n);
+  __syncthreads();
   for (int i = tid; i < n; i += NT) {
-    const int r = rank_of(list, n, i);
+    const int r = rank[i];
     if (r < k) {
       const size_t to = (size_t)g * k + r;
       rows_out[to] = (int)row0 + (list[i].at >> 24);
@@ -376,9 +471,11 @@ ls_status ls_beam_select(const float* logits, const float* scores, const int32_t
   const int nseg = (vocab + ls::SEG - 1) / ls::SEG, n = groups * beams;
   ls::SegSum* sums = (ls::SegSum*)scratch;
   ls::Set* sets = (ls::Set*)(sums + (size_t)n * nseg);
+  // x / nseg = umulhi(2 x, nseg_inv) for the x < 64 nseg there are, nseg <= 2048: the product is off by less than x nseg < 2^31
+  const unsigned nseg_inv = (unsigned)(((1ull << 31) + nseg - 1) / nseg);
   hipStream_t st = (hipStream_t)hip_stream;
   ls::k_beam_rows<<<dim3(n, nseg), 256, 0, st>>>(logits, ended, vocab, nseg, sets, sums);
-  ls::k_beam_pick<<<groups, 1024, 0, st>>>(logits, scores, ended, beams, vocab, k, eos, nseg, sets, sums, rows, tokens, scores_out);
+  ls::k_beam_pick<<<groups, 1024, 0, st>>>(logits, scores, ended, beams, vocab, k, eos, nseg, nseg_inv, sets, sums, rows, tokens, scores_out);
   return launched(who);
 }
 
