@@ -129,12 +129,16 @@ __device__ __forceinline__ float row16_sum(float v) {
 // index), among `rows` <= 64 C rows with positions below `limit`, and its position.  Every wavefront finds it on its
 // own, a bit of the position at a time by counting the rows that reach it: no LDS, no barrier.  (Comparing every row
 // with every other through LDS took 5 us of every workgroup at 256 rows.)
-template <int C>
+// ANY: positions may lie outside [-1, limit) and count as those bounds.
+template <int C, bool ANY = false>
 __device__ __forceinline__ int row_by_length(const int32_t* __restrict__ row_pos, int rows, int rank, int limit, int& pos) {
   const int lane = threadIdx.x & 63;
   int len[C];  // position + 1: a sequence without room has 0, a row that is not there -1
 #pragma unroll
-  for (int c = 0; c < C; ++c) len[c] = c * 64 + lane < rows ? row_pos[c * 64 + lane] + 1 : -1;
+  for (int c = 0; c < C; ++c) {
+    len[c] = c * 64 + lane < rows ? row_pos[c * 64 + lane] + 1 : -1;
+    if (ANY && c * 64 + lane < rows) len[c] = min(max(len[c], 0), limit);
+  }
   auto reach = [&](int v) {
     int n = 0;
 #pragma unroll

@@ -15,9 +15,9 @@
 // lane holds 4 apart.
 //
 // A workgroup is a (sequence, kv head, block of columns, chunk of keys).  Of its four wavefronts CW share keys, each with columns
-// of its own, and 4 / CW split the chunk's keys.  Up to 16 columns each walks keys of its own, a step at a time through registers into LDS of
-// its own, no barriers (CW = 1); wavefronts that share keys fill double-buffered tiles together.  The splits' results are joined
-// through LDS, chunks' by a second kernel, both in order.
+// of its own, and 4 / CW split the chunk's keys.  Up to 16 columns each walks keys of its own, a tile at a time through registers into LDS of
+// its own, no barriers (CW = 1); wavefronts that share keys fill a ring of tiles together, straight from memory, one barrier a tile.
+// The splits' results are joined through LDS, chunks' by a second kernel, both in order.
 //
 // The nodes' own rows are turned, rounded and written to their slots by whoever reads those, a wavefront (CW = 1) or a workgroup,
 // before it reads them: blocks of columns write the same bytes, and none depends on another workgroup's.  Only in the tiles of
@@ -87,18 +87,19 @@ __device__ __forceinline__ u32x4 turned(u32x4 v, const float* turn, float) {
 
 constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns' equal dims in different banks
 
-template <class T> constexpr int STEP_KEYS = sizeof(T) == 2 ? 32 : 16;
-// Steps in a tile: two where tiles are shared by all and the registers suffice.
-template <class T, int HD, int CT, int CW> constexpr int steps_of() { return CW == 4 && (CT == 1 || HD == 64) ? 2 : 1; }
+constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds in registers
+constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
+constexpr int RESIDENT = 512;      // workgroups on the chip at once
+template <class T> constexpr int TILE_KEYS = sizeof(T) == 2 ? 32 : 16;  // 16 KB of keys and values of 128 dims
 
-template <class T, int HD, int CT, int CW>
+// NB: tiles of the ring, a power of two (CW > 1).
+template <class T, int HD, int CT, int CW, int NB>
 __global__ void __launch_bounds__(256, 2)
 k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ parents, const T* __restrict__ qkv,
             const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, T* __restrict__ out, int rows, int hq, int hkv, int max_seq,
-            int nchunk, int chunk_tiles, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+            int nchunk, int chunk_tiles, int half, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   constexpr int KW = 4 / CW;             // wavefronts that split the keys
-  constexpr int SK = STEP_KEYS<T>, SUB = steps_of<T, HD, CT, CW>();
-  constexpr int TK = SK * SUB;
+  constexpr int TK = TILE_KEYS<T>;
   constexpr int ROWB = HD * sizeof(T), EPC = 16 / sizeof(T);
   constexpr int CPR = HD / EPC;          // 16-byte chunks of a row
   constexpr int RPI = 64 / CPR;          // rows that a wavefront's load covers
@@ -110,7 +111,11 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   const int G = hq / hkv;
-  const int b = blockIdx.z, kh = blockIdx.y % hkv, cb = blockIdx.y / hkv, z = blockIdx.x;
+  const int kh = blockIdx.y % hkv, cb = blockIdx.y / hkv, z = blockIdx.x;
+  int b = blockIdx.z, pos_of_b;
+  // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest
+  if (half) b = row_by_length<ORDERED / 64, true>(seq_lens, gridDim.z, b < half ? b : (int)gridDim.z - 1 - (b - half), max_seq, pos_of_b);
+  b = __builtin_amdgcn_readfirstlane(b);
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TreeSeq t;
@@ -160,9 +165,62 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       for (int i = 0; i < NL; ++i) fetch(i, min(i * RPI + lrow, keys - 1 - row0));
     }
   };
-  const bool early = t_begin < t_end && (t_begin + 1) * TK <= t.ctx;
-  if (early) load(t_begin);  // on its way while nodes and queries are made ready
+  // CW > 1: straight into the ring.  Written in assembly: of the builtin the compiler knows that it writes LDS but not where, and would
+  // wait for the fills on their way before it reads what has arrived.  (m0 is reserved, of which the compiler warns.)
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem + split * (NB * 2 * TILE) + first_row * ROWB;
+  unsigned koff[NL], voff[NL];  // a row's piece from the tile's first row
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int r = first_row + i * RPI + lrow;
+    koff[i] = r * ROWB + ((lchunk ^ key_swizzle<T, HD>(r)) << 4);
+    voff[i] = r * ROWB + ((lchunk ^ value_swizzle<T, HD>(r)) << 4);
+  }
+  auto fill = [&](int tile) {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    auto piece = [](const T* base, unsigned off, unsigned to) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+    };
+#pragma clang diagnostic pop
+    const T *kt = kb + (size_t)tile * TK * HD, *vt = vb + (size_t)tile * TK * HD;
+    const unsigned to = lds0 + ((tile - t_begin) & (NB - 1)) * (2 * TILE);
+    const int have = keys - tile * TK;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      unsigned back = 0;  // rows behind the last key: that one again, which their weights of zero leave out
+      if (have < TK) {
+        const int r = first_row + i * RPI + lrow;
+        back = (unsigned)(r - min(r, have - 1)) * ROWB;
+      }
+      piece(kt, koff[i] - back, to + i * 1024);
+      piece(vt, voff[i] - back, to + TILE + i * 1024);
+    }
+  };
+  // on their way while nodes and queries are made ready: tiles without nodes
+  bool early = false;
+  int next = t_begin;  // the next tile to be filled
+  if constexpr (CW == 1) {
+    early = t_begin < t_end && (t_begin + 1) * TK <= t.ctx;
+    if (early) load(t_begin);
+  } else {
+    while (next < min(t_end, t_begin + NB - 1) && (next + 1) * TK <= t.ctx) fill(next++);
+  }
 
+  // this wavefront's columns: 16-column tiles share, share + CW, .. of the workgroup's, so that few columns are spread over all
+  constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a row
+  const int G16 = t.n * G - cb * COLS - share * 16;
+  const int tiles_here = CT == 1 ? G16 > 0 : (G16 > 0) + (G16 > 16 * CW);
+  u32x4 raw[CT][KS];
+  int node[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int col = cb * COLS + (share + CW * c) * 16 + lr;
+    const bool in = col < t.n * G;
+    node[c] = in ? col / G : 0;
+    const T* q = rows0 + (size_t)node[c] * stride + (size_t)(kh * G + (in ? col % G : 0)) * HD;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) raw[c][kk] = *reinterpret_cast<const u32x4*>(q + (kk * 4 + lg) * EPC);
+  }
   const uint64_t path = tree_path(parents, t);
   {  // the nodes' rows among the keys of this wavefront (CW = 1) or workgroup
     const int depth = __builtin_popcountll(path) - 1;
@@ -180,45 +238,35 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
         *reinterpret_cast<u32x4*>(vb + (size_t)key * HD + ch * EPC) = v;
       }
     }
-    if constexpr (CW == 1) {
-      if (items > 0) __threadfence_block();  // other lanes of this wavefront read them
-    } else {
-      __syncthreads();
+    if (items > 0) {  // other lanes of this wavefront read them, or of the workgroup
+      if constexpr (CW == 1) __threadfence_block();
+      else __syncthreads();
     }
   }
 
-  // ---- this wavefront's columns: queries, bf16 as two parts, and the nodes they see
-  const int col0 = cb * COLS + share * 16 * CT + lr;
-  constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a key's row
+  // ---- queries, bf16 as two parts, and the nodes they see
   typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Q;
   Q qh[CT][KS], ql[CT][sizeof(T) == 2 ? KS : 1];
   uint64_t sees[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
-    const int col = col0 + 16 * c;
-    const bool in = col < t.n * G;
-    const int node = in ? col / G : 0;
-    sees[c] = (uint64_t)(unsigned)__shfl((int)(unsigned)(path >> 32), node) << 32 | (unsigned)__shfl((int)(unsigned)path, node);
-    const int pos = t.ctx + __builtin_popcountll(sees[c]) - 1;
-    const T* q = rows0 + (size_t)node * stride + (size_t)(kh * G + (in ? col % G : 0)) * HD;
+    sees[c] = (uint64_t)(unsigned)__shfl((int)(unsigned)(path >> 32), node[c]) << 32 | (unsigned)__shfl((int)(unsigned)path, node[c]);
+    const float* turn = cs + (size_t)(t.ctx + __builtin_popcountll(sees[c]) - 1) * HD;
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
+      const int d0 = (kk * 4 + lg) * EPC;
       if constexpr (sizeof(T) == 4) {
-        const int d0 = kk * 16 + lg * 4;
-        u32x4 raw = *reinterpret_cast<const u32x4*>(q + d0);
-        if (cs) raw = turned(raw, cs + (size_t)pos * HD + d0, T{});
-        qh[c][kk] = __builtin_bit_cast(f32x4, raw);
+        qh[c][kk] = __builtin_bit_cast(f32x4, cs ? turned(raw[c][kk], turn + d0, T{}) : raw[c][kk]);
       } else {
-        const int d0 = kk * 32 + lg * 8;
-        const bf16x8 raw = *reinterpret_cast<const bf16x8*>(q + d0);
+        const bf16x8 u = __builtin_bit_cast(bf16x8, raw[c][kk]);
         f32x4 ta{}, tb{};
         if (cs) {
-          ta = reinterpret_cast<const f32x4*>(cs + (size_t)pos * HD + d0)[0];
-          tb = reinterpret_cast<const f32x4*>(cs + (size_t)pos * HD + d0)[1];
+          ta = reinterpret_cast<const f32x4*>(turn + d0)[0];
+          tb = reinterpret_cast<const f32x4*>(turn + d0)[1];
         }
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          float u0 = (float)raw[2 * p], u1 = (float)raw[2 * p + 1];
+          float u0 = (float)u[2 * p], u1 = (float)u[2 * p + 1];
           if (cs) {
             const float2 c2 = p < 2 ? float2{ta[2 * p], ta[2 * p + 1]} : float2{tb[2 * p - 4], tb[2 * p - 3]};
             const float w0 = turn0(u0, u1, c2), w1 = turn1(u0, u1, c2);
@@ -252,20 +300,21 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   };
   auto piece = [&](int c, int i) { return f32x4{out_at(c, i, 0), out_at(c, i, 1), out_at(c, i, 2), out_at(c, i, 3)}; };
 
-  // ---- a step of a tile in LDS
-  constexpr int HALVES = SK / 16;
-  auto attend = [&](const unsigned char* ks, const unsigned char* vs, int sub, int key0, bool odd) {
-    f32x4 s[CT][HALVES];
+  // ---- a tile in LDS
+  constexpr int HALVES = TK / 16;
+  auto attend = [&](auto tiles_, const unsigned char* ks, const unsigned char* vs, int key0, bool odd) {
+    constexpr int NC = decltype(tiles_)::value;
+    f32x4 s[NC][HALVES];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
-      const int kl = sub * SK + h * 16 + lr;
+      const int kl = h * 16 + lr;
 #pragma unroll
-      for (int c = 0; c < CT; ++c) s[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < NC; ++c) s[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const Q kf = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
+        for (int c = 0; c < NC; ++c) {
           if constexpr (sizeof(T) == 2) {
             s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, ql[c][kk], s[c][h], 0, 0, 0);
             s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qh[c][kk], s[c][h], 0, 0, 0);
@@ -278,8 +327,8 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     }
     const int behind = key0 - t.ctx;  // of the cached positions
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      if (behind > -SK) {  // slots of nodes
+    for (int c = 0; c < NC; ++c) {
+      if (behind > -TK) {  // slots of nodes
         const unsigned seen = behind >= 64 ? 0u : behind >= 0 ? (unsigned)(sees[c] >> behind) : (unsigned)(sees[c] << -behind) | ((1u << -behind) - 1u);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h)
@@ -312,12 +361,12 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       l_run[c] += sum;
     }
     if constexpr (sizeof(T) == 2) {
-      bf16x8 pf[CT];
+      bf16x8 pf[NC];
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) pf[c][i] = (bf16)s[c][i >> 2][i & 3];
-      const int k0 = sub * SK + 4 * lg + (lr >> 2), k1 = k0 + 16;
+      const int k0 = 4 * lg + (lr >> 2), k1 = k0 + 16;
       const int within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
@@ -326,26 +375,26 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k1 * ROWB + ((ch ^ value_swizzle<T, HD>(k1)) << 4) + within));
         const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
-        for (int c = 0; c < CT; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[c], o[c][d], 0, 0, 0);
+        for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[c], o[c][d], 0, 0, 0);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const f32x4 vt = *reinterpret_cast<const f32x4*>(vs + (sub * SK + 4 * lg + e) * ROWB + (j * 16 + lr) * 16);
+          const f32x4 vt = *reinterpret_cast<const f32x4*>(vs + (4 * lg + e) * ROWB + (j * 16 + lr) * 16);
 #pragma unroll
-          for (int c = 0; c < CT; ++c)
+          for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int d = 0; d < 4; ++d) o[c][j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[d], s[c][0][e], o[c][j * 4 + d], 0, 0, 0);
         }
     }
     if (odd) {  // nodes' values that are no numbers lie in the tile as zeros: only the columns that see the nodes take them
-      for (int j = max(0, -behind); j < SK && behind + j < t.n; ++j) {
+      for (int j = max(0, -behind); j < TK && behind + j < t.n; ++j) {
         const T* v = rows0 + (size_t)(behind + j) * stride + (size_t)(hq + hkv + kh) * HD;
         const int from = ((j >> 2) & 3) * 16 + lr;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
+        for (int c = 0; c < NC; ++c) {
           float p = 0.f;
 #pragma unroll
           for (int i = 0; i < 4 * HALVES; ++i) p = (j >> 4) * 4 + (j & 3) == i ? s[c][i >> 2][i & 3] : p;
@@ -384,34 +433,60 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   const size_t pieces = (size_t)z * rows * hq;
   auto row_of = [&](int col) { return (size_t)(t.row0 + col / G) * hq + kh * G + col % G; };
 
-  __shared__ int odd_flags[2][4];
-  unsigned char* tiles = smem + split * ((CW == 1 ? 1 : 2) * 2 * TILE);  // one buffer of keys and values, or two
-  for (int i = t_begin - 1; i < t_begin + per; ++i) {  // tile i is attended to while i + 1 is on its way; as many turns for all
+  __shared__ int odd_flags[NB][4];
+  unsigned char* tiles = smem + split * ((CW == 1 ? 1 : NB) * 2 * TILE);
+  if constexpr (CW > 1)
+    while (next < min(t_end, t_begin + NB - 1)) fill(next++);
+  // a wavefront's loop for as many 16-column tiles as it has: of 128 columns two, of less one or none, so that small trees among large
+  // ones cost what they are (loops of their own, as one with both forms inside kept 54 registers in memory)
+  auto walk = [&](auto n_) {
     if constexpr (CW == 1) {
-      bool odd = false;
-      if (i >= t_begin && i < t_end) odd = put(tiles, tiles + TILE, i);
-      if (i + 1 < t_end && (i >= t_begin || !early)) load(i + 1);
-      if (i >= t_begin && i < t_end) attend(tiles, tiles + TILE, 0, i * TK, odd);
+      for (int i = t_begin - 1; i < t_end; ++i) {  // tile i is attended to while i + 1 is on its way
+        bool odd = false;
+        if (i >= t_begin) odd = put(tiles, tiles + TILE, i);
+        if (i + 1 < t_end && (i >= t_begin || !early)) load(i + 1);
+        if (i >= t_begin) attend(n_, tiles, tiles + TILE, i * TK, odd);
+      }
     } else {
-      const int buf = (i - t_begin) & 1;
-      const unsigned char *ks = tiles + buf * (2 * TILE), *vs = ks + TILE;
-      if (i + 1 < t_end && (i >= t_begin || !early)) load(i + 1);
-      if (i >= t_begin && i < t_end) {
-        int odd = 0;
+      for (int i = t_begin; i < t_begin + per; ++i) {  // as many turns for all
+        unsigned char* ks = tiles + ((i - t_begin) & (NB - 1)) * (2 * TILE);
+        int* flags = odd_flags[(i - t_begin) & (NB - 1)];
+        const bool last = (i + 1) * TK > t.ctx;  // slots of nodes
+        if (i < t_end) {
+          // this wavefront's fills of tile i have landed: those behind it are 2 NL for each tile
+          if (next - i == NB - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((NB - 2) * 2 * NL));
+          else wait_vm((next - 1 - i) * 2 * NL);
+          asm volatile("" ::: "memory");
+          if (last) {  // as put() does, in what this wavefront has filled
+            bool odd = false;
 #pragma unroll
-        for (int w = 0; w < CW; ++w) odd |= odd_flags[buf][split * CW + w];
-#pragma unroll 1
-        for (int sub = 0; sub < SUB; ++sub)
-          if (i * TK + sub * SK < keys) attend(ks, vs, sub, i * TK + sub * SK, odd != 0);
+            for (int j = 0; j < NL; ++j) {
+              const int r = first_row + j * RPI;
+              u32x4* at = reinterpret_cast<u32x4*>(ks + TILE + r * ROWB + lane * 16);
+              u32x4 v = *at;
+              if (i * TK + r + lrow >= t.ctx && drop_nonfinite<T>(v)) {
+                odd = true;
+                *at = v;
+              }
+            }
+            if (lane == 0) flags[wave] = 0;
+            if (__builtin_amdgcn_ballot_w64(odd) != 0 && lane == 0) flags[wave] = 1;
+          }
+        }
+        slot_barrier<true>();
+        if (next < t_end) fill(next++);  // over tile i - 1, which all have left
+        if (i < t_end && tiles_here) {
+          int odd = 0;
+          if (last)
+#pragma unroll
+            for (int w = 0; w < CW; ++w) odd |= flags[split * CW + w];
+          attend(n_, ks, ks + TILE, i * TK, odd != 0);
+        }
       }
-      if (i + 1 < t_end) {
-        unsigned char* to = tiles + (buf ^ 1) * (2 * TILE);
-        const bool odd = put(to, to + TILE, i + 1);
-        if (lane == 0) odd_flags[buf ^ 1][wave] = odd;
-      }
-      __syncthreads();
     }
-  }
+  };
+  if (CT == 1 || tiles_here == CT) walk(std::integral_constant<int, CT>{});
+  else walk(std::integral_constant<int, 1>{});
 
   if constexpr (KW > 1) {  // ---- the splits' results, in their order
     __shared__ float sm_m[KW][COLS], sm_l[KW][COLS];
@@ -420,7 +495,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const float l = exchange<16, 32>(l_run[c], Add{});
-      const int at = (share * CT + c) * 16 + lr;
+      const int at = (share + CW * c) * 16 + lr;
       if (lg == 0) {
         sm_m[split][at] = m_run[c];
         sm_l[split][at] = l;
@@ -459,7 +534,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   } else {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      const int col = col0 + 16 * c;
+      const int col = cb * COLS + (share + CW * c) * 16 + lr;
       const float l = exchange<16, 32>(l_run[c], Add{});
       if (col >= t.n * G) continue;
       const size_t row = row_of(col);
@@ -496,19 +571,34 @@ k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_len
   if (n == 1) return;  // the first pass wrote these rows
   const float scale = 1.4426950408889634f / sqrtf((float)HD);
   const size_t row = (size_t)(t.row0 + node) * hq + h, step = (size_t)rows * hq;
-  float m = -INFINITY;
-#pragma unroll 8
-  for (int z = 0; z < n; ++z) m = fmaxf(m, part_ml[row + z * step].x);
+  constexpr int U = 8;  // chunks on their way at once
+  float m = -INFINITY, den = 0.f;
   f32x4 num{0.f, 0.f, 0.f, 0.f};
-  float den = 0.f;
-#pragma unroll 8
-  for (int z = 0; z < n; ++z) {
-    const float2 ml = part_ml[row + z * step];
-    const float wt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - m) * scale);
-    const f32x4 v = *reinterpret_cast<const f32x4*>(part_o + (row + z * step) * HD + d);
+  for (int z0 = 0; z0 < n; z0 += U) {
+    float2 ml[U];
+    f32x4 v[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) num[e] += v[e] * wt;
-    den += ml.y * wt;
+    for (int u = 0; u < U; ++u) {
+      const size_t at = row + min(z0 + u, n - 1) * step;
+      ml[u] = part_ml[at];
+      v[u] = *reinterpret_cast<const f32x4*>(part_o + at * HD + d);
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+    const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * scale);
+    den *= corr;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) num[e] *= corr;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (z0 + u < n) {
+        const float wt = ml[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[u].x - top) * scale);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) num[e] += v[u][e] * wt;
+        den += ml[u].y * wt;
+      }
+    m = top;
   }
   T4 v;
 #pragma unroll
@@ -516,16 +606,19 @@ k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_len
   *reinterpret_cast<T4*>(out + row * HD + d) = v;
 }
 
-template <class T, int HD, int CT, int CW>
+template <class T, int HD, int CT, int CW, int NB>
 void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
-  constexpr int COLS = 16 * CT * CW, KW = 4 / CW, TK = STEP_KEYS<T> * steps_of<T, HD, CT, CW>();
-  constexpr int TILES = KW * (CW == 1 ? 1 : 2) * 2 * TK * HD * (int)sizeof(T), JOIN = KW > 1 ? KW * COLS * (HD + SM_PAD) * 4 : 0;
+  constexpr int COLS = 16 * CT * CW, KW = 4 / CW, TK = TILE_KEYS<T>;
+  constexpr int TILES = KW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = KW > 1 ? KW * COLS * (HD + SM_PAD) * 4 : 0;
   constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
   static std::atomic<uint64_t> lds_allowed{0};
-  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CT, CW>, SMEM, lds_allowed);
+  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CT, CW, NB>, SMEM, lds_allowed);
   const int blocks = (a.max_nodes * (a.hq / a.hkv) + COLS - 1) / COLS;
-  k_tree_mfma<T, HD, CT, CW><<<dim3(p.n, a.hkv * blocks, a.batch), 256, SMEM, st>>>(
-      a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, p.o, p.ml);
+  const long each = (long)a.hkv * blocks;  // workgroups of a sequence
+  int half = 0;
+  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = each * a.batch <= RESIDENT ? std::max(1, (int)(RESIDENT / 2 / each)) : a.batch;
+  k_tree_mfma<T, HD, CT, CW, NB><<<dim3(p.n, a.hkv * blocks, a.batch), 256, SMEM, st>>>(
+      a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, half, p.o, p.ml);
   if (p.n > 1)
     k_tree_merge<T, HD><<<dim3(a.max_nodes, a.batch, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(
         a.cu, a.seq_lens, a.rows, a.hq, a.max_seq, p.n, p.keys, p.o, p.ml, (T*)a.out);
@@ -534,10 +627,10 @@ void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
 template <class T, int HD>
 void launch_hd(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
   const int cols = a.max_nodes * (a.hq / a.hkv);
-  if (cols <= 16) launch<T, HD, 1, 1>(a, p, st);
-  else if (cols <= 32) launch<T, HD, 1, 2>(a, p, st);
-  else if (cols <= 64) launch<T, HD, 1, 4>(a, p, st);
-  else launch<T, HD, 2, 4>(a, p, st);
+  if (cols <= 16) launch<T, HD, 1, 1, 1>(a, p, st);
+  else if (cols <= 32) launch<T, HD, 1, 2, 2>(a, p, st);
+  else if (cols <= 64) launch<T, HD, 1, 4, 4>(a, p, st);
+  else launch<T, HD, 2, 4, 4>(a, p, st);
 }
 
 }  // namespace
