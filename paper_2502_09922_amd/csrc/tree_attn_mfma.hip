@@ -305,26 +305,52 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   auto attend = [&](auto tiles_, const unsigned char* ks, const unsigned char* vs, int key0, bool odd) {
     constexpr int NC = decltype(tiles_)::value;
     f32x4 s[NC][HALVES];
+    // all of a tile's keys are asked for at once, and all of its values before the softmax: with a few reads at a time each of them
+    // was waited for
+    Q kf[HALVES][KS];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
       const int kl = h * 16 + lr;
 #pragma unroll
+      for (int kk = 0; kk < KS; ++kk) kf[h][kk] = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
+#pragma unroll
       for (int c = 0; c < NC; ++c) s[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int kk = 0; kk < KS; ++kk) {
-        const Q kf = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
+    for (int kk = 0; kk < KS; ++kk) {
+      if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          if constexpr (sizeof(T) == 2) {
-            s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, ql[c][kk], s[c][h], 0, 0, 0);
-            s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qh[c][kk], s[c][h], 0, 0, 0);
-          } else {
+        for (int part = 0; part < 2; ++part)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[c][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qh[c][kk][e], s[c][h], 0, 0, 0);
-          }
-        }
+          for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], part ? qh[c][kk] : ql[c][kk], s[c][h], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) s[c][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[0][kk][e], qh[c][kk][e], s[c][0], 0, 0, 0);
       }
     }
+    Q vt[DT];  // bf16: 16 dims each; fp32: a read of four, of which there are as many
+    if constexpr (sizeof(T) == 2) {
+      const int k0 = 4 * lg + (lr >> 2), k1 = k0 + 16;
+      const int within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const int ch = d * 2 + ((lr & 3) >> 1);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<T, HD>(k0)) << 4) + within));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k1 * ROWB + ((ch ^ value_swizzle<T, HD>(k1)) << 4) + within));
+        vt[d] = __builtin_bit_cast(Q, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vt[j * 4 + e] = *reinterpret_cast<const Q*>(vs + (4 * lg + e) * ROWB + (j * 16 + lr) * 16);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     const int behind = key0 - t.ctx;  // of the cached positions
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -366,28 +392,19 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) pf[c][i] = (bf16)s[c][i >> 2][i & 3];
-      const int k0 = 4 * lg + (lr >> 2), k1 = k0 + 16;
-      const int within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const int ch = d * 2 + ((lr & 3) >> 1);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<T, HD>(k0)) << 4) + within));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k1 * ROWB + ((ch ^ value_swizzle<T, HD>(k1)) << 4) + within));
-        const bf16x8 vt = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, pf[c], o[c][d], 0, 0, 0);
-      }
+        for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf[c], o[c][d], 0, 0, 0);
     } else {
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f32x4 vt = *reinterpret_cast<const f32x4*>(vs + (4 * lg + e) * ROWB + (j * 16 + lr) * 16);
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int d = 0; d < 4; ++d) o[c][j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[d], s[c][0][e], o[c][j * 4 + d], 0, 0, 0);
-        }
+            for (int d = 0; d < 4; ++d) o[c][j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[j * 4 + e][d], s[c][0][e], o[c][j * 4 + d], 0, 0, 0);
     }
     if (odd) {  // nodes' values that are no numbers lie in the tile as zeros: only the columns that see the nodes take them
       for (int j = max(0, -behind); j < TK && behind + j < t.n; ++j) {
