@@ -8,8 +8,7 @@
 //   bf16: v_mfma_f32_16x16x32_bf16, steps of 32 keys.  The k index of the second product runs over keys {4g..4g+3, 16+4g..16+4g+3},
 // g = lane / 16; V^T comes out of transposing LDS reads of the row-major tile.  Queries are turned in fp32 and enter as a sum of two
 // bf16 (16 bits and more of them): rounded once they would move every score by 2^-9 of its size, which costs more than the
-// rounding of the output.  Weights are rounded to bf16 for the second product (their sum is of the unrounded ones), as the prompt
-// kernel does.
+// rounding of the output.  Weights are rounded to bf16 for the second product, their sums are of the rounded ones.
 //   fp32: v_mfma_f32_16x16x4_f32, steps of 16 keys.  The k index is lane / 16; a 16-byte read of a key's or a value's row serves four
 // products, of dims 16 j + 4 g + e of a key, and of rows 64 j + 4 (lane % 16) + e of V^T, which are the dims that a result's
 // lane holds 4 apart.
@@ -89,16 +88,17 @@ constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns
 
 constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds in registers
 constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
+constexpr float FOLLOW = 8.f;
 constexpr int RESIDENT = 512;      // workgroups on the chip at once
 template <class T> constexpr int TILE_KEYS = sizeof(T) == 2 ? 32 : 16;  // 16 KB of keys and values of 128 dims
 
 // NB: tiles of the ring, a power of two (CW > 1).
-template <class T, int HD, int CT, int CW, int NB>
-__global__ void __launch_bounds__(256, 2)
+template <class T, int HD, int CT, int CW, int KW, int NB>
+__global__ void __launch_bounds__(64 * CW * KW, 2)
 k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ parents, const T* __restrict__ qkv,
             const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, T* __restrict__ out, int rows, int hq, int hkv, int max_seq,
             int nchunk, int chunk_tiles, int half, float* __restrict__ part_o, float2* __restrict__ part_ml) {
-  constexpr int KW = 4 / CW;             // wavefronts that split the keys
+  constexpr int THREADS = 64 * CW * KW;
   constexpr int TK = TILE_KEYS<T>;
   constexpr int ROWB = HD * sizeof(T), EPC = 16 / sizeof(T);
   constexpr int CPR = HD / EPC;          // 16-byte chunks of a row
@@ -123,7 +123,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   if (t.n <= 0 || t.n > TREE_MAX || t.row0 < 0 || t.row0 > rows - t.n || cb * COLS >= t.n * G) return;
   if (!room) {  // the rows hold zeros
     if (z == 0 && cb == 0)
-      for (int i = threadIdx.x; i < t.n * G * HD; i += 256) {
+      for (int i = threadIdx.x; i < t.n * G * HD; i += THREADS) {
         const int c = i / HD;
         out[((size_t)(t.row0 + c / G) * hq + kh * G + c % G) * HD + i % HD] = from_f<T>(0.f);
       }
@@ -185,15 +185,20 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     const T *kt = kb + (size_t)tile * TK * HD, *vt = vb + (size_t)tile * TK * HD;
     const unsigned to = lds0 + ((tile - t_begin) & (NB - 1)) * (2 * TILE);
     const int have = keys - tile * TK;
+    if (have >= TK) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      unsigned back = 0;  // rows behind the last key: that one again, which their weights of zero leave out
-      if (have < TK) {
-        const int r = first_row + i * RPI + lrow;
-        back = (unsigned)(r - min(r, have - 1)) * ROWB;
+      for (int i = 0; i < NL; ++i) {
+        piece(kt, koff[i], to + i * 1024);
+        piece(vt, voff[i], to + TILE + i * 1024);
       }
-      piece(kt, koff[i] - back, to + i * 1024);
-      piece(vt, voff[i] - back, to + TILE + i * 1024);
+    } else {  // rows behind the last key: that one again, which their weights of zero leave out
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int r = first_row + i * RPI + lrow;
+        const unsigned back = (unsigned)(r - min(r, have - 1)) * ROWB;
+        piece(kt, koff[i] - back, to + i * 1024);
+        piece(vt, voff[i] - back, to + TILE + i * 1024);
+      }
     }
   };
   // on their way while nodes and queries are made ready: tiles without nodes
@@ -225,7 +230,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   {  // the nodes' rows among the keys of this wavefront (CW = 1) or workgroup
     const int depth = __builtin_popcountll(path) - 1;
     const int n_lo = max((CW == 1 ? t_begin : t_lo) * TK, t.ctx), items = (min((CW == 1 ? t_end : t_hi) * TK, keys) - n_lo) * CPR;
-    constexpr int STEP = CW == 1 ? 64 : 256;
+    constexpr int STEP = CW == 1 ? 64 : THREADS;
     for (int i0 = 0; i0 < items; i0 += STEP) {
       const int i = i0 + (CW == 1 ? lane : (int)threadIdx.x), key = n_lo + i / CPR, ch = i % CPR, node = min(key - t.ctx, t.n - 1);
       const int d = __shfl(depth, node);
@@ -283,11 +288,15 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   }
 
   f32x4 o[CT][DT];
-  float m_run[CT], l_run[CT];
+  float m_run[CT];
+  f32x4 l_run[CT];  // all rows of a product alike
+  bf16x8 ones;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.f;
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     m_run[c] = -INFINITY;
-    l_run[c] = 0.f;
+    l_run[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -361,30 +370,25 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[c][h][e] = seen >> (h * 16 + 4 * lg + e) & 1u ? s[c][h][e] : -INFINITY;
       }
-      float mx = -INFINITY;
+      // a NaN score makes its weight NaN, and the sums with it, whatever the maximum is
+      float mx = s[c][0][0];
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) mx = fmaxf(mx, fmaxf(fmaxf(s[c][h][0], s[c][h][1]), fmaxf(s[c][h][2], s[c][h][3])));
+      for (int i = 1; i < 4 * HALVES; ++i) mx = __builtin_elementwise_maximum(mx, s[c][i >> 2][i & 3]);
       mx = exchange<16, 32>(mx, Max{});
-      const float m_new = fmaxf(m_run[c], mx), m_ref = m_new == -INFINITY ? 0.f : m_new;
-      if (__builtin_amdgcn_ballot_w64(m_new > m_run[c]) != 0) {
-        const float corr = __builtin_amdgcn_exp2f((m_run[c] - m_ref) * scale);
+      // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: bf16 and fp32 weights above
+      // one are as exact as below.  Following every move, and adding up the sums here, took 70B, 64 ragged trees @F@
+      const float m_new = fmaxf(m_run[c], mx);
+      const bool moved = (m_new - m_run[c]) * scale > FOLLOW;  // false for (-inf, -inf)
+      if (__builtin_amdgcn_ballot_w64(moved) != 0) {           // the others keep their bits
+        const float corr = moved ? __builtin_amdgcn_exp2f((m_run[c] - m_new) * scale) : 1.f;
         l_run[c] *= corr;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[c][d][e] *= corr;
-        m_run[c] = m_new;
+        for (int d = 0; d < DT; ++d) o[c][d] *= corr;
+        m_run[c] = moved ? m_new : m_run[c];
       }
-      const float mc = m_ref * scale;
-      float sum = 0.f;
+      const float mc = m_run[c] == -INFINITY ? 0.f : m_run[c] * scale;
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[c][h][e] = __builtin_amdgcn_exp2f(fmaf(s[c][h][e], scale, -mc));
-          sum += s[c][h][e];
-        }
-      l_run[c] += sum;
+      for (int i = 0; i < 4 * HALVES; ++i) s[c][i >> 2][i & 3] = __builtin_amdgcn_exp2f(fmaf(s[c][i >> 2][i & 3], scale, -mc));
     }
     if constexpr (sizeof(T) == 2) {
       bf16x8 pf[NC];
@@ -392,11 +396,18 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) pf[c][i] = (bf16)s[c][i >> 2][i & 3];
+      // their sum is of the rounded ones, another row of the product: a single large weight then divides out
+#pragma unroll
+      for (int c = 0; c < NC; ++c) l_run[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[c], l_run[c], 0, 0, 0);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf[c], o[c][d], 0, 0, 0);
     } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) l_run[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, s[c][0][e], l_run[c], 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
@@ -450,7 +461,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   const size_t pieces = (size_t)z * rows * hq;
   auto row_of = [&](int col) { return (size_t)(t.row0 + col / G) * hq + kh * G + col % G; };
 
-  __shared__ int odd_flags[NB][4];
+  __shared__ int odd_flags[NB][CW * KW];
   unsigned char* tiles = smem + split * ((CW == 1 ? 1 : NB) * 2 * TILE);
   if constexpr (CW > 1)
     while (next < min(t_end, t_begin + NB - 1)) fill(next++);
@@ -511,7 +522,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     float* sm_o = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      const float l = exchange<16, 32>(l_run[c], Add{});
+      const float l = l_run[c][0];
       const int at = (share + CW * c) * 16 + lr;
       if (lg == 0) {
         sm_m[split][at] = m_run[c];
@@ -521,7 +532,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(sm_o + (split * COLS + at) * (HD + SM_PAD) + dim_of(i)) = piece(c, i);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < COLS * (HD / 4); i += 256) {
+    for (int i = threadIdx.x; i < COLS * (HD / 4); i += THREADS) {
       const int c = i / (HD / 4), d = i % (HD / 4) * 4, col = cb * COLS + c;
       if (col >= t.n * G) break;
       float m = -INFINITY;
@@ -552,7 +563,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       const int col = cb * COLS + (share + CW * c) * 16 + lr;
-      const float l = exchange<16, 32>(l_run[c], Add{});
+      const float l = l_run[c][0];
       if (col >= t.n * G) continue;
       const size_t row = row_of(col);
       if (whole) {
@@ -623,18 +634,18 @@ k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_len
   *reinterpret_cast<T4*>(out + row * HD + d) = v;
 }
 
-template <class T, int HD, int CT, int CW, int NB>
+template <class T, int HD, int CT, int CW, int KW, int NB>
 void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
-  constexpr int COLS = 16 * CT * CW, KW = 4 / CW, TK = TILE_KEYS<T>;
+  constexpr int COLS = 16 * CT * CW, TK = TILE_KEYS<T>;
   constexpr int TILES = KW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = KW > 1 ? KW * COLS * (HD + SM_PAD) * 4 : 0;
   constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
   static std::atomic<uint64_t> lds_allowed{0};
-  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CT, CW, NB>, SMEM, lds_allowed);
+  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CT, CW, KW, NB>, SMEM, lds_allowed);
   const int blocks = (a.max_nodes * (a.hq / a.hkv) + COLS - 1) / COLS;
   const long each = (long)a.hkv * blocks;  // workgroups of a sequence
   int half = 0;
-  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = each * a.batch <= RESIDENT ? std::max(1, (int)(RESIDENT / 2 / each)) : a.batch;
-  k_tree_mfma<T, HD, CT, CW, NB><<<dim3(p.n, a.hkv * blocks, a.batch), 256, SMEM, st>>>(
+  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = each * a.batch <= RESIDENT / (CW * KW / 4) ? std::max(1, (int)(RESIDENT / 2 / each)) : a.batch;
+  k_tree_mfma<T, HD, CT, CW, KW, NB><<<dim3(p.n, a.hkv * blocks, a.batch), 64 * CW * KW, SMEM, st>>>(
       a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, half, p.o, p.ml);
   if (p.n > 1)
     k_tree_merge<T, HD><<<dim3(a.max_nodes, a.batch, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(
@@ -644,10 +655,10 @@ void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
 template <class T, int HD>
 void launch_hd(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
   const int cols = a.max_nodes * (a.hq / a.hkv);
-  if (cols <= 16) launch<T, HD, 1, 1, 1>(a, p, st);
-  else if (cols <= 32) launch<T, HD, 1, 2, 2>(a, p, st);
-  else if (cols <= 64) launch<T, HD, 1, 4, 4>(a, p, st);
-  else launch<T, HD, 2, 4, 4>(a, p, st);
+  if (cols <= 16) launch<T, HD, 1, 1, 4, 1>(a, p, st);
+  else if (cols <= 32) launch<T, HD, 1, 2, 2, 2>(a, p, st);
+  else if (cols <= 64) launch<T, HD, 1, 4, 1, 4>(a, p, st);
+  else launch<T, HD, 2, 4, 1, 4>(a, p, st);
 }
 
 }  // namespace
