@@ -281,7 +281,7 @@ typedef struct {
   uint32_t n_q_heads;  /* query head h reads kv head h / (n_q_heads / n_kv_heads)                         */
   uint32_t n_kv_heads; /* divides n_q_heads                                                               */
   uint32_t head_dim;   /* even, at most 256                                                               */
-  uint32_t max_batch;  /* sequences the cache is laid out for                                             */
+  uint32_t max_batch;  /* sequences the cache is laid out for, below 2^24                                 */
   uint32_t max_seq;    /* positions the cache is laid out for                                             */
 } ls_heads;
 
@@ -295,7 +295,9 @@ typedef struct {
  * b has nodes [cu_nodes[b], cu_nodes[b+1]), none to LS_TREE_MAX of them; one without nodes takes no part in the call.
  *   parents        device int32 [nodes]: index of a node's parent within its own tree; the root's is not read.  A parent
  *                  that does not stand in front of its child counts as none: the child then follows the cache itself.
- *   cu_nodes       device int32 [batch+1], cu_nodes[0] = 0.   cu_nodes_host: host copy (validation and launch sizing).
+ *   cu_nodes       device int32 [batch+1], cu_nodes[0] = 0.   cu_nodes_host: host copy (validation and launch sizing).  The
+ *                  device's copy counts, for replays of a captured call too: a sequence whose bounds there leave the call's rows, or
+ *                  whose tree is larger than the call's largest, takes no part.  Rows of no sequence are left as they are.
  */
 typedef struct {
   const int32_t* parents;
@@ -361,7 +363,8 @@ ls_status ls_tree_accept(const ls_tree* tree, int batch, const int32_t* tokens, 
 ls_status ls_tree_keep(const ls_heads* heads, int layers, const ls_tree* tree, int batch, const uint64_t* kept, const ls_kv* kv, void* hip_stream);
 
 /*
- * The k best continuations of each of `groups` requests with `beams` beams (both 1..LS_BEAMS_MAX): row g * beams + b is beam b
+ * The k best continuations of each of `groups` requests with `beams` beams (k and beams 1..LS_BEAMS_MAX, at most 2^24 - 1 rows and 2^22 - 1
+ * requests, vocab at most 2^24): row g * beams + b is beam b
  * of request g, candidate (b, token) scores scores[row] + logits[row][token] - log(sum(exp(logits[row]))).  Best first; equal
  * scores go by the lower beam, then the larger logit, then the lower token.  Scores are compared in 64 bits (the sums of
  * exponentials are of fp32 terms) and rounded to fp32 on output.  A beam whose score is not finite has no candidates but at -inf,

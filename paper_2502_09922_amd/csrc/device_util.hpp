@@ -136,8 +136,9 @@ __device__ __forceinline__ int row_by_length(const int32_t* __restrict__ row_pos
   int len[C];  // position + 1: a sequence without room has 0, a row that is not there -1
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    len[c] = c * 64 + lane < rows ? row_pos[c * 64 + lane] + 1 : -1;
-    if (ANY && c * 64 + lane < rows) len[c] = min(max(len[c], 0), limit);
+    int at = c * 64 + lane < rows ? row_pos[c * 64 + lane] : -2;
+    if (ANY && c * 64 + lane < rows) at = min(max(at, -1), limit - 1);
+    len[c] = at + 1;
   }
   auto reach = [&](int v) {
     int n = 0;

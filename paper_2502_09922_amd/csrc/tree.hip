@@ -14,11 +14,11 @@ namespace {
 // the path are the tokens that the sequence has gained: those of the accepted drafts and one more.
 __global__ void __launch_bounds__(64)
 k_tree_accept(const int32_t* __restrict__ cu, const int32_t* __restrict__ parents, const int32_t* __restrict__ tokens,
-              const int32_t* __restrict__ said, int rows, uint64_t* __restrict__ kept, int32_t* __restrict__ count,
+              const int32_t* __restrict__ said, int rows, int most, uint64_t* __restrict__ kept, int32_t* __restrict__ count,
               int32_t* __restrict__ emitted, int32_t* __restrict__ following) {
   const int b = blockIdx.x, lane = threadIdx.x;
   TreeSeq t{cu[b], cu[b + 1] - cu[b], 0};
-  if (t.n < 0 || t.n > TREE_MAX || t.row0 < 0 || t.row0 > rows - t.n) t.n = 0;
+  if (t.n < 0 || t.n > most || t.row0 < 0 || t.row0 > rows - t.n) t.n = 0;
   const bool in = lane < t.n;
   const int up = in && lane > 0 ? parents[t.row0 + lane] : -1;
   const int here = in ? said[t.row0 + lane] : -1;
@@ -47,11 +47,11 @@ k_tree_accept(const int32_t* __restrict__ cu, const int32_t* __restrict__ parent
 // row.  The j-th kept node is node j or a later one, so in index order no row is overwritten before it has moved.
 template <class U>
 __global__ void __launch_bounds__(256)
-k_tree_keep(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const uint64_t* __restrict__ kept, int rows, int max_batch,
+k_tree_keep(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const uint64_t* __restrict__ kept, int rows, int most, int max_batch,
             int heads, int hkv, int max_seq, int pieces, U* __restrict__ kc, U* __restrict__ vc) {
   const int b = blockIdx.x;
   TreeSeq t;
-  if (!tree_seq(cu, seq_lens, b, rows, max_seq, t)) return;
+  if (!tree_seq(cu, seq_lens, b, rows, most, max_seq, t)) return;
   uint64_t keep = kept[b];
   if (t.n < 64) keep &= (1ull << t.n) - 1;
   const int item = blockIdx.y * 256 + threadIdx.x;
@@ -80,10 +80,10 @@ k_tree_keep(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 
 // In a launch of its own: the one before reads the lengths in every workgroup.
 __global__ void __launch_bounds__(256)
-k_tree_lens(const int32_t* __restrict__ cu, const uint64_t* __restrict__ kept, int rows, int max_seq, int batch, int32_t* __restrict__ seq_lens) {
+k_tree_lens(const int32_t* __restrict__ cu, const uint64_t* __restrict__ kept, int rows, int most, int max_seq, int batch, int32_t* __restrict__ seq_lens) {
   const int b = blockIdx.x * 256 + threadIdx.x;
   TreeSeq t;
-  if (b >= batch || !tree_seq(cu, seq_lens, b, rows, max_seq, t)) return;
+  if (b >= batch || !tree_seq(cu, seq_lens, b, rows, most, max_seq, t)) return;
   const uint64_t keep = t.n < 64 ? kept[b] & ((1ull << t.n) - 1) : kept[b];
   seq_lens[b] = t.ctx + __builtin_popcountll(keep);
 }
@@ -95,7 +95,7 @@ const char* heads_error(const ls_heads* h) {
   if (h->dtype > LS_DTYPE_BF16) return "unknown dtype";
   if (!h->n_q_heads || !h->n_kv_heads || h->n_q_heads % h->n_kv_heads || h->n_q_heads > 65535) return "n_kv_heads has to divide n_q_heads (65535 at most)";
   if (!h->head_dim || (h->head_dim & 1) || h->head_dim > 256) return "head_dim has to be even and 256 at most";
-  if (!h->max_batch || !h->max_seq || h->max_seq > (1u << 24) || h->max_batch > (1u << 24)) return "max_batch or max_seq outside [1, 2^24]";
+  if (!h->max_batch || !h->max_seq || h->max_seq > (1u << 24) || h->max_batch >= (1u << 24)) return "max_batch outside [1, 2^24) or max_seq outside [1, 2^24]";
   return nullptr;
 }
 
@@ -168,10 +168,10 @@ ls_status ls_tree_accept(const ls_tree* tree, int batch, const int32_t* tokens, 
                          int32_t* emitted, int32_t* following, void* hip_stream) {
   static const char* who = "ls_tree_accept";
   int rows = 0, min_nodes = 0, max_nodes = 0;
-  if (const char* e = ls::tree_error(tree, batch, INT32_MAX, true, &rows, &min_nodes, &max_nodes)) return bad(who, e);
+  if (const char* e = ls::tree_error(tree, batch, (1 << 24) - 1, true, &rows, &min_nodes, &max_nodes)) return bad(who, e);
   if ((rows && (!tokens || !said)) || !kept || !count || !emitted || !following) return bad(who, "NULL argument");
   if ((uintptr_t)kept & 7) return bad(who, "kept is not aligned to 8 bytes");
-  ls::k_tree_accept<<<batch, 64, 0, (hipStream_t)hip_stream>>>(tree->cu_nodes, tree->parents, tokens, said, rows, kept, count, emitted, following);
+  ls::k_tree_accept<<<batch, 64, 0, (hipStream_t)hip_stream>>>(tree->cu_nodes, tree->parents, tokens, said, rows, max_nodes, kept, count, emitted, following);
   return launched(who);
 }
 
@@ -193,13 +193,13 @@ ls_status ls_tree_keep(const ls_heads* h, int layers, const ls_tree* tree, int b
   const dim3 grid(batch, (2 * heads * pieces + 255) / 256);
   if (max_nodes > 1) {  // a root alone lies where it has to
     if (wide)
-      ls::k_tree_keep<ls::u32x4><<<grid, 256, 0, st>>>(tree->cu_nodes, kv->seq_lens, kept, rows, (int)h->max_batch, heads, (int)h->n_kv_heads,
+      ls::k_tree_keep<ls::u32x4><<<grid, 256, 0, st>>>(tree->cu_nodes, kv->seq_lens, kept, rows, max_nodes, (int)h->max_batch, heads, (int)h->n_kv_heads,
                                                    (int)h->max_seq, pieces, (ls::u32x4*)kv->k, (ls::u32x4*)kv->v);
     else
-      ls::k_tree_keep<uint32_t><<<grid, 256, 0, st>>>(tree->cu_nodes, kv->seq_lens, kept, rows, (int)h->max_batch, heads, (int)h->n_kv_heads,
+      ls::k_tree_keep<uint32_t><<<grid, 256, 0, st>>>(tree->cu_nodes, kv->seq_lens, kept, rows, max_nodes, (int)h->max_batch, heads, (int)h->n_kv_heads,
                                                       (int)h->max_seq, pieces, (uint32_t*)kv->k, (uint32_t*)kv->v);
   }
-  ls::k_tree_lens<<<(batch + 255) / 256, 256, 0, st>>>(tree->cu_nodes, kept, rows, (int)h->max_seq, batch, kv->seq_lens);
+  ls::k_tree_lens<<<(batch + 255) / 256, 256, 0, st>>>(tree->cu_nodes, kept, rows, max_nodes, (int)h->max_seq, batch, kv->seq_lens);
   return launched(who);
 }
 

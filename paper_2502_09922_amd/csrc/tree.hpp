@@ -19,14 +19,15 @@ struct TreeSeq {
   int row0, n, ctx;  // rows [row0, row0 + n) of the call, cached positions
 };
 
-// The tree of sequence b.  False for one that does not take part: no nodes, no room for them behind its cached
-// positions, or bounds on the device that are not those of the call (`rows`), which then reach nothing.
-__device__ __forceinline__ bool tree_seq(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, int b, int rows, int max_seq,
-                                         TreeSeq& t) {
+// The tree of sequence b.  False for one that does not take part: no nodes, no room for them behind its cached positions, or
+// bounds on the device that the call was not made for (`rows` in all, `most` of a tree: TREE_MAX at most), which count as none.
+__device__ __forceinline__ bool tree_seq(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, int b, int rows, int most,
+                                         int max_seq, TreeSeq& t) {
   t.row0 = cu[b];
   t.n = cu[b + 1] - t.row0;
   t.ctx = seq_lens[b];
-  return t.n > 0 && t.n <= TREE_MAX && t.row0 >= 0 && t.row0 <= rows - t.n && t.ctx >= 0 && t.ctx <= max_seq - t.n;
+  if (t.n < 0 || t.n > most || t.row0 < 0 || t.row0 > rows - t.n) t.n = 0;
+  return t.n > 0 && t.ctx >= 0 && t.ctx <= max_seq - t.n;
 }
 
 // Lane i: the nodes on the path from the root to node i, itself included, as bits; 0 for lanes without a node.  A parent that

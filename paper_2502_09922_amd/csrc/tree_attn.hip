@@ -15,10 +15,10 @@ namespace {
 template <class T>
 __global__ void __launch_bounds__(256)
 k_tree_append(const T* __restrict__ qkv, const float2* __restrict__ cs, const int32_t* __restrict__ cu, const int32_t* __restrict__ parents,
-              const int32_t* __restrict__ seq_lens, int rows, int hq, int hkv, int hd, int max_seq, T* __restrict__ kc, T* __restrict__ vc) {
+              const int32_t* __restrict__ seq_lens, int rows, int most, int hq, int hkv, int hd, int max_seq, T* __restrict__ kc, T* __restrict__ vc) {
   const int b = blockIdx.x, kh = blockIdx.y;
   TreeSeq t;
-  if (!tree_seq(cu, seq_lens, b, rows, max_seq, t)) return;
+  if (!tree_seq(cu, seq_lens, b, rows, most, max_seq, t)) return;
   __shared__ int depth[TREE_MAX];
   const uint64_t path = tree_path(parents, t);
   if (threadIdx.x < 64) depth[threadIdx.x] = __builtin_popcountll(path) - 1;
@@ -49,15 +49,16 @@ k_tree_append(const T* __restrict__ qkv, const float2* __restrict__ cs, const in
 template <class T>
 __global__ void __launch_bounds__(64)
 k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int32_t* __restrict__ cu, const int32_t* __restrict__ parents,
-            const int32_t* __restrict__ seq_lens, int rows, int hq, int hkv, int hd, int max_seq, const T* __restrict__ kc,
+            const int32_t* __restrict__ seq_lens, int rows, int most, int hq, int hkv, int hd, int max_seq, const T* __restrict__ kc,
             const T* __restrict__ vc, T* __restrict__ out) {
   constexpr int MAXP = 2;  // pairs of a lane: head_dim <= 256
   const int b = blockIdx.x, node = blockIdx.y, h = blockIdx.z, lane = threadIdx.x, half = hd >> 1;
-  const int row0 = cu[b], n = cu[b + 1] - row0;
-  if (node >= n || row0 < 0 || row0 + node >= rows) return;
-  T* o = out + (size_t)(row0 + node) * hq * hd + (size_t)h * hd;
   TreeSeq t;
-  if (!tree_seq(cu, seq_lens, b, rows, max_seq, t)) {  // no room: the rows hold zeros
+  const bool room = tree_seq(cu, seq_lens, b, rows, most, max_seq, t);
+  if (node >= t.n) return;
+  const int row0 = t.row0;
+  T* o = out + (size_t)(row0 + node) * hq * hd + (size_t)h * hd;
+  if (!room) {  // no room: the rows hold zeros
     for (int i = lane; i < hd; i += 64) o[i] = from_f<T>(0.f);
     return;
   }
@@ -118,20 +119,23 @@ k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int3
 
 template <class T>
 void launch_any(const TreeAttn& a, hipStream_t st) {
-  k_tree_append<T><<<dim3(a.batch, a.hkv), 256, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.hq, a.hkv, a.hd,
+  k_tree_append<T><<<dim3(a.batch, a.hkv), 256, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.max_nodes, a.hq, a.hkv, a.hd,
                                                          a.max_seq, (T*)a.kc, (T*)a.vc);
-  k_tree_attn<T><<<dim3(a.batch, a.max_nodes, a.hq), 64, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.hq,
+  k_tree_attn<T><<<dim3(a.batch, a.max_nodes, a.hq), 64, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.max_nodes, a.hq,
                                                                   a.hkv, a.hd, a.max_seq, (const T*)a.kc, (const T*)a.vc, (T*)a.out);
 }
 
-// Chunks of a call.  One workgroup to a (sequence, kv head, block of columns) where they fill the chip, two to a CU; fewer are
-// cut along the keys, into pieces of CHUNK_MIN keys at least.
-constexpr int WG_TARGET = 512, CHUNK_MIN = 256;
+// Chunks of a call.  One workgroup to a (sequence, kv head, block of columns) where they fill the chip; fewer are cut along the keys
+// until each CU has one, in pieces of 128 keys at least.  More than 32 columns, whose wavefronts wait for each other, want two to a CU
+// and, as more rows are joined, 256 keys.  7B, one sequence of 3000 keys, 26 nodes: 18.3 us for 256 workgroups, 20.0 for 512; 8 of 900
+// keys 33.3 and 35.9; 600 keys, 5 nodes in pieces of 128 10.3, of 256 11.4.  70B, 16 ragged sequences of up to 3000 keys, 16 nodes (128
+// columns): 67 us for 256 workgroups, 57 for 512; one of 4000 keys, 8 nodes in pieces of 128 20.2, of 256 15.8.
 TreeChunks chunks_for(const TreeAttn& a) {
   TreeChunks p;
   const int cols = a.max_nodes * (a.hq / a.hkv), wide = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
   const long base = (long)a.batch * a.hkv * ((cols + wide - 1) / wide);
-  const long want = std::min((WG_TARGET + base - 1) / base, (long)(a.max_keys + CHUNK_MIN - 1) / CHUNK_MIN);
+  const long target = cols <= 32 ? 256 : 512, least = cols <= 32 ? 128 : 256;
+  const long want = std::min((target + base - 1) / base, (a.max_keys + least - 1) / least);
   p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
   p.n = (a.max_keys + p.keys - 1) / p.keys;
   return p;
@@ -160,8 +164,8 @@ void launch_tree_attn(uint32_t dt, const TreeAttn& a, hipStream_t st) {
       p.keys = ((a.max_keys + std::max(fit, 1) - 1) / std::max(fit, 1) + 63) / 64 * 64;
       p.n = (a.max_keys + p.keys - 1) / p.keys;
     }
-    p.ml = (float2*)a.scratch;
-    p.o = a.scratch ? a.scratch + ((size_t)p.n * a.rows * a.hq * 2) : nullptr;
+    p.o = a.scratch;
+    p.ml = a.scratch ? (float2*)(a.scratch + (size_t)p.n * a.rows * a.hq * a.hd) : nullptr;
     launch_tree_attn_mfma(dt, a, p, st);
     return;
   }

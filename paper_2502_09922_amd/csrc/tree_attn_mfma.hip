@@ -96,7 +96,7 @@ template <class T> constexpr int TILE_KEYS = sizeof(T) == 2 ? 32 : 16;  // 16 KB
 template <class T, int HD, int CT, int CW, int KW, int NB>
 __global__ void __launch_bounds__(64 * CW * KW, 2)
 k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ parents, const T* __restrict__ qkv,
-            const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, T* __restrict__ out, int rows, int hq, int hkv, int max_seq,
+            const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, T* __restrict__ out, int rows, int most, int hq, int hkv, int max_seq,
             int nchunk, int chunk_tiles, int half, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   constexpr int THREADS = 64 * CW * KW;
   constexpr int TK = TILE_KEYS<T>;
@@ -119,8 +119,8 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TreeSeq t;
-  const bool room = tree_seq(cu, seq_lens, b, rows, max_seq, t);
-  if (t.n <= 0 || t.n > TREE_MAX || t.row0 < 0 || t.row0 > rows - t.n || cb * COLS >= t.n * G) return;
+  const bool room = tree_seq(cu, seq_lens, b, rows, most, max_seq, t);
+  if (cb * COLS >= t.n * G) return;
   if (!room) {  // the rows hold zeros
     if (z == 0 && cb == 0)
       for (int i = threadIdx.x; i < t.n * G * HD; i += THREADS) {
@@ -376,7 +376,8 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       for (int i = 1; i < 4 * HALVES; ++i) mx = __builtin_elementwise_maximum(mx, s[c][i >> 2][i & 3]);
       mx = exchange<16, 32>(mx, Max{});
       // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: bf16 and fp32 weights above
-      // one are as exact as below.  Following every move, and adding up the sums here, took 70B, 64 ragged trees @F@
+      // one are as exact as below.  Following every move, and adding up the sums here, took 70B, 64 ragged
+      // trees 97 us instead of 92.
       const float m_new = fmaxf(m_run[c], mx);
       const bool moved = (m_new - m_run[c]) * scale > FOLLOW;  // false for (-inf, -inf)
       if (__builtin_amdgcn_ballot_w64(moved) != 0) {           // the others keep their bits
@@ -585,39 +586,48 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   }
 }
 
-// Rows of sequences of several chunks: the chunks' results in chunk order, four dims to a thread.
+// Rows of sequences of several chunks: the chunks' results in chunk order, four dims to a thread.  They are asked for before it is known
+// whose row this is, and how many of them there are.
 template <class T, int HD>
 __global__ void __launch_bounds__(256)
-k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, int rows, int hq, int max_seq, int nchunk, int chunk_keys,
-             const float* __restrict__ part_o, const float2* __restrict__ part_ml, T* __restrict__ out) {
+k_tree_merge(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
+             int rows, int most, int hq, int batch, int max_seq, int nchunk, int chunk_keys, T* __restrict__ out) {
   typedef T T4 __attribute__((ext_vector_type(4)));
-  constexpr int TPR = HD / 4;
-  const int node = blockIdx.x, b = blockIdx.y, h = blockIdx.z * (256 / TPR) + threadIdx.x / TPR, d = threadIdx.x % TPR * 4;
-  TreeSeq t;
-  if (!tree_seq(cu, seq_lens, b, rows, max_seq, t) || node >= t.n || h >= hq) return;
-  const int n = min((t.ctx + t.n + chunk_keys - 1) / chunk_keys, nchunk);
-  if (n == 1) return;  // the first pass wrote these rows
-  const float scale = 1.4426950408889634f / sqrtf((float)HD);
-  const size_t row = (size_t)(t.row0 + node) * hq + h, step = (size_t)rows * hq;
-  constexpr int U = 8;  // chunks on their way at once
-  float m = -INFINITY, den = 0.f;
-  f32x4 num{0.f, 0.f, 0.f, 0.f};
-  for (int z0 = 0; z0 < n; z0 += U) {
-    float2 ml[U];
-    f32x4 v[U];
+  constexpr int TPR = HD / 4, U = 8;  // chunks on their way at once
+  const int r = blockIdx.x, h = min((int)(blockIdx.y * (256 / TPR) + threadIdx.x / TPR), hq - 1), d = threadIdx.x % TPR * 4;
+  const size_t row = (size_t)r * hq + h, step = (size_t)rows * hq;
+  float2 ml[U];
+  f32x4 v[U];
+  auto load = [&](int z0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const size_t at = row + min(z0 + u, n - 1) * step;
+      const size_t at = row + min(z0 + u, nchunk - 1) * step;
       ml[u] = part_ml[at];
       v[u] = *reinterpret_cast<const f32x4*>(part_o + at * HD + d);
     }
+  };
+  load(0);
+  int b = 0, end = batch;  // the sequence with cu[b] <= r < cu[b + 1]
+  while (end - b > 1) {
+    const int mid = (b + end) >> 1;
+    if (cu[mid] <= r) b = mid;
+    else end = mid;
+  }
+  TreeSeq t;
+  if (!tree_seq(cu, seq_lens, b, rows, most, max_seq, t) || r < t.row0 || r >= t.row0 + t.n) return;
+  const int n = min((t.ctx + t.n + chunk_keys - 1) / chunk_keys, nchunk);
+  if (n == 1) return;  // the first pass wrote these rows
+  const float scale = 1.4426950408889634f / sqrtf((float)HD);
+  float m = -INFINITY, den = 0.f;
+  f32x4 num{0.f, 0.f, 0.f, 0.f};
+  for (int z0 = 0; z0 < n; z0 += U) {
+    if (z0) load(z0);
     float top = m;
 #pragma unroll
-    for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);
+    for (int u = 0; u < U; ++u) top = z0 + u < n ? fmaxf(top, ml[u].x) : top;
     const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * scale);
     den *= corr;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) num[e] *= corr;
+    num *= corr;
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (z0 + u < n) {
@@ -628,10 +638,10 @@ k_tree_merge(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_len
       }
     m = top;
   }
-  T4 v;
+  T4 w;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = from_f<T>(num[e] / den);
-  *reinterpret_cast<T4*>(out + row * HD + d) = v;
+  for (int e = 0; e < 4; ++e) w[e] = from_f<T>(num[e] / den);
+  *reinterpret_cast<T4*>(out + row * HD + d) = w;
 }
 
 template <class T, int HD, int CT, int CW, int KW, int NB>
@@ -646,10 +656,10 @@ void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
   int half = 0;
   if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = each * a.batch <= RESIDENT / (CW * KW / 4) ? std::max(1, (int)(RESIDENT / 2 / each)) : a.batch;
   k_tree_mfma<T, HD, CT, CW, KW, NB><<<dim3(p.n, a.hkv * blocks, a.batch), 64 * CW * KW, SMEM, st>>>(
-      a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, half, p.o, p.ml);
+      a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.max_nodes, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, half, p.o, p.ml);
   if (p.n > 1)
-    k_tree_merge<T, HD><<<dim3(a.max_nodes, a.batch, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(
-        a.cu, a.seq_lens, a.rows, a.hq, a.max_seq, p.n, p.keys, p.o, p.ml, (T*)a.out);
+    k_tree_merge<T, HD><<<dim3(a.rows, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(p.o, p.ml, a.cu, a.seq_lens, a.rows, a.max_nodes, a.hq, a.batch, a.max_seq,
+                                                                                       p.n, p.keys, (T*)a.out);
 }
 
 template <class T, int HD>

@@ -112,3 +112,12 @@ def test_tensors_on_the_host_are_refused():
         b.beam_select(torch.zeros(4, 10), torch.zeros(4), beams=2, k=2)
     with pytest.raises(ValueError):
         b.tree_accept(*[torch.zeros(3, dtype=torch.int32)] * 3, torch.zeros(2, dtype=torch.int32), [0, 3])
+
+
+@pytest.mark.parametrize("wrong", [dict(groups=1 << 22), dict(groups=1 << 20, beams=16)], ids=str)
+def test_selections_that_no_launch_takes(wrong):
+    assert select(**wrong) == b.LS_ERR_INVALID_ARG and b.lib.ls_beam_select_scratch_bytes(wrong["groups"], wrong.get("beams", 3), 10, 4) == 0
+
+
+def test_batches_that_no_launch_takes():
+    assert b.lib.ls_kv_reorder(C.byref(heads(max_batch=1 << 24)), 1, HERE, 4, 2, None, 50, C.byref(b.ls_kv(HERE, HERE, HERE)), None) == b.LS_ERR_INVALID_ARG

@@ -123,3 +123,55 @@ def test_the_best_lie_side_by_side(beams, vocab, k):
     check(fall.repeat(beams, 1), -torch.arange(beams).float() / 1e5, beams, k)
     check(torch.zeros(beams, vocab), torch.zeros(beams), beams, k)
     check(torch.full((beams, vocab), -math.inf), torch.zeros(beams), beams, k)
+
+
+def test_reorder_captured_and_replayed():
+    from paper_2502_09922_amd import kv_reorder
+
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn(2, 8, 2, 40, 64, generator=g).bfloat16() for _ in range(2))
+    gk, gv = k.cuda(), v.cuda()
+    src, lens = torch.arange(8, dtype=torch.int32).cuda(), torch.full((8,), 33, dtype=torch.int32).cuda()
+    kv_reorder(src, 4, gk, gv, lens, max_ctx=40)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kv_reorder(src, 4, gk, gv, lens, max_ctx=40)
+    assert torch.equal(gk.cpu(), k)
+    n = torch.full((8,), 33, dtype=torch.int32)
+    for moves in ([1, 2, 3, 0, 4, 4, 4, 5], [0, 0, 0, 0, 7, 6, 5, 4], [3, 3, 1, 2, 4, 5, 6, 7]):
+        src.copy_(torch.tensor(moves, dtype=torch.int32))
+        lens[7] = 20 + moves[0]
+        n[7] = 20 + moves[0]
+        graph.replay()
+        torch.cuda.synchronize()
+        old = k.clone(), v.clone()
+        for b, s in enumerate(moves):
+            k[:, b, :, : n[s]], v[:, b, :, : n[s]] = old[0][:, s, :, : n[s]], old[1][:, s, :, : n[s]]
+        n = n[moves]
+        assert torch.equal(gk.cpu(), k) and torch.equal(gv.cpu(), v) and torch.equal(lens.cpu(), n)
+
+
+def test_calls_on_streams_of_their_own():
+    """Selections and reorderings on two streams at once, each behind the work that makes its inputs."""
+    from paper_2502_09922_amd import beam_select, kv_reorder
+
+    sides, runs = [torch.cuda.Stream() for _ in range(2)], []
+    for i in range(6):
+        g = torch.Generator().manual_seed(i)
+        logits, scores = torch.randn(12, 20011, generator=g), torch.randn(12, generator=g)
+        k = torch.randn(1, 12, 2, 30, 64, generator=g)
+        want = beam_select(logits.cuda(), scores.cuda(), beams=4, k=4)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(sides[i % 2]):
+            a, gk = logits.cuda() * 1, k.cuda() * 1
+            got = beam_select(a, scores.cuda(), beams=4, k=4)
+            gv, lens = gk.clone(), torch.full((12,), 30, dtype=torch.int32, device="cuda")
+            kv_reorder(got[0].view(-1), 4, gk, gv, lens, max_ctx=30)
+            runs.append((want, got, k, gk, gv))
+    for s in sides:
+        s.synchronize()
+    for want, got, k, gk, gv in runs:
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+        moved = k[:, want[0].view(-1).long().cpu()]
+        assert torch.equal(gk.cpu(), moved) and torch.equal(gv.cpu(), moved)

@@ -279,3 +279,137 @@ def test_keep(heads, dtype, layers):
             c[:, b, :, ctx : ctx + len(kept)] = c[:, b, :, [ctx + i for i in kept]].clone()
         lens[b] = ctx + len(kept)
     assert torch.equal(gk.cpu(), k) and torch.equal(gv.cpu(), v) and torch.equal(gl.cpu(), lens)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_offsets_beyond_32_bits(dtype):
+    """A cache of 2^32 values and more: keys are all alike, so that the softmax counts them; nodes, values and moved rows lie at its end."""
+    from paper_2502_09922_amd import kv_reorder, tree_attention, tree_keep
+
+    S, hd, n = 1 << 24, 64, 5
+    ctx = S - 9
+    k, v = (torch.zeros(5, 1, S, hd, dtype=dtype, device="cuda") for _ in range(2))
+    v[4, 0, ctx - 1000 : ctx] = 1.0
+    qkv = torch.zeros(n, 3 * hd, dtype=dtype, device="cuda")
+    qkv[:, 2 * hd :] = torch.arange(1, n + 1, device="cuda")[:, None] * 256.0
+    cu_host = np.array([0, 0, 0, 0, 0, n], np.int32)
+    cu, parents = torch.from_numpy(cu_host).cuda(), torch.tensor([-1, 0, 0, 2, 1], dtype=torch.int32).cuda()
+    lens = torch.tensor([0, 0, 0, 0, ctx], dtype=torch.int32).cuda()
+    out = tree_attention(qkv, parents, cu, cu_host, None, k, v, lens, ctx).double().cpu()
+    for i, seen in enumerate(([0], [0, 1], [0, 2], [0, 2, 3], [0, 1, 4])):
+        want = (1000 + 256 * sum(j + 1 for j in seen)) / (ctx + len(seen))
+        # weights of one and sums of whole numbers below 2^24, of which the last ones are rounded: 2^-24 each of up to ctx + 5 terms
+        # where a wavefront's share of the keys is at most 2^16, so 2^-8 of it; the output's own rounding
+        assert (out[i] - want).abs().max() <= want * (U[dtype] + 2.0**-8)
+    assert torch.equal(v[4, 0, ctx : ctx + n, 0].cpu().double(), torch.arange(1, n + 1).double() * 256)
+    tree_keep(torch.tensor([0, 0, 0, 0, 0b11001], device="cuda"), cu, cu_host, k[None], v[None], lens)
+    assert lens.tolist() == [0, 0, 0, 0, ctx + 3] and v[4, 0, ctx : ctx + 3, 7].tolist() == [256.0, 1024.0, 1280.0]
+    src = torch.tensor([0, 1, 2, 4, 4], dtype=torch.int32, device="cuda")
+    kv_reorder(src, 5, k[None], v[None], lens, S, first=torch.full((5,), ctx - 3, dtype=torch.int32, device="cuda"))
+    assert torch.equal(v[3, 0, ctx - 3 : ctx + 3], v[4, 0, ctx - 3 : ctx + 3]) and (v[3, 0, : ctx - 3] == 0).all() and lens.tolist()[3] == ctx + 3
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads", [(8, 8, 128), (39, 13, 64), (104, 13, 64), (208, 13, 64)], ids=lambda h: "%dx%dx%d" % h)
+def test_lengths_in_any_order_and_outside_the_cache(heads, dtype):
+    """Sequences that are taken by length, among them lengths that the device alone knows: negative, too long, past 31 bits."""
+    r = random.Random(12)
+    ctxs, nodes = [r.randrange(600) for _ in range(40)], [8 if b % 13 == 5 else 1 for b in range(40)]
+    ctxs[20] = 599
+    c = make(heads, dtype, ctxs, nodes, 12, max_seq=620)
+    for b, n in ((1, -5), (3, 620), (7, 2**31 - 1), (8, -(2**31))):
+        c["lens"][b] = n
+    check(c, call(c, max_ctx=599), skipped=(1, 3, 7, 8))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_more_sequences_than_are_ordered(dtype):
+    r = random.Random(13)
+    n = 300
+    c = make((2, 1, 64), dtype, [r.randrange(40) if b % 50 else 550 for b in range(n)], [r.randrange(3) for _ in range(n)], 13)
+    check(c, call(c))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("what", ["qkv", "k", "v", "rope", "out"])
+def test_buffers_off_16_bytes(what, dtype):
+    """Views that start a row's alignment off: the kernels for every shape take them."""
+    from paper_2502_09922_amd import tree_attention
+
+    c = make((4, 2, 64), dtype, [20, 33], [5, 9], 14)
+    d = {n: c[n].cuda() for n in ("qkv", "k", "v", "rope", "lens", "parents")}
+    d["out"] = torch.zeros(14, 4 * 64, dtype=dtype, device="cuda")
+    at = torch.zeros(d[what].numel() + 8, dtype=d[what].dtype, device="cuda")[2 : 2 + d[what].numel()].view(d[what].shape)
+    at.copy_(d[what])
+    d[what] = at
+    assert at.data_ptr() % 16
+    out = tree_attention(d["qkv"], d["parents"], torch.from_numpy(c["cu"]).cuda(), c["cu"], d["rope"], d["k"], d["v"], d["lens"], 33, out=d["out"])
+    assert out is d["out"]
+    check(c, (out.cpu(), d["k"].cpu(), d["v"].cpu()))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_scratch_of_any_size(dtype):
+    """None, too little, enough: the same results but for the order of sums; a byte behind its end stays."""
+    from paper_2502_09922_amd import binding as b
+
+    c = make((6, 3, 128), dtype, [900, 3], [5, 1], 15)
+    d = {n: c[n].cuda() for n in ("qkv", "rope", "lens", "parents")}
+    cu, heads = torch.from_numpy(c["cu"]).cuda(), b.ls_heads(int(dtype == torch.bfloat16), 6, 3, 128, c["k"].shape[0], c["k"].shape[2])
+    tree = b.ls_tree(d["parents"].data_ptr(), cu.data_ptr(), c["cu"].__array_interface__["data"][0])
+    need = b.lib.ls_tree_attention_scratch_bytes(b.C.byref(heads), b.C.byref(tree), 2, 900)
+    assert need > 0
+    stream = torch.cuda.current_stream().cuda_stream
+    for nb in (0, 16, need // 3, need - 1, need):
+        out, k, v = torch.zeros(6, 6 * 128, dtype=dtype, device="cuda"), c["k"].cuda(), c["v"].cuda()
+        scratch = torch.full((need + 64,), 77, dtype=torch.uint8, device="cuda")
+        kv = b.ls_kv(k.data_ptr(), v.data_ptr(), d["lens"].data_ptr())
+        assert b.lib.ls_tree_attention(b.C.byref(heads), b.C.byref(tree), 2, 900, d["qkv"].data_ptr(), d["rope"].data_ptr(), b.C.byref(kv), out.data_ptr(),
+                                       scratch.data_ptr() if nb else None, nb, stream) == b.LS_OK
+        check(c, (out.cpu(), k.cpu(), v.cpu()))
+        assert (scratch[nb:] == 77).all()
+
+
+@pytest.mark.parametrize("heads", [(4, 2, 128), (4, 4, 80)], ids=lambda h: "%dx%dx%d" % h)
+@pytest.mark.parametrize("now", [[2, 0, 9], [0, 4, 3], [9, 9, 1], [3, 10, 2], [12, 3, 1]], ids=str)
+def test_replayed_with_other_trees(heads, now):
+    """A captured call whose bounds on the device change: smaller trees; trees that exceed its rows or its largest tree take no part."""
+    from paper_2502_09922_amd import tree_accept, tree_attention, tree_keep
+
+    most = [9, 8, 5]
+    c = make(heads, torch.bfloat16, [40, 700, 3], now, 16, max_seq=740)
+    rows = sum(most)
+    qkv, parents = torch.zeros(rows, c["qkv"].shape[1], dtype=torch.bfloat16), torch.zeros(rows, dtype=torch.int32)
+    qkv[: len(c["qkv"])], parents[: len(c["parents"])] = c["qkv"][:rows], c["parents"][:rows]
+    host = np.cumsum([0] + most).astype(np.int32)
+    d = {n: c[n].cuda() for n in ("k", "v", "rope", "lens")}
+    qkv, parents, cu, tokens = qkv.cuda(), parents.cuda(), torch.from_numpy(host).cuda(), torch.zeros(rows, dtype=torch.int32).cuda()
+    out = torch.full((rows, heads[0] * heads[2]), 7.0, dtype=torch.bfloat16, device="cuda")
+    kept = torch.full((3,), -1, dtype=torch.int64, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    tree_attention(qkv, parents, cu, host, d["rope"], c["k"].cuda(), c["v"].cuda(), d["lens"], 700)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        tree_attention(qkv, parents, cu, host, d["rope"], d["k"], d["v"], d["lens"], 700, out=out)
+        accepted = tree_accept(tokens, tokens, parents, cu, host)
+        tree_keep(kept, cu, host, d["k"][None], d["v"][None], d["lens"])
+    cu.copy_(torch.from_numpy(c["cu"]))
+    graph.replay()
+    torch.cuda.synchronize()
+    part = [n if n <= max(most) and c["cu"][b + 1] <= rows else 0 for b, n in enumerate(now)]
+    assert d["lens"][:3].tolist() == [ctx + n for ctx, n in zip(c["ctxs"], part)]
+    deepest = [max(len(plain.path(t, i)) for i in range(len(t))) if n else 0 for t, n in zip(c["trees"], part)]
+    assert accepted[1].tolist() == deepest
+    there = torch.zeros(rows, dtype=torch.bool)
+    for b, n in enumerate(part):
+        there[c["cu"][b] : c["cu"][b] + n] = True
+    got = out.cpu()
+    assert (got[~there] == 7).all()
+    k, v = d["k"].cpu(), d["v"].cpu()
+    for b, n in enumerate(part):
+        if n != now[b]:
+            assert same(k[b], c["k"][b]) and same(v[b], c["v"][b])
+    alone = dict(c, trees=[t if n else [] for t, n in zip(c["trees"], part)])
+    full = torch.zeros(max(rows, int(c["cu"][-1])), got.shape[1], dtype=got.dtype)
+    full[:rows] = got
+    check(alone, (full, k, v))
