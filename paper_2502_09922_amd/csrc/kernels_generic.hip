@@ -43,8 +43,8 @@ __global__ void k_seq_lens_inc(int batch, int max_seq, int32_t* seq_lens) {
 }
 
 // One decode step's bookkeeping and first-layer inputs in a single launch, one workgroup
-// per sequence: row maps, seq_lens += 1 (a full sequence is left alone and marked -1), the
-// fp32 residual row, its bf16 copy, and the sum of squares of every 16-column tile.
+// per sequence: row maps, seq_lens += 1 (a full sequence is left alone and marked -1; neither for
+// nodes of trees, whose rows come without seq_lens), the fp32 residual row, its bf16 copy, and the sum of squares of every 16-column tile.
 template <class T>
 __global__ void __launch_bounds__(256) k_decode_prologue(const T* __restrict__ table, const void* __restrict__ in,
                                                          int32_t* seq_lens, int max_seq, int d, int vocab,
@@ -52,7 +52,7 @@ __global__ void __launch_bounds__(256) k_decode_prologue(const T* __restrict__ t
                                                          float* __restrict__ x, T* __restrict__ xb,
                                                          float* __restrict__ ss_part, const T* __restrict__ gamma) {
   const int b = blockIdx.x;
-  if (threadIdx.x == 0) {
+  if (threadIdx.x == 0 && seq_lens) {
     const int p = seq_lens[b];
     const bool ok = p >= 0 && p < max_seq;
     row_seq[b] = b;

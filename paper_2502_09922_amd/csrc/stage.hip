@@ -140,6 +140,9 @@ struct Carve {
 // more than 64 MiB of partial tiles are never wanted: a call that long fills the chip without splits
 constexpr size_t TILED_SCRATCH_MAX = 64u << 20;
 
+// most rows of a pass with the norms inside its GEMMs: a generation step's, or a few nodes of trees
+size_t fused_rows(const ls_cfg* c) { return std::max(c->max_batch, std::min(c->max_tokens, 16u)); }
+
 Carve carve(const ls_cfg* c, int lo, int hi) {
   Carve w{};
   const size_t e = isz(c), T = c->max_tokens, B = c->max_batch, d = c->hidden;
@@ -159,10 +162,11 @@ Carve carve(const ls_cfg* c, int lo, int hi) {
   w.last_rows = take(B * sizeof(int32_t));
   w.next_tok = take(B * sizeof(int32_t));
   // decode-step fusion: bf16 copies of the residual rows and per-tile sums of squares
-  w.xb = take(B * d * e);
-  w.xb2 = take(B * d * e);
-  w.ss_a = take(B * ((d + 15) / 16) * sizeof(float));
-  w.ss_b = take(B * ((d + 15) / 16) * sizeof(float));
+  const size_t fused = fused_rows(c);
+  w.xb = take(fused * d * e);
+  w.xb2 = take(fused * d * e);
+  w.ss_a = take(fused * ((d + 15) / 16) * sizeof(float));
+  w.ss_b = take(fused * ((d + 15) / 16) * sizeof(float));
   {
     // split-K scratch: the weight-streaming GEMMs for 17..64 rows (bf16: hidden sizes above 8192, logits at an
     // odd address)
@@ -636,10 +640,22 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   const bool few_rows = dt == BF16 && rows <= (d > 4096 ? 8 : 16);
 
   // ---- decode step with the RMSNorms folded into the weight-streaming GEMMs
-  const bool fused = !prefill && !trees && dt == BF16 && d % 16 == 0 && (few_rows || !rows_supported(d)) &&
-                     (attn_decode_supported(hq, hkv, hd) || attn_decode_gqa_supported(hq, hkv, hd)) &&
+  const bool fused = !prefill && dt == BF16 && (size_t)rows <= fused_rows(&c) && d % 16 == 0 && (few_rows || !rows_supported(d)) &&
+                     (trees || attn_decode_supported(hq, hkv, hd) || attn_decode_gqa_supported(hq, hkv, hd)) &&
                      gemm_decode_fusable(rows, qkv_cols, d) && gemm_decode_fusable(rows, d, hq * hd) &&
                      gemm_decode_fusable(rows, F, d) && gemm_decode_fusable(rows, d, F);
+  // rows of the head: the sequences' last ones, or all nodes, which without logits_out go max_batch at a time, as many as the
+  // workspace has logits for
+  const int heads = trees ? rows : batch, heads_at_once = logits_out ? heads : std::min(heads, (int)c.max_batch);
+  auto attend_trees = [&](const void* qkv, char* kc, char* vc, void* attn) {
+    TreeAttn a = *trees;
+    a.qkv = qkv; a.cs = cs; a.kc = kc; a.vc = vc; a.out = attn;
+    // the GEMMs' partial tiles are added up by now, their room is the larger one mostly
+    const bool tiles = s->w.splitk_bytes > s->w.attn_part_bytes;
+    a.scratch = (float*)(ws + (tiles ? s->w.splitk : s->w.attn_part));
+    a.scratch_bytes = tiles ? s->w.splitk_bytes : s->w.attn_part_bytes;
+    launch_tree_attn(dt, a, st);
+  };
   if (fused) {
     __bf16* xb = (__bf16*)(ws + s->w.xb);
     __bf16* xb2 = (__bf16*)(ws + s->w.xb2);
@@ -671,9 +687,9 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       block_tensors(&c, hb->layer, head_sp, nullptr);
       head = s->slab + hb->off;
     }
-    const bool head_folds = hb && rows <= 16 && gemm_decode_fusable(rows, (int)c.vocab, d);
+    const bool head_folds = hb && rows <= 16 && heads_at_once == heads && gemm_decode_fusable(rows, (int)c.vocab, d);
     LS_HIP(gate(s->blocks[s->layer0], st));  // the gate of the first layer
-    launch_decode_prologue(dt, table, in, kv->seq_lens, batch, c.max_seq, d, c.vocab, row_seq, row_pos, last_rows, x,
+    launch_decode_prologue(dt, table, in, trees ? nullptr : kv->seq_lens, rows, c.max_seq, d, c.vocab, row_seq, row_pos, last_rows, x,
                            xb, ss_a, gain(0, 0), st);
     for (int li = 0; li < n_layers; ++li) {
       Block& b = s->blocks[s->layer0 + li];
@@ -692,10 +708,13 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       f_dn.xb_out = (!more && !s->last) ? (__bf16*)out : xb; f_dn.ss_out = ss_a;
       f_dn.gamma_out = more ? gain(li + 1, 0) : head_folds ? (const __bf16*)(head + head_sp[0].off) : nullptr;
       PROBE(LS_OP_GEMM_QKV, launch_gemm(dt, EPI_STORE, xb, base + sp[1].off, rows, qkv_cols, d, qkv, nullptr, st, &gsc, &f_qkv));
-      PROBE(LS_OP_ATTENTION, launch_attention_block(dt, nullptr, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
-                                                    hq, hkv, hd, c.max_seq, attn, st,
-                                                    s->w.attn_part_bytes ? (float*)(ws + s->w.attn_part) : nullptr,
-                                                    s->w.attn_part_bytes));
+      if (trees)
+        attend_trees(qkv, kc, vc, attn);
+      else
+        PROBE(LS_OP_ATTENTION, launch_attention_block(dt, nullptr, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
+                                                      hq, hkv, hd, c.max_seq, attn, st,
+                                                      s->w.attn_part_bytes ? (float*)(ws + s->w.attn_part) : nullptr,
+                                                      s->w.attn_part_bytes));
       PROBE(LS_OP_GEMM_O, launch_gemm(dt, EPI_RESID, attn, base + sp[2].off, rows, d, hq * hd, nullptr, x, st, &gsc, &f_o));
       PROBE(LS_OP_GEMM_GATEUP, launch_gemm(dt, EPI_SWIGLU, xb2, base + sp[4].off, rows, F, d, hbuf, nullptr, st, &gsc, &f_gu));
       if (more) LS_HIP(gate(s->blocks[s->layer0 + li + 1], st));  // its gain is read next
@@ -708,12 +727,16 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       if (head_folds) {
         SkinnyFusion f_head;
         f_head.ss_in = ss_a; f_head.n_part = d / 16; f_head.eps = c.rms_eps;
-        launch_gemm(dt, EPI_F32, xb, head + head_sp[1].off, batch, c.vocab, d, logits, nullptr, st, &gsc, &f_head);
+        launch_gemm(dt, EPI_F32, xb, head + head_sp[1].off, heads, c.vocab, d, logits, nullptr, st, &gsc, &f_head);
+        launch_argmax(logits, heads, c.vocab, (int32_t*)out, st);
       } else {
-        launch_rmsnorm(dt, x, head + head_sp[0].off, y, batch, d, c.rms_eps, last_rows, st);
-        launch_gemm(dt, EPI_F32, y, head + head_sp[1].off, batch, c.vocab, d, logits, nullptr, st, &gsc);
+        for (int r0 = 0; r0 < heads; r0 += heads_at_once) {
+          const int n = std::min(heads_at_once, heads - r0);
+          launch_rmsnorm(dt, x + (size_t)r0 * d, head + head_sp[0].off, y, n, d, c.rms_eps, trees ? nullptr : last_rows, st);
+          launch_gemm(dt, EPI_F32, y, head + head_sp[1].off, n, c.vocab, d, logits, nullptr, st, &gsc);
+          launch_argmax(logits, n, c.vocab, (int32_t*)out + r0, st);
+        }
       }
-      launch_argmax(logits, batch, c.vocab, (int32_t*)out, st);
     }
     LS_HIP(hipGetLastError());
     return LS_OK;
@@ -896,13 +919,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       PROBE(LS_OP_GEMM_QKV, launch_gemm(dt, EPI_STORE, y, tensor(b, 1), rows, qkv_cols, d, qkv, nullptr, st, &gsc));
     }
     if (trees) {
-      TreeAttn a = *trees;
-      a.qkv = qkv; a.cs = cs; a.kc = kc; a.vc = vc; a.out = attn;
-      // the GEMMs' partial tiles are added up by now, their room is the larger one mostly
-      const bool tiles = s->w.splitk_bytes > s->w.attn_part_bytes;
-      a.scratch = (float*)(ws + (tiles ? s->w.splitk : s->w.attn_part));
-      a.scratch_bytes = tiles ? s->w.splitk_bytes : s->w.attn_part_bytes;
-      launch_tree_attn(dt, a, st);
+      attend_trees(qkv, kc, vc, attn);
     } else {
       PROBE(LS_OP_ATTENTION, launch_attention_block(dt, cu_dev, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
                                                     hq, hkv, hd, c.max_seq, attn, st,
@@ -937,11 +954,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     block_tensors(&c, hb->layer, sp, nullptr);
     const char* base = s->slab + hb->off;
     LS_HIP(gate(*hb, st));  // gate: head block has landed
-    // rows of the head: the sequences' last ones, or all nodes, which without logits_out go max_batch at a time, as many as the
-    // workspace has logits for
-    const int heads = trees ? rows : batch, at_once = logits_out ? heads : std::min(heads, (int)c.max_batch);
-    for (int r0 = 0; r0 < heads; r0 += at_once) {
-      const int n = std::min(at_once, heads - r0);
+    for (int r0 = 0; r0 < heads; r0 += heads_at_once) {
+      const int n = std::min(heads_at_once, heads - r0);
       const int32_t* map = trees ? nullptr : last_rows;
       const float* xr = x + (size_t)r0 * d;
       float* logits = logits_out ? logits_out : (float*)(ws + s->w.logits);

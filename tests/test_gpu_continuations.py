@@ -57,6 +57,49 @@ def test_tree_pass_equals_prompt_passes_over_paths(shape, nodes):
     st.close()
 
 
+ODD = synth.StageShape("bf16", 2, 160, 3, 1, 80, 224, 301)  # heads that only the kernels for every shape take
+
+
+@pytest.mark.parametrize("shape", [BF16, WIDE, ODD], ids=["bf16", "wide", "odd"])
+@pytest.mark.parametrize("lo,hi", [(0, 2), (0, 1), (1, 2)], ids=str)
+@pytest.mark.parametrize("nodes", [[1], [3], [0, 2, 1], [9, 3, 4]], ids=str)
+def test_passes_of_few_rows(shape, lo, hi, nodes):
+    """Stages with or without embedding and head, whose rows are few enough for norms inside the GEMMs: the rows that a stage has
+    to say, with logits and without, and each sequence's chain of the deepest node against generation steps along it."""
+    r = random.Random(sum(nodes))
+    lengths = [9, 30, 14][: len(nodes)]
+    trees = [plain.random_tree(r, n) if n else [] for n in nodes]
+    outs = []
+    for steps in (False, True):
+        st = make_gpu(shape, 3, lo, hi, 3, 60, 60)
+        g = torch.Generator().manual_seed(1)
+        rows = lambda n: (torch.randint(0, shape.vocab, (n,), dtype=torch.int32, generator=g).cuda() if lo == 0  # noqa: E731
+                          else torch.randn(n, shape.hidden, generator=g).bfloat16().cuda())
+        st.prefill(rows(sum(lengths)), lengths)
+        feed = rows(sum(nodes))
+        parents, cu, host = bounds(trees)
+        if not steps:
+            out = st.tree(feed, parents, cu, host, max(lengths), want_logits=hi == 2)
+            if hi == 2:
+                assert torch.equal(out[0], out[1].argmax(1).int())
+                alone = st.tree(feed, parents, cu, host, max(lengths))
+                assert (alone != out[0]).float().mean() <= 0.1 + 1.0 / sum(nodes) * (sum(nodes) > 3)  # see above: other kernels
+                out = out[1]
+            assert torch.equal(st.seq_lens[: len(nodes)].cpu(), torch.tensor(lengths, dtype=torch.int32))
+            outs.append(out.clone())
+        else:
+            paths = [max((plain.path(t, i) for i in range(len(t))), key=len, default=[]) for t in trees]
+            for b, p in enumerate(paths):
+                for j, node in enumerate(p):
+                    st.seq_lens.copy_(torch.tensor([(n + j if i == b else n) for i, n in enumerate(lengths)] + [0] * (3 - len(lengths)), dtype=torch.int32))
+                    at = int(host[b]) + node
+                    got = st.decode(feed[at : at + 1].repeat(*([len(nodes)] + [1] * (feed.dim() - 1))), len(nodes), 40, want_logits=hi == 2)
+                    got = got[1] if hi == 2 else got
+                    check_close(to_host(got[b : b + 1]), to_host(outs[0][at : at + 1]), "bf16", "few rows")
+        torch.cuda.synchronize()
+        st.close()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_middle_stages_and_pipelines_of_them(dtype):
     """Hidden rows in and out; two stages one behind the other, each with its own cache."""
