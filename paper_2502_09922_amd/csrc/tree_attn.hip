@@ -3,7 +3,11 @@
 // Node i of a sequence with c cached positions stands at position c + depth(i) and takes cache slot c + i.  Its query sees the c
 // cached keys and the slots of the nodes on its path from the root, itself included.
 //
-// Here the kernels for every shape (the fast ones: tree_attn_mfma.hip): one rotates and appends the nodes' keys and values, one attends, a wavefront to a (row, query head).
+// Here the kernels for every shape (the fast ones: tree_attn_mfma.hip): one rotates and appends the nodes' keys and values, one
+// attends, a wavefront to a (row, query head), a lane to one or two pairs of dims, eight keys and values on their way at once.
+// Bound by a wavefront's instructions, of which the sums over its lanes are half: 32 heads of 96 dims over 8, four sequences of 600
+// keys, 12 nodes each 115 us in bf16, 106 in fp32 (a key at a time 253 and 335; sixteen at once 116 and 109).  The same of 128 dims
+// takes 20 on the matrix cores.
 #include "tree.hpp"
 
 #include <algorithm>
@@ -46,12 +50,14 @@ k_tree_append(const T* __restrict__ qkv, const float2* __restrict__ cs, const in
   }
 }
 
-template <class T>
+// MAXP: pairs of a lane
+template <class T, int MAXP>
 __global__ void __launch_bounds__(64)
 k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int32_t* __restrict__ cu, const int32_t* __restrict__ parents,
             const int32_t* __restrict__ seq_lens, int rows, int most, int hq, int hkv, int hd, int max_seq, const T* __restrict__ kc,
             const T* __restrict__ vc, T* __restrict__ out) {
-  constexpr int MAXP = 2;  // pairs of a lane: head_dim <= 256
+  typedef T T2 __attribute__((ext_vector_type(2), aligned(sizeof(T))));  // a row may start anywhere
+  constexpr int AT_ONCE = 8;  // keys and values on their way
   const int b = blockIdx.x, node = blockIdx.y, h = blockIdx.z, lane = threadIdx.x, half = hd >> 1;
   TreeSeq t;
   const bool room = tree_seq(cu, seq_lens, b, rows, most, max_seq, t);
@@ -83,26 +89,50 @@ k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int3
   const T* kb = kc + ((size_t)b * hkv + kh) * max_seq * hd;
   const T* vb = vc + ((size_t)b * hkv + kh) * max_seq * hd;
   float m = -INFINITY, l = 0.f;
-  for (int key = 0; key < t.ctx + t.n; ++key) {
-    if (key >= t.ctx && !(path >> (key - t.ctx) & 1)) continue;
-    const T* kr = kb + (size_t)key * hd;
-    const T* vr = vb + (size_t)key * hd;
-    float s = 0.f;
+  for (int key0 = 0; key0 < t.ctx + t.n; key0 += AT_ONCE) {
+    T2 kr[AT_ONCE][MAXP], vr[AT_ONCE][MAXP];
+    bool seen[AT_ONCE];
+    float s[AT_ONCE], mn = m;
 #pragma unroll
-    for (int i = 0; i < MAXP; ++i) {
-      const int p = lane + 64 * i;
-      if (p < half) s = fmaf(q0[i], to_f(kr[2 * p]), fmaf(q1[i], to_f(kr[2 * p + 1]), s));
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int key = min(key0 + j, t.ctx + t.n - 1);
+      seen[j] = key0 + j < t.ctx || (key0 + j < t.ctx + t.n && (path >> (key - t.ctx) & 1));
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i) {
+        const int p = min(lane + 64 * i, half - 1);
+        const size_t at = (size_t)key * hd + 2 * p;
+        kr[j][i] = *reinterpret_cast<const T2*>(kb + at);
+        vr[j][i] = *reinterpret_cast<const T2*>(vb + at);
+      }
     }
-    s = wave_sum(s);
-    const float mn = fmaxf(m, s);
-    const float corr = mn == -INFINITY ? 1.f : __expf(m - mn), w = s == -INFINITY ? 0.f : __expf(s - mn);
-    l = fmaf(l, corr, w);
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      s[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i)
+        if (lane + 64 * i < half) s[j] = fmaf(q0[i], to_f(kr[j][i][0]), fmaf(q1[i], to_f(kr[j][i][1]), s[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) s[j] = wave_sum(s[j]);
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (seen[j]) mn = fmaxf(mn, s[j]);
+    const float corr = mn == -INFINITY ? 1.f : __expf(m - mn);
+    l *= corr;
 #pragma unroll
     for (int i = 0; i < MAXP; ++i) {
-      const int p = lane + 64 * i;
-      if (p < half) {
-        a0[i] = fmaf(w, to_f(vr[2 * p]), a0[i] * corr);
-        a1[i] = fmaf(w, to_f(vr[2 * p + 1]), a1[i] * corr);
+      a0[i] *= corr;
+      a1[i] *= corr;
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      if (!seen[j]) continue;
+      const float w = s[j] == -INFINITY ? 0.f : __expf(s[j] - mn);
+      l += w;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i) {
+        a0[i] = fmaf(w, to_f(vr[j][i][0]), a0[i]);
+        a1[i] = fmaf(w, to_f(vr[j][i][1]), a1[i]);
       }
     }
     m = mn;
@@ -121,8 +151,9 @@ template <class T>
 void launch_any(const TreeAttn& a, hipStream_t st) {
   k_tree_append<T><<<dim3(a.batch, a.hkv), 256, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.max_nodes, a.hq, a.hkv, a.hd,
                                                          a.max_seq, (T*)a.kc, (T*)a.vc);
-  k_tree_attn<T><<<dim3(a.batch, a.max_nodes, a.hq), 64, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.max_nodes, a.hq,
-                                                                  a.hkv, a.hd, a.max_seq, (const T*)a.kc, (const T*)a.vc, (T*)a.out);
+  auto attn = a.hd <= 128 ? k_tree_attn<T, 1> : k_tree_attn<T, 2>;
+  attn<<<dim3(a.batch, a.max_nodes, a.hq), 64, 0, st>>>((const T*)a.qkv, (const float2*)a.cs, a.cu, a.parents, a.seq_lens, a.rows, a.max_nodes, a.hq, a.hkv,
+                                                        a.hd, a.max_seq, (const T*)a.kc, (const T*)a.vc, (T*)a.out);
 }
 
 // Chunks of a call.  One workgroup to a (sequence, kv head, block of columns) where they fill the chip; fewer are cut along the keys
