@@ -156,17 +156,18 @@ void launch_any(const TreeAttn& a, hipStream_t st) {
                                                         a.hd, a.max_seq, (const T*)a.kc, (const T*)a.vc, (T*)a.out);
 }
 
-// Chunks of a call.  One workgroup to a (sequence, kv head, block of columns) where they fill the chip; fewer are cut along the keys
-// until each CU has one, in pieces of 128 keys at least.  More than 32 columns, whose wavefronts wait for each other, want two to a CU
-// and, as more rows are joined, 256 keys.  7B, one sequence of 3000 keys, 26 nodes: 18.3 us for 256 workgroups, 20.0 for 512; 8 of 900
-// keys 33.3 and 35.9; 600 keys, 5 nodes in pieces of 128 10.3, of 256 11.4.  70B, 16 ragged sequences of up to 3000 keys, 16 nodes (128
-// columns): 67 us for 256 workgroups, 57 for 512; one of 4000 keys, 8 nodes in pieces of 128 20.2, of 256 15.8.
+// Chunks of a call.  One workgroup to a (sequence, kv head, block of columns) where they fill the chip.  Fewer with up to 32 columns are cut
+// along the keys until each CU has one, in pieces of 128 keys at least: 7B, one sequence of 3000 keys, 26 nodes 18.3 us for 256
+// workgroups, 20.0 for 512; 8 of 900 keys 33.3 and 35.9; 600 keys, 5 nodes in pieces of 128 10.3, of 256 11.4.  With more columns,
+// whose wavefronts wait for each other, until all three places of a CU are taken, but not beyond: 70B, 16 ragged sequences of up to
+// 3000 keys, 16 nodes 53 us for 768 workgroups, 59 for 512, 63 for 1536; 13B, 16 of 1000 keys, 64 nodes (640 workgroups) 89, cut in
+// two 110.  As more rows are joined their pieces have 256 keys: 70B, 4000 keys, 8 nodes 16.8, in pieces of 128 20.2.
 TreeChunks chunks_for(const TreeAttn& a) {
   TreeChunks p;
-  const int cols = a.max_nodes * (a.hq / a.hkv), wide = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : 128;
+  const int cols = a.max_nodes * (a.hq / a.hkv), wide = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;
   const long base = (long)a.batch * a.hkv * ((cols + wide - 1) / wide);
-  const long target = cols <= 32 ? 256 : 512, least = cols <= 32 ? 128 : 256;
-  const long want = std::min((target + base - 1) / base, (a.max_keys + least - 1) / least);
+  const long target = cols <= 32 ? 256 : 768, least = cols <= 32 ? 128 : 256;
+  const long want = std::min(cols <= 32 ? (target + base - 1) / base : std::max(target / base, 1l), (a.max_keys + least - 1) / least);
   p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
   p.n = (a.max_keys + p.keys - 1) / p.keys;
   return p;

@@ -21,6 +21,12 @@
 // The nodes' own rows are turned, rounded and written to their slots by whoever reads those, a wavefront (CW = 1) or a workgroup,
 // before it reads them: blocks of columns write the same bytes, and none depends on another workgroup's.  Only in the tiles of
 // those slots columns see different keys.
+//
+// Bound by memory where columns are few: 13B, 32 sequences of 1024 to 1087 keys, 16 nodes (723 MB of cache) 131 us, 5.5 TB/s.  With
+// many columns a tile's chain of reads, products, softmax and products is waited for, with two or three wavefronts on a SIMD: 70B, 64
+// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 89 us, the matrix cores busy for a quarter of it, the vector
+// units for a third, LDS for an eighth, no bank conflicts.  One sequence waits for its preamble (bounds, parents, table, queries:
+// 5 us) and the second launch (3 us): 7B, 3000 keys, 26 nodes 18.5 us of which 7 are the cache's reading.
 #include "tree.hpp"
 
 #include <algorithm>
@@ -89,12 +95,16 @@ constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns
 constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds in registers
 constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
 constexpr float FOLLOW = 8.f;
-constexpr int RESIDENT = 512;      // workgroups on the chip at once
+constexpr int CUS = 256;
+// CW = 4 lives with two tiles and 168 registers, so that three workgroups fit a CU: 13B, 16 trees of 64 nodes over 1000 keys 89 us, with
+// two (four tiles, 170 registers) 96; fp32, 4 such trees 71 and 82.  CW = 2 in 168 registers gains nothing (148 and 151 us for 13B, 32
+// x 26 nodes): its tiles leave room for two.
+template <int CW> constexpr int PER_CU = CW == 4 ? 3 : 2;  // workgroups on a CU, wavefronts on a SIMD
 template <class T> constexpr int TILE_KEYS = sizeof(T) == 2 ? 32 : 16;  // 16 KB of keys and values of 128 dims
 
-// NB: tiles of the ring, a power of two (CW > 1).
-template <class T, int HD, int CT, int CW, int KW, int NB>
-__global__ void __launch_bounds__(64 * CW * KW, 2)
+// NB: tiles of the ring, a power of two (CW > 1).  Four instead of two, where LDS had room, changed nothing but what fits a CU.
+template <class T, int HD, int CW, int KW, int NB>
+__global__ void __launch_bounds__(64 * CW * KW, PER_CU<CW>)
 k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const int32_t* __restrict__ parents, const T* __restrict__ qkv,
             const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, T* __restrict__ out, int rows, int most, int hq, int hkv, int max_seq,
             int nchunk, int chunk_tiles, int half, float* __restrict__ part_o, float2* __restrict__ part_ml) {
@@ -105,7 +115,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   constexpr int RPI = 64 / CPR;          // rows that a wavefront's load covers
   constexpr int NL = TK / RPI / CW;      // loads of a wavefront for a tile's keys, as many for its values
   constexpr int TILE = TK * ROWB;
-  constexpr int COLS = 16 * CT * CW;     // of a workgroup
+  constexpr int COLS = 16 * CW;  // of a workgroup
   constexpr int DT = HD / 16;
   typedef T T4 __attribute__((ext_vector_type(4)));
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -211,31 +221,25 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     while (next < min(t_end, t_begin + NB - 1) && (next + 1) * TK <= t.ctx) fill(next++);
   }
 
-  // this wavefront's columns: 16-column tiles share, share + CW, .. of the workgroup's, so that few columns are spread over all
+  // this wavefront's 16 columns
   constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a row
-  const int G16 = t.n * G - cb * COLS - share * 16;
-  const int tiles_here = CT == 1 ? G16 > 0 : (G16 > 0) + (G16 > 16 * CW);
-  u32x4 raw[CT][KS];
-  int node[CT];
+  const int col = cb * COLS + share * 16 + lr;
+  const bool busy = cb * COLS + share * 16 < t.n * G, in = col < t.n * G;
+  const int node = in ? col / G : 0;
+  const T* q = rows0 + (size_t)node * stride + (size_t)(kh * G + (in ? col % G : 0)) * HD;
+  u32x4 raw[KS];
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    const int col = cb * COLS + (share + CW * c) * 16 + lr;
-    const bool in = col < t.n * G;
-    node[c] = in ? col / G : 0;
-    const T* q = rows0 + (size_t)node[c] * stride + (size_t)(kh * G + (in ? col % G : 0)) * HD;
-#pragma unroll
-    for (int kk = 0; kk < KS; ++kk) raw[c][kk] = *reinterpret_cast<const u32x4*>(q + (kk * 4 + lg) * EPC);
-  }
+  for (int kk = 0; kk < KS; ++kk) raw[kk] = *reinterpret_cast<const u32x4*>(q + (kk * 4 + lg) * EPC);
   const uint64_t path = tree_path(parents, t);
   {  // the nodes' rows among the keys of this wavefront (CW = 1) or workgroup
     const int depth = __builtin_popcountll(path) - 1;
     const int n_lo = max((CW == 1 ? t_begin : t_lo) * TK, t.ctx), items = (min((CW == 1 ? t_end : t_hi) * TK, keys) - n_lo) * CPR;
     constexpr int STEP = CW == 1 ? 64 : THREADS;
     for (int i0 = 0; i0 < items; i0 += STEP) {
-      const int i = i0 + (CW == 1 ? lane : (int)threadIdx.x), key = n_lo + i / CPR, ch = i % CPR, node = min(key - t.ctx, t.n - 1);
-      const int d = __shfl(depth, node);
+      const int i = i0 + (CW == 1 ? lane : (int)threadIdx.x), key = n_lo + i / CPR, ch = i % CPR, j = min(key - t.ctx, t.n - 1);
+      const int d = __shfl(depth, j);
       if (i < items) {
-        const T* row = rows0 + (size_t)node * stride + ch * EPC;
+        const T* row = rows0 + (size_t)j * stride + ch * EPC;
         u32x4 k = *reinterpret_cast<const u32x4*>(row + (size_t)(hq + kh) * HD);
         const u32x4 v = *reinterpret_cast<const u32x4*>(row + (size_t)(hq + hkv + kh) * HD);
         if (cs) k = turned(k, cs + (size_t)(t.ctx + d) * HD + ch * EPC, T{});
@@ -251,69 +255,59 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 
   // ---- queries, bf16 as two parts, and the nodes they see
   typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Q;
-  Q qh[CT][KS], ql[CT][sizeof(T) == 2 ? KS : 1];
-  uint64_t sees[CT];
+  Q qh[KS], ql[sizeof(T) == 2 ? KS : 1];
+  const uint64_t sees = (uint64_t)(unsigned)__shfl((int)(unsigned)(path >> 32), node) << 32 | (unsigned)__shfl((int)(unsigned)path, node);
+  const float* turn = cs + (size_t)(t.ctx + __builtin_popcountll(sees) - 1) * HD;
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    sees[c] = (uint64_t)(unsigned)__shfl((int)(unsigned)(path >> 32), node[c]) << 32 | (unsigned)__shfl((int)(unsigned)path, node[c]);
-    const float* turn = cs + (size_t)(t.ctx + __builtin_popcountll(sees[c]) - 1) * HD;
+  for (int kk = 0; kk < KS; ++kk) {
+    const int d0 = (kk * 4 + lg) * EPC;
+    if constexpr (sizeof(T) == 4) {
+      qh[kk] = __builtin_bit_cast(f32x4, cs ? turned(raw[kk], turn + d0, T{}) : raw[kk]);
+    } else {
+      const bf16x8 u = __builtin_bit_cast(bf16x8, raw[kk]);
+      f32x4 ta{}, tb{};
+      if (cs) {
+        ta = reinterpret_cast<const f32x4*>(turn + d0)[0];
+        tb = reinterpret_cast<const f32x4*>(turn + d0)[1];
+      }
 #pragma unroll
-    for (int kk = 0; kk < KS; ++kk) {
-      const int d0 = (kk * 4 + lg) * EPC;
-      if constexpr (sizeof(T) == 4) {
-        qh[c][kk] = __builtin_bit_cast(f32x4, cs ? turned(raw[c][kk], turn + d0, T{}) : raw[c][kk]);
-      } else {
-        const bf16x8 u = __builtin_bit_cast(bf16x8, raw[c][kk]);
-        f32x4 ta{}, tb{};
+      for (int p = 0; p < 4; ++p) {
+        float u0 = (float)u[2 * p], u1 = (float)u[2 * p + 1];
         if (cs) {
-          ta = reinterpret_cast<const f32x4*>(turn + d0)[0];
-          tb = reinterpret_cast<const f32x4*>(turn + d0)[1];
+          const float2 c2 = p < 2 ? float2{ta[2 * p], ta[2 * p + 1]} : float2{tb[2 * p - 4], tb[2 * p - 3]};
+          const float w0 = turn0(u0, u1, c2), w1 = turn1(u0, u1, c2);
+          u0 = w0;
+          u1 = w1;
         }
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          float u0 = (float)u[2 * p], u1 = (float)u[2 * p + 1];
-          if (cs) {
-            const float2 c2 = p < 2 ? float2{ta[2 * p], ta[2 * p + 1]} : float2{tb[2 * p - 4], tb[2 * p - 3]};
-            const float w0 = turn0(u0, u1, c2), w1 = turn1(u0, u1, c2);
-            u0 = w0;
-            u1 = w1;
-          }
-          qh[c][kk][2 * p] = (bf16)u0;
-          qh[c][kk][2 * p + 1] = (bf16)u1;
-          ql[c][kk][2 * p] = (bf16)(u0 - (float)qh[c][kk][2 * p]);
-          ql[c][kk][2 * p + 1] = (bf16)(u1 - (float)qh[c][kk][2 * p + 1]);
-        }
+        qh[kk][2 * p] = (bf16)u0;
+        qh[kk][2 * p + 1] = (bf16)u1;
+        ql[kk][2 * p] = (bf16)(u0 - (float)qh[kk][2 * p]);
+        ql[kk][2 * p + 1] = (bf16)(u1 - (float)qh[kk][2 * p + 1]);
       }
     }
   }
 
-  f32x4 o[CT][DT];
-  float m_run[CT];
-  f32x4 l_run[CT];  // all rows of a product alike
+  f32x4 o[DT];
+  float m_run = -INFINITY;
+  f32x4 l_run{0.f, 0.f, 0.f, 0.f};  // all rows of a product alike
   bf16x8 ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.f;
 #pragma unroll
-  for (int c = 0; c < CT; ++c) {
-    m_run[c] = -INFINITY;
-    l_run[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[c][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float scale = 1.4426950408889634f / sqrtf((float)HD);  // score -> exponent of 2
   // four neighbouring dims that a lane holds of a column: i of DT such, from dim_of(i) on
   auto dim_of = [&](int i) { return sizeof(T) == 2 ? i * 16 + 4 * lg : (i >> 2) * 64 + 16 * lg + 4 * (i & 3); };
-  auto out_at = [&](int c, int i, int e) -> float& {
-    float* at = reinterpret_cast<float*>(&o[c][0]);
+  auto out_at = [&](int i, int e) -> float& {
+    float* at = reinterpret_cast<float*>(&o[0]);
     return sizeof(T) == 2 ? at[i * 4 + e] : at[((i & ~3) + e) * 4 + (i & 3)];
   };
-  auto piece = [&](int c, int i) { return f32x4{out_at(c, i, 0), out_at(c, i, 1), out_at(c, i, 2), out_at(c, i, 3)}; };
+  auto piece = [&](int i) { return f32x4{out_at(i, 0), out_at(i, 1), out_at(i, 2), out_at(i, 3)}; };
 
   // ---- a tile in LDS
   constexpr int HALVES = TK / 16;
-  auto attend = [&](auto tiles_, const unsigned char* ks, const unsigned char* vs, int key0, bool odd) {
-    constexpr int NC = decltype(tiles_)::value;
-    f32x4 s[NC][HALVES];
+  auto attend = [&](const unsigned char* ks, const unsigned char* vs, int key0, bool odd) {
+    f32x4 s[HALVES];
     // all of a tile's keys are asked for at once, and all of its values before the softmax: with a few reads at a time each of them
     // was waited for
     Q kf[HALVES][KS];
@@ -322,8 +316,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       const int kl = h * 16 + lr;
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) kf[h][kk] = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
-#pragma unroll
-      for (int c = 0; c < NC; ++c) s[c][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+      s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -332,14 +325,10 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
-          for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) s[c][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], part ? qh[c][kk] : ql[c][kk], s[c][h], 0, 0, 0);
+          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], part ? qh[kk] : ql[kk], s[h], 0, 0, 0);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int c = 0; c < NC; ++c) s[c][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[0][kk][e], qh[c][kk][e], s[c][0], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[0][kk][e], qh[kk][e], s[0], 0, 0, 0);
       }
     }
     Q vt[DT];  // bf16: 16 dims each; fp32: a read of four, of which there are as many
@@ -361,82 +350,63 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     }
     __builtin_amdgcn_sched_barrier(0);
     const int behind = key0 - t.ctx;  // of the cached positions
+    if (behind > -TK) {               // slots of nodes
+      const unsigned seen = behind >= 64 ? 0u : behind >= 0 ? (unsigned)(sees >> behind) : (unsigned)(sees << -behind) | ((1u << -behind) - 1u);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      if (behind > -TK) {  // slots of nodes
-        const unsigned seen = behind >= 64 ? 0u : behind >= 0 ? (unsigned)(sees[c] >> behind) : (unsigned)(sees[c] << -behind) | ((1u << -behind) - 1u);
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[c][h][e] = seen >> (h * 16 + 4 * lg + e) & 1u ? s[c][h][e] : -INFINITY;
-      }
-      // a NaN score makes its weight NaN, and the sums with it, whatever the maximum is
-      float mx = s[c][0][0];
-#pragma unroll
-      for (int i = 1; i < 4 * HALVES; ++i) mx = __builtin_elementwise_maximum(mx, s[c][i >> 2][i & 3]);
-      mx = exchange<16, 32>(mx, Max{});
-      // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: bf16 and fp32 weights above
-      // one are as exact as below.  Following every move, and adding up the sums here, took 70B, 64 ragged
-      // trees 97 us instead of 92.
-      const float m_new = fmaxf(m_run[c], mx);
-      const bool moved = (m_new - m_run[c]) * scale > FOLLOW;  // false for (-inf, -inf)
-      if (__builtin_amdgcn_ballot_w64(moved) != 0) {           // the others keep their bits
-        const float corr = moved ? __builtin_amdgcn_exp2f((m_run[c] - m_new) * scale) : 1.f;
-        l_run[c] *= corr;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) o[c][d] *= corr;
-        m_run[c] = moved ? m_new : m_run[c];
-      }
-      const float mc = m_run[c] == -INFINITY ? 0.f : m_run[c] * scale;
-#pragma unroll
-      for (int i = 0; i < 4 * HALVES; ++i) s[c][i >> 2][i & 3] = __builtin_amdgcn_exp2f(fmaf(s[c][i >> 2][i & 3], scale, -mc));
+      for (int i = 0; i < 4 * HALVES; ++i) s[i >> 2][i & 3] = seen >> ((i >> 2) * 16 + 4 * lg + (i & 3)) & 1u ? s[i >> 2][i & 3] : -INFINITY;
     }
+    // a NaN score makes its weight NaN, and the sums with it, whatever the maximum is
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 4 * HALVES; ++i) mx = __builtin_elementwise_maximum(mx, s[i >> 2][i & 3]);
+    mx = exchange<16, 32>(mx, Max{});
+    // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: bf16 and fp32 weights above one
+    // are as exact as below.  Following every move, and adding up the sums here, took 70B, 64 ragged trees 5 % longer.
+    const float m_new = fmaxf(m_run, mx);
+    const bool moved = (m_new - m_run) * scale > FOLLOW;  // false for (-inf, -inf)
+    if (__builtin_amdgcn_ballot_w64(moved) != 0) {        // the others keep their bits
+      const float corr = moved ? __builtin_amdgcn_exp2f((m_run - m_new) * scale) : 1.f;
+      l_run *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
+      m_run = moved ? m_new : m_run;
+    }
+    const float mc = m_run == -INFINITY ? 0.f : m_run * scale;
+#pragma unroll
+    for (int i = 0; i < 4 * HALVES; ++i) s[i >> 2][i & 3] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale, -mc));
     if constexpr (sizeof(T) == 2) {
-      bf16x8 pf[NC];
+      bf16x8 pf;
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pf[c][i] = (bf16)s[c][i >> 2][i & 3];
+      for (int i = 0; i < 8; ++i) pf[i] = (bf16)s[i >> 2][i & 3];
       // their sum is of the rounded ones, another row of the product: a single large weight then divides out
+      l_run = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf, l_run, 0, 0, 0);
 #pragma unroll
-      for (int c = 0; c < NC; ++c) l_run[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[c], l_run[c], 0, 0, 0);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) o[c][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf[c], o[c][d], 0, 0, 0);
+      for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf, o[d], 0, 0, 0);
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) l_run[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, s[c][0][e], l_run[c], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) l_run = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, s[0][e], l_run, 0, 0, 0);
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int d = 0; d < 4; ++d) o[c][j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[j * 4 + e][d], s[c][0][e], o[c][j * 4 + d], 0, 0, 0);
+          for (int d = 0; d < 4; ++d) o[j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vt[j * 4 + e][d], s[0][e], o[j * 4 + d], 0, 0, 0);
     }
     if (odd) {  // nodes' values that are no numbers lie in the tile as zeros: only the columns that see the nodes take them
       for (int j = max(0, -behind); j < TK && behind + j < t.n; ++j) {
         const T* v = rows0 + (size_t)(behind + j) * stride + (size_t)(hq + hkv + kh) * HD;
-        const int from = ((j >> 2) & 3) * 16 + lr;
+        float p = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          float p = 0.f;
+        for (int i = 0; i < 4 * HALVES; ++i) p = (j >> 4) * 4 + (j & 3) == i ? s[i >> 2][i & 3] : p;
+        p = __shfl(p, ((j >> 2) & 3) * 16 + lr);
+        if (!(sees >> (behind + j) & 1)) continue;
 #pragma unroll
-          for (int i = 0; i < 4 * HALVES; ++i) p = (j >> 4) * 4 + (j & 3) == i ? s[c][i >> 2][i & 3] : p;
-          p = __shfl(p, from);
-          if (!(sees[c] >> (behind + j) & 1)) continue;
+        for (int i = 0; i < DT; ++i) {
+          const T4 x = *reinterpret_cast<const T4*>(v + dim_of(i));
 #pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            const T4 x = *reinterpret_cast<const T4*>(v + dim_of(i));
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!(fabsf(to_f(x[e])) < INFINITY)) out_at(c, i, e) += p * to_f(x[e]);
-            __builtin_amdgcn_sched_barrier(0);  // rare: no registers for it
-          }
+          for (int e = 0; e < 4; ++e)
+            if (!(fabsf(to_f(x[e])) < INFINITY)) out_at(i, e) += p * to_f(x[e]);
+          __builtin_amdgcn_sched_barrier(0);  // rare: no registers for it
         }
       }
     }
@@ -466,72 +436,62 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   unsigned char* tiles = smem + split * ((CW == 1 ? 1 : NB) * 2 * TILE);
   if constexpr (CW > 1)
     while (next < min(t_end, t_begin + NB - 1)) fill(next++);
-  // a wavefront's loop for as many 16-column tiles as it has: of 128 columns two, of less one or none, so that small trees among large
-  // ones cost what they are (loops of their own, as one with both forms inside kept 54 registers in memory)
-  auto walk = [&](auto n_) {
-    if constexpr (CW == 1) {
-      for (int i = t_begin - 1; i < t_end; ++i) {  // tile i is attended to while i + 1 is on its way
-        bool odd = false;
-        if (i >= t_begin) odd = put(tiles, tiles + TILE, i);
-        if (i + 1 < t_end && (i >= t_begin || !early)) load(i + 1);
-        if (i >= t_begin) attend(n_, tiles, tiles + TILE, i * TK, odd);
-      }
-    } else {
-      for (int i = t_begin; i < t_begin + per; ++i) {  // as many turns for all
-        unsigned char* ks = tiles + ((i - t_begin) & (NB - 1)) * (2 * TILE);
-        int* flags = odd_flags[(i - t_begin) & (NB - 1)];
-        const bool last = (i + 1) * TK > t.ctx;  // slots of nodes
-        if (i < t_end) {
-          // this wavefront's fills of tile i have landed: those behind it are 2 NL for each tile
-          if (next - i == NB - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((NB - 2) * 2 * NL));
-          else wait_vm((next - 1 - i) * 2 * NL);
-          asm volatile("" ::: "memory");
-          if (last) {  // as put() does, in what this wavefront has filled
-            bool odd = false;
+  if constexpr (CW == 1) {
+    for (int i = t_begin - 1; i < t_end; ++i) {  // tile i is attended to while i + 1 is on its way
+      bool odd = false;
+      if (i >= t_begin) odd = put(tiles, tiles + TILE, i);
+      if (i + 1 < t_end && (i >= t_begin || !early)) load(i + 1);
+      if (i >= t_begin) attend(tiles, tiles + TILE, i * TK, odd);
+    }
+  } else {
+    for (int i = t_begin; i < t_begin + per; ++i) {  // as many turns for all
+      unsigned char* ks = tiles + ((i - t_begin) & (NB - 1)) * (2 * TILE);
+      int* flags = odd_flags[(i - t_begin) & (NB - 1)];
+      const bool last = (i + 1) * TK > t.ctx;  // slots of nodes
+      if (i < t_end) {
+        // this wavefront's fills of tile i have landed: those behind it are 2 NL for each tile
+        if (next - i == NB - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((NB - 2) * 2 * NL));
+        else wait_vm((next - 1 - i) * 2 * NL);
+        asm volatile("" ::: "memory");
+        if (last) {  // as put() does, in what this wavefront has filled
+          bool odd = false;
 #pragma unroll
-            for (int j = 0; j < NL; ++j) {
-              const int r = first_row + j * RPI;
-              u32x4* at = reinterpret_cast<u32x4*>(ks + TILE + r * ROWB + lane * 16);
-              u32x4 v = *at;
-              if (i * TK + r + lrow >= t.ctx && drop_nonfinite<T>(v)) {
-                odd = true;
-                *at = v;
-              }
+          for (int j = 0; j < NL; ++j) {
+            const int r = first_row + j * RPI;
+            u32x4* at = reinterpret_cast<u32x4*>(ks + TILE + r * ROWB + lane * 16);
+            u32x4 v = *at;
+            if (i * TK + r + lrow >= t.ctx && drop_nonfinite<T>(v)) {
+              odd = true;
+              *at = v;
             }
-            if (lane == 0) flags[wave] = 0;
-            if (__builtin_amdgcn_ballot_w64(odd) != 0 && lane == 0) flags[wave] = 1;
           }
+          if (lane == 0) flags[wave] = 0;
+          if (__builtin_amdgcn_ballot_w64(odd) != 0 && lane == 0) flags[wave] = 1;
         }
-        slot_barrier<true>();
-        if (next < t_end) fill(next++);  // over tile i - 1, which all have left
-        if (i < t_end && tiles_here) {
-          int odd = 0;
-          if (last)
+      }
+      slot_barrier<true>();
+      if (next < t_end) fill(next++);  // over tile i - 1, which all have left
+      if (i < t_end && busy) {
+        int odd = 0;
+        if (last)
 #pragma unroll
-            for (int w = 0; w < CW; ++w) odd |= flags[split * CW + w];
-          attend(n_, ks, ks + TILE, i * TK, odd != 0);
-        }
+          for (int w = 0; w < CW; ++w) odd |= flags[split * CW + w];
+        attend(ks, ks + TILE, i * TK, odd != 0);
       }
     }
-  };
-  if (CT == 1 || tiles_here == CT) walk(std::integral_constant<int, CT>{});
-  else walk(std::integral_constant<int, 1>{});
+  }
 
   if constexpr (KW > 1) {  // ---- the splits' results, in their order
     __shared__ float sm_m[KW][COLS], sm_l[KW][COLS];
     __syncthreads();  // nobody reads tiles any more
     float* sm_o = reinterpret_cast<float*>(smem);
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const float l = l_run[c][0];
-      const int at = (share + CW * c) * 16 + lr;
-      if (lg == 0) {
-        sm_m[split][at] = m_run[c];
-        sm_l[split][at] = l;
-      }
-#pragma unroll
-      for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(sm_o + (split * COLS + at) * (HD + SM_PAD) + dim_of(i)) = piece(c, i);
+    const int at = share * 16 + lr;
+    if (lg == 0) {
+      sm_m[split][at] = m_run;
+      sm_l[split][at] = l_run[0];
     }
+#pragma unroll
+    for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(sm_o + (split * COLS + at) * (HD + SM_PAD) + dim_of(i)) = piece(i);
     __syncthreads();
     for (int i = threadIdx.x; i < COLS * (HD / 4); i += THREADS) {
       const int c = i / (HD / 4), d = i % (HD / 4) * 4, col = cb * COLS + c;
@@ -561,27 +521,25 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
       }
     }
   } else {
+    int at = threadIdx.x;  // the column found again: it would hold a register through the loop
+    asm volatile("" : "+v"(at));
+    at = cb * COLS + share * 16 + (at & 15);
+    if (at >= t.n * G) return;
+    const size_t row = row_of(at);
+    if (whole) {
+      const float inv = 1.0f / l_run[0];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      const int col = cb * COLS + (share + CW * c) * 16 + lr;
-      const float l = l_run[c][0];
-      if (col >= t.n * G) continue;
-      const size_t row = row_of(col);
-      if (whole) {
-        const float inv = 1.0f / l;
+      for (int i = 0; i < DT; ++i) {
+        const f32x4 p = piece(i);
+        T4 v;
 #pragma unroll
-        for (int i = 0; i < DT; ++i) {
-          const f32x4 p = piece(c, i);
-          T4 v;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = from_f<T>(p[e] * inv);
-          *reinterpret_cast<T4*>(out + row * HD + dim_of(i)) = v;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(part_o + (pieces + row) * HD + dim_of(i)) = piece(c, i);
-        if (lg == 0) part_ml[pieces + row] = float2{m_run[c], l};
+        for (int e = 0; e < 4; ++e) v[e] = from_f<T>(p[e] * inv);
+        *reinterpret_cast<T4*>(out + row * HD + dim_of(i)) = v;
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(part_o + (pieces + row) * HD + dim_of(i)) = piece(i);
+      if (lg == 0) part_ml[pieces + row] = float2{m_run, l_run[0]};
     }
   }
 }
@@ -644,31 +602,34 @@ k_tree_merge(const float* __restrict__ part_o, const float2* __restrict__ part_m
   *reinterpret_cast<T4*>(out + row * HD + d) = w;
 }
 
-template <class T, int HD, int CT, int CW, int KW, int NB>
+template <class T, int HD, int CW, int KW, int NB>
 void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
-  constexpr int COLS = 16 * CT * CW, TK = TILE_KEYS<T>;
+  constexpr int COLS = 16 * CW, TK = TILE_KEYS<T>;
   constexpr int TILES = KW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = KW > 1 ? KW * COLS * (HD + SM_PAD) * 4 : 0;
   constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
   static std::atomic<uint64_t> lds_allowed{0};
-  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CT, CW, KW, NB>, SMEM, lds_allowed);
+  allow_dynamic_lds((const void*)k_tree_mfma<T, HD, CW, KW, NB>, SMEM, lds_allowed);
   const int blocks = (a.max_nodes * (a.hq / a.hkv) + COLS - 1) / COLS;
   const long each = (long)a.hkv * blocks;  // workgroups of a sequence
   int half = 0;
-  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = each * a.batch <= RESIDENT / (CW * KW / 4) ? std::max(1, (int)(RESIDENT / 2 / each)) : a.batch;
-  k_tree_mfma<T, HD, CT, CW, KW, NB><<<dim3(p.n, a.hkv * blocks, a.batch), 64 * CW * KW, SMEM, st>>>(
+  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = each * a.batch <= PER_CU<CW> * CUS ? std::max(1, (int)(CUS / each)) : a.batch;
+  k_tree_mfma<T, HD, CW, KW, NB><<<dim3(p.n, a.hkv * blocks, a.batch), 64 * CW * KW, SMEM, st>>>(
       a.cu, a.seq_lens, a.parents, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, (T*)a.out, a.rows, a.max_nodes, a.hq, a.hkv, a.max_seq, p.n, p.keys / TK, half, p.o, p.ml);
   if (p.n > 1)
     k_tree_merge<T, HD><<<dim3(a.rows, (a.hq + 1024 / HD - 1) / (1024 / HD)), 256, 0, st>>>(p.o, p.ml, a.cu, a.seq_lens, a.rows, a.max_nodes, a.hq, a.batch, a.max_seq,
                                                                                        p.n, p.keys, (T*)a.out);
 }
 
+// Wavefronts share keys where columns are too many for one, as few as do.  7B, one sequence of 3000 keys, 26 nodes: 18.5 us with two 16-
+// column tiles in each pair of wavefronts, 23 with both in every wavefront, keys of its own.  Blocks of 64 columns at most, which read the cache
+// again, out of L2: blocks of 128, two tiles to a wavefront and two workgroups to a CU, took 92 us instead of 89 for 70B, 64 ragged
+// trees, 58 instead of 53 for 16 of them, 34 instead of 30 for one of 64 nodes over 4000 keys.
 template <class T, int HD>
 void launch_hd(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
   const int cols = a.max_nodes * (a.hq / a.hkv);
-  if (cols <= 16) launch<T, HD, 1, 1, 4, 1>(a, p, st);
-  else if (cols <= 32) launch<T, HD, 1, 2, 2, 2>(a, p, st);
-  else if (cols <= 64) launch<T, HD, 1, 4, 1, 4>(a, p, st);
-  else launch<T, HD, 2, 4, 1, 4>(a, p, st);
+  if (cols <= 16) launch<T, HD, 1, 4, 1>(a, p, st);
+  else if (cols <= 32) launch<T, HD, 2, 2, 2>(a, p, st);
+  else launch<T, HD, 4, 1, 2>(a, p, st);
 }
 
 }  // namespace
