@@ -11,7 +11,8 @@ namespace {
 
 // One wavefront to a sequence, a lane to a node.  Node i > 0 agrees if its token is what the model said behind its parent; a node
 // is on if all of its path agrees; of the deepest ones on, the lowest index, the path is kept.  What the model said along
-// the path are the tokens that the sequence has gained: those of the accepted drafts and one more.
+// the path are the tokens that the sequence has gained: those of the accepted drafts and one more.  Loads that wait for each other: one tree of
+// 26 nodes 2.0 us, 32 of 16 3.1.
 __global__ void __launch_bounds__(64)
 k_tree_accept(const int32_t* __restrict__ cu, const int32_t* __restrict__ parents, const int32_t* __restrict__ tokens,
               const int32_t* __restrict__ said, int rows, int most, uint64_t* __restrict__ kept, int32_t* __restrict__ count,
@@ -44,7 +45,9 @@ k_tree_accept(const int32_t* __restrict__ cu, const int32_t* __restrict__ parent
 }
 
 // Rows of kept nodes move to the slots behind the context, all layers and heads, keys and values; a thread to a U-sized piece of a
-// row.  The j-th kept node is node j or a later one, so in index order no row is overwritten before it has moved.
+// row.  The j-th kept node is node j or a later one, so in index order no row is overwritten before it has moved.  Eight rows are on their way at once; bound by
+// its start and by two loads that wait for each other: 7B, one sequence, 26 nodes, 8 layers 5.0 us, 13B, 32 of 16 nodes, 4 layers (11
+// MB) 8.4.
 template <class U>
 __global__ void __launch_bounds__(256)
 k_tree_keep(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens, const uint64_t* __restrict__ kept, int rows, int most, int max_batch,
