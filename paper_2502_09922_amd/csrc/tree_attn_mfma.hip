@@ -124,7 +124,12 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   const int kh = blockIdx.y % hkv, cb = blockIdx.y / hkv, z = blockIdx.x;
   int b = blockIdx.z, pos_of_b;
   // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest
-  if (half) b = row_by_length<ORDERED / 64, true>(seq_lens, gridDim.z, b < half ? b : (int)gridDim.z - 1 - (b - half), max_seq, pos_of_b);
+  // (70B, 64 ragged trees take 89 us instead of 110; equal lengths pay for it: 13B, 16 trees of 64 nodes 88.2 and 86.5)
+  if (half) {
+    const int rank = b < half ? b : (int)gridDim.z - 1 - (b - half);
+    b = gridDim.z <= 64 ? row_by_length<1, true>(seq_lens, gridDim.z, rank, max_seq, pos_of_b)
+                        : row_by_length<ORDERED / 64, true>(seq_lens, gridDim.z, rank, max_seq, pos_of_b);
+  }
   b = __builtin_amdgcn_readfirstlane(b);
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -359,12 +364,13 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     float mx = s[0][0];
 #pragma unroll
     for (int i = 1; i < 4 * HALVES; ++i) mx = __builtin_elementwise_maximum(mx, s[i >> 2][i & 3]);
-    mx = exchange<16, 32>(mx, Max{});
     // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: bf16 and fp32 weights above one
     // are as exact as below.  Following every move, and adding up the sums here, took 70B, 64 ragged trees 5 % longer.
-    const float m_new = fmaxf(m_run, mx);
-    const bool moved = (m_new - m_run) * scale > FOLLOW;  // false for (-inf, -inf)
-    if (__builtin_amdgcn_ballot_w64(moved) != 0) {        // the others keep their bits
+    auto far = [&] { return (mx - m_run) * scale > FOLLOW; };  // false for (-inf, -inf)
+    if (__builtin_amdgcn_ballot_w64(far()) != 0) {             // lanes of a column exchange their maxima only then
+      mx = exchange<16, 32>(mx, Max{});
+      const bool moved = far();  // the others keep their bits
+      const float m_new = fmaxf(m_run, mx);
       const float corr = moved ? __builtin_amdgcn_exp2f((m_run - m_new) * scale) : 1.f;
       l_run *= corr;
 #pragma unroll
