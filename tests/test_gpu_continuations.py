@@ -252,3 +252,29 @@ def test_refusals_of_the_tree_pass():
         st.tree(one, one, cu, [0, 1], 3)
     assert e.value.status == b.LS_ERR_NOT_LOADED
     st.close()
+
+
+@pytest.mark.parametrize("shape", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("nodes", [[5, 1], [33, 14]], ids=str)
+def test_a_pass_while_blocks_arrive(shape, nodes):
+    """The first pass of a stage whose blocks are on their way, last ones first, over trees without a context: the bits of a stage that has them."""
+    from helpers import packed_blocks
+
+    r = random.Random(3)
+    trees = [plain.random_tree(r, n) for n in nodes]
+    parents, cu, host = bounds(trees)
+    feed = torch.from_numpy(synth.token_ids(9, sum(nodes), shape.vocab)).cuda()
+    outs = []
+    for streamed in (False, True):
+        n = shape.n_layers_total
+        st = make_gpu(shape, 3, 0, n, 2, 80, 80, load=not streamed)
+        st.seq_lens.zero_()
+        if streamed:
+            torch.cuda.synchronize()
+            copy, blocks = torch.cuda.Stream(), [(i, st.stage_host_block(i, buf)) for i, buf in packed_blocks(st, 3).items()]
+            for i, buf in reversed(blocks):
+                st.load_block(i, buf, stream=copy)
+        outs.append([t.clone() for t in st.tree(feed, parents, cu, host, 0, want_logits=True)])
+        torch.cuda.synchronize()
+        st.close()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])

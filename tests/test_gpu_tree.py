@@ -413,3 +413,14 @@ def test_replayed_with_other_trees(heads, now):
     full = torch.zeros(max(rows, int(c["cu"][-1])), got.shape[1], dtype=got.dtype)
     full[:rows] = got
     check(alone, (full, k, v))
+
+
+def test_bounds_that_may_not_be_written():
+    from paper_2502_09922_amd import tree_accept
+
+    cu = np.array([0, 2, 3], np.int32)
+    cu.flags.writeable = False
+    t = torch.tensor([5, 7, 5], dtype=torch.int32).cuda()
+    for host in (cu, [0, 2, 3], torch.tensor([0, 2, 3]).numpy(), np.array([0, 9, 2, 9, 3], np.int32)[::2]):
+        kept, count, emitted, following = tree_accept(t, t, torch.tensor([-1, 0, -1], dtype=torch.int32).cuda(), torch.tensor([0, 2, 3], dtype=torch.int32).cuda(), host)
+        assert kept.tolist() == [1, 1] and count.tolist() == [1, 1] and emitted[:, 0].tolist() == [5, 5] and following.tolist() == [5, 5]
