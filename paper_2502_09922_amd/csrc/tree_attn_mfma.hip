@@ -24,7 +24,7 @@
 //
 // Bound by memory where columns are few: 13B, 32 sequences of 1024 to 1087 keys, 16 nodes (723 MB of cache) 131 us, 5.5 TB/s.  With
 // many columns a tile's chain of reads, products, softmax and products is waited for, with two or three wavefronts on a SIMD: 70B, 64
-// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 89 us, the matrix cores busy for a quarter of it, the vector
+// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 88 us, the matrix cores busy for a quarter of it, the vector
 // units for a third, LDS for an eighth, no bank conflicts.  One sequence waits for its preamble (bounds, parents, table, queries:
 // 5 us) and the second launch (3 us): 7B, 3000 keys, 26 nodes 18.5 us of which 7 are the cache's reading.
 #include "tree.hpp"
@@ -97,7 +97,7 @@ constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may b
 constexpr float FOLLOW = 8.f;
 constexpr int CUS = 256;
 // CW = 4 lives with two tiles and 168 registers, so that three workgroups fit a CU: 13B, 16 trees of 64 nodes over 1000 keys 89 us, with
-// two (four tiles, 170 registers) 96; fp32, 4 such trees 71 and 82.  CW = 2 in 168 registers gains nothing (148 and 151 us for 13B, 32
+// two (four tiles, 170 registers) 96; fp32, 4 such trees 69 and 82.  CW = 2 in 168 registers gains nothing (148 and 151 us for 13B, 32
 // x 26 nodes): its tiles leave room for two.
 template <int CW> constexpr int PER_CU = CW == 4 ? 3 : 2;  // workgroups on a CU, wavefronts on a SIMD
 template <class T> constexpr int TILE_KEYS = sizeof(T) == 2 ? 32 : 16;  // 16 KB of keys and values of 128 dims
@@ -124,7 +124,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
   const int kh = blockIdx.y % hkv, cb = blockIdx.y / hkv, z = blockIdx.x;
   int b = blockIdx.z, pos_of_b;
   // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest
-  // (70B, 64 ragged trees take 89 us instead of 110; equal lengths pay for it: 13B, 16 trees of 64 nodes 88.2 and 86.5)
+  // (70B, 64 ragged trees take 88 us instead of 110; equal lengths pay for it: 13B, 16 trees of 64 nodes 88.2 and 86.5)
   if (half) {
     const int rank = b < half ? b : (int)gridDim.z - 1 - (b - half);
     b = gridDim.z <= 64 ? row_by_length<1, true>(seq_lens, gridDim.z, rank, max_seq, pos_of_b)
@@ -294,7 +294,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 
   f32x4 o[DT];
   float m_run = -INFINITY;
-  f32x4 l_run{0.f, 0.f, 0.f, 0.f};  // all rows of a product alike
+  f32x4 l_run{0.f, 0.f, 0.f, 0.f};  // bf16: all rows of a product alike; fp32: the first, a lane's sum
   bf16x8 ones;
 #pragma unroll
   for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.f;
@@ -389,8 +389,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf, o[d], 0, 0, 0);
     } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) l_run = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, s[0][e], l_run, 0, 0, 0);
+      l_run[0] += (s[0][0] + s[0][1]) + (s[0][2] + s[0][3]);  // of this lane's keys; four products less of 68
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
@@ -487,6 +486,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     }
   }
 
+  if constexpr (sizeof(T) == 4) l_run[0] = exchange<16, 32>(l_run[0], Add{});
   if constexpr (KW > 1) {  // ---- the splits' results, in their order
     __shared__ float sm_m[KW][COLS], sm_l[KW][COLS];
     __syncthreads();  // nobody reads tiles any more
@@ -628,7 +628,7 @@ void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
 
 // Wavefronts share keys where columns are too many for one, as few as do.  7B, one sequence of 3000 keys, 26 nodes: 18.5 us with two 16-
 // column tiles in each pair of wavefronts, 23 with both in every wavefront, keys of its own.  Blocks of 64 columns at most, which read the cache
-// again, out of L2: blocks of 128, two tiles to a wavefront and two workgroups to a CU, took 92 us instead of 89 for 70B, 64 ragged
+// again, out of L2: blocks of 128, two tiles to a wavefront and two workgroups to a CU, took 92 us instead of 88 for 70B, 64 ragged
 // trees, 58 instead of 53 for 16 of them, 34 instead of 30 for one of 64 nodes over 4000 keys.
 template <class T, int HD>
 void launch_hd(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
