@@ -318,8 +318,8 @@ size_t ls_tree_attention_scratch_bytes(const ls_heads* heads, const ls_tree* tre
  *             (the table that a stage's workspace starts with), or NULL: rows come turned
  *   layer     one layer's cache, k and v [max_batch][n_kv_heads][max_seq][head_dim], and seq_lens
  *   out       [nodes, n_q_heads * head_dim]
- *   max_ctx   host-side upper bound of seq_lens[b]; max_ctx + the smallest tree beyond max_seq is LS_ERR_KV_OVERFLOW.  An
- *             understated bound costs speed, never keys.
+ *   max_ctx   host-side upper bound of seq_lens[b] of the sequences that have nodes; max_ctx + the smallest of their trees
+ *             beyond max_seq is LS_ERR_KV_OVERFLOW.  An understated bound costs speed, never keys.
  *   scratch   16-byte aligned, or NULL: holds partial results of contexts that several workgroups share; less than
  *             ls_tree_attention_scratch_bytes, or none, costs speed.  Nothing in it outlasts the call.
  * Scores, softmax and sums are fp32.  A sequence whose tree finds no room behind seq_lens[b] on the device keeps its cache, and its

@@ -235,7 +235,7 @@ def tree_attention(qkv, parents, cu_nodes, cu_nodes_host, rope, k, v, seq_lens, 
     """Attention of one layer for trees of drafted tokens (ls_tree_attention): the nodes' keys and values are written behind
     the cached positions of k and v [max_batch, n_kv_heads, max_seq, head_dim].  qkv [nodes, (n_q_heads + 2 n_kv_heads) * head_dim];
     parents, cu_nodes: int32 on the GPU, cu_nodes_host: the same bounds on the host; rope: float32 [max_seq, head_dim/2, 2]
-    or None.  Returns [nodes, n_q_heads * head_dim]."""
+    or None; max_ctx: a bound of the seq_lens of sequences that have nodes.  Returns [nodes, n_q_heads * head_dim]."""
     device = _gpu(qkv)
     if k.dim() != 4 or qkv.dim() != 2 or qkv.shape[1] % k.shape[3]:
         raise ValueError("k of 4 dimensions and qkv of 2, whose columns are heads, are wanted")
