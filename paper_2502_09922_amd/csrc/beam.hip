@@ -13,20 +13,24 @@ constexpr int BEAMS_MAX = LS_BEAMS_MAX;
 // ---- selection in two launches.
 //
 // k_beam_rows reads the logits once.  A row is cut into segments of SEG tokens, a workgroup to each; a thread's EACH tokens of a segment
-// (float4s 256 apart) are a set of which it leaves the largest logit and its float4, the segment leaves its maximum and its sum of
-// exponentials.  k_beam_pick, a workgroup to a request, makes scores of them: the k best candidates of a request lie in the k
+// (float4s 256 apart), or four neighbours' together, are a set of which it leaves the largest logit and its float4, the segment leaves
+// its maximum and its sum of exponentials.  k_beam_pick, a workgroup to a request, makes scores of them: the k best candidates of a request lie in the k
 // sets whose best ones are the best, for a candidate of another set has k better ones in front of it.  It chooses those sets and reads
-// their logits again, k x EACH of beams x vocab.
+// their logits again, k x EACH (x 4) of beams x vocab.
 //
 // Order: the higher score; of equal ones the lower beam, the larger logit, the lower token.  Within a beam that is the order of the
 // logits, so that a set's best is known before its row's sum is.
 //
-// Bound by the one reading: 64 x 5 rows of 50257 tokens (64 MB) 13.4 us, 4.8 TB/s; the choice 10.1, most of it waits one after
-// the other (sums, bound, sets, tokens), 7.2 for one request.
+// Bound by the one reading: 64 x 5 rows of 50257 tokens (64 MB) 13.3 us, 4.8 TB/s; the choice 7.9, most of it waits one after the
+// other (sums, bound, sets, tokens), 6.0 for one request.
 constexpr int SEG = 8192, EACH = SEG / 256;
-constexpr int HELD = 12288;            // sets in LDS: what 5 beams of 64k tokens leave, or 12 of 32k
-constexpr int LIST = 2048;             // candidates in LDS: >= BEAMS_MAX * EACH
+constexpr int HELD = 12288;            // sets in LDS: what 5 beams of 64k tokens leave, four times as many for up to 16 candidates
+constexpr int LIST = 2048;             // candidates in LDS: >= BEAMS_MAX * EACH, 16 * 4 EACH
 constexpr float LOG2E = 1.4426950408889634f;
+
+// Sets of a segment, as a power of two: those of four threads together for up to 16 candidates, whose sets' tokens then still fit LIST.
+// 8 requests of 8 beams of 128256 tokens, 16 candidates 18.0 us, 31.7 with a set to a thread; 64 of 5 of 50257, 10 candidates 20.4 and 22.5.
+__host__ __device__ constexpr int set_bits(int k) { return k <= 16 ? 6 : 8; }
 
 struct Set {
   float m;  // the largest logit of its tokens
@@ -57,7 +61,7 @@ __device__ __forceinline__ Cand cand_xor(Cand c, int off) {
 }
 
 __global__ void __launch_bounds__(256)
-k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended, int vocab, int nseg, Set* __restrict__ sets, SegSum* __restrict__ sums) {
+k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended, int vocab, int nseg, int bits, Set* __restrict__ sets, SegSum* __restrict__ sums) {
   typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));  // a row may start anywhere
   const int row = blockIdx.x, seg = blockIdx.y, tid = threadIdx.x;
   if (ended && ended[row]) return;  // its logits are not used
@@ -86,7 +90,22 @@ k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended,
       best = first + j * 1024;
     }
   }
-  sets[((size_t)row * nseg + seg) * 256 + tid] = Set{m, best};
+  if (bits == 8) {
+    sets[((size_t)row * nseg + seg) * 256 + tid] = Set{m, best};
+  } else {  // of equal ones the lowest
+    float m4 = m;
+    int best4 = best;
+#pragma unroll
+    for (int off = 1; off < 4; off *= 2) {
+      const float mo = __shfl_xor(m4, off);
+      const int bo = __shfl_xor(best4, off);
+      if (mo > m4 || (mo == m4 && bo < best4)) {
+        m4 = mo;
+        best4 = bo;
+      }
+    }
+    if ((tid & 3) == 0) sets[((size_t)row * nseg + seg) * 64 + (tid >> 2)] = Set{m4, best4};
+  }
   // sums behind the workgroup's maximum; the difference before the product, whose rounding then is each addend's own
   __shared__ float top[4];
   __shared__ double part[4];
@@ -110,7 +129,7 @@ k_beam_rows(const float* __restrict__ logits, const int32_t* __restrict__ ended,
 
 __global__ void __launch_bounds__(1024)
 k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, const int32_t* __restrict__ ended, int beams, int vocab, int k, int eos,
-            int nseg, unsigned nseg_inv, const Set* __restrict__ sets, const SegSum* __restrict__ sums, int32_t* __restrict__ rows_out, int32_t* __restrict__ tokens,
+            int nseg, unsigned nseg_inv, int bits, const Set* __restrict__ sets, const SegSum* __restrict__ sums, int32_t* __restrict__ rows_out, int32_t* __restrict__ tokens,
             float* __restrict__ scores_out) {
   constexpr int NT = 1024;
   enum { DEAD = 0, LIVE = 1, ENDED = 2 };
@@ -129,7 +148,12 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
   __shared__ float rough_bound;
   const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const size_t row0 = (size_t)g * beams;
-  const int C = nseg * 256, N = beams * C;
+  const int C = nseg << bits, N = beams * C;
+  const int wide = 10 - bits, each_set = 13 - bits;  // neighbouring tokens of a set, all of its tokens, as powers of two
+  static_assert(SEG == 1 << 13, "");
+  auto beam_of = [&](int e) { return (int)__umulhi((unsigned)(e >> bits) * 2u, nseg_inv); };
+  auto first_of = [&](int c) { return (c >> bits) * SEG + ((c & ((1 << bits) - 1)) << wide); };  // of the c-th set of a row
+  const int eos_at = (eos / SEG << bits) + ((eos & 1023) >> wide);  // the set that holds it
   const Set* mine_sets = sets + row0 * C;
   // Sets go through LDS, HELD at a time: all on their way at once, and then short loops.  (The loops unrolled: 18.4 us for 64 x 5 beams
   // instead of 15.1.)
@@ -168,7 +192,7 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
       base[beam] = b;
       most[beam] = end ? score : M;
       const bool live = state[beam] == LIVE, over = state[beam] == ENDED;
-      rough[beam] = Rough{live ? M : 0.f, live ? (float)b : -INFINITY, score, over ? beam * C + eos / SEG * 256 + (eos / 4 & 255) : -1};
+      rough[beam] = Rough{live ? M : 0.f, live ? (float)b : -INFINITY, score, over ? beam * C + eos_at : -1};
     }
   }
   if (tid == 0) {
@@ -190,11 +214,10 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
   };
   // the best of set e.  Its token is that of a float4: sets share none, so that it orders them
   auto best_of = [&](int e, Set s) {
-    const int beam = (int)__umulhi((unsigned)(e >> 8) * 2u, nseg_inv), c = e - beam * C, first = (c >> 8) * SEG + (c & 255) * 4;
+    const int beam = beam_of(e), c = e - beam * C, first = first_of(c);
     if (first >= vocab) return Cand{-INFINITY, 0.f, NONE};
     if (state[beam] == LIVE) return score_of(beam, s.m, s.at);
-    const bool has_eos = eos >= first && eos < (c >> 8) * SEG + SEG && (((eos - first) >> 2) & 255) == 0;
-    return score_of(beam, 0.f, state[beam] == ENDED && has_eos ? eos : first);
+    return score_of(beam, 0.f, state[beam] == ENDED && c == eos_at ? eos : first);
   };
   // f(set, what it left) for all of this thread's: it reads what it has written itself
   auto each = [&](auto f) {
@@ -229,7 +252,7 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
   // ---- a bound: the k-th best of 64 parts' best sets; then the sets that are no worse.  In 32 bits with room for their rounding, 2^-24
   // of the logit, the base (twice) and the sum each
   auto rounded = [&](int e, float m, float way) {  // 64 neighbouring sets are one beam's
-    const Rough b = rough[__umulhi((unsigned)(__builtin_amdgcn_readfirstlane(e) >> 8) * 2u, nseg_inv)];
+    const Rough b = rough[beam_of(__builtin_amdgcn_readfirstlane(e))];
     const float f = (m - b.most) + b.base;
     return e == b.eos_set ? b.score : f + way * 0x1p-21f * (fabsf(f) + fabsf(b.base));  // of a dead beam NaN
   };
@@ -351,9 +374,9 @@ k_beam_pick(const float* __restrict__ logits, const float* __restrict__ scores, 
   // ---- the tokens of the chosen sets: the k-th best set's best one bounds the k-th best token
   Cand least = bound;
   least.at |= 3;  // the last token of its float4 that may be it
-  for (int i = tid; i < sel * EACH; i += NT) {
-    const int e = chosen[i / EACH], q = i % EACH;
-    const int beam = (int)__umulhi((unsigned)(e >> 8) * 2u, nseg_inv), c = e - beam * C, token = (c >> 8) * SEG + (c & 255) * 4 + (q >> 2) * 1024 + (q & 3);
+  for (int i = tid; i < sel << each_set; i += NT) {
+    const int e = chosen[i >> each_set], q = i & ((1 << each_set) - 1);
+    const int beam = beam_of(e), token = first_of(e - beam * C) + (q >> wide) * 1024 + (q & ((1 << wide) - 1));
     if (token >= vocab) continue;
     const Cand d = score_of(beam, state[beam] == LIVE ? logits[(row0 + beam) * vocab + token] : 0.f, token);
     if (sel < k || !before(least, d)) {
@@ -478,7 +501,7 @@ extern "C" {
 
 size_t ls_beam_select_scratch_bytes(int groups, int beams, int vocab, int k) {
   if (!select_ok(groups, beams, vocab, k)) return 0;
-  return (size_t)groups * beams * ((vocab + ls::SEG - 1) / ls::SEG) * (256 * sizeof(ls::Set) + sizeof(ls::SegSum));
+  return (size_t)groups * beams * ((vocab + ls::SEG - 1) / ls::SEG) * ((sizeof(ls::Set) << ls::set_bits(k)) + sizeof(ls::SegSum));
 }
 
 ls_status ls_beam_select(const float* logits, const float* scores, const int32_t* ended, int groups, int beams, int vocab, int k, int eos,
@@ -498,9 +521,10 @@ ls_status ls_beam_select(const float* logits, const float* scores, const int32_t
   ls::Set* sets = (ls::Set*)(sums + (size_t)n * nseg);
   // x / nseg = umulhi(2 x, nseg_inv) for the x < 64 nseg there are, nseg <= 2048: the product is off by less than x nseg < 2^31
   const unsigned nseg_inv = (unsigned)(((1ull << 31) + nseg - 1) / nseg);
+  const int bits = ls::set_bits(k);
   hipStream_t st = (hipStream_t)hip_stream;
-  ls::k_beam_rows<<<dim3(n, nseg), 256, 0, st>>>(logits, ended, vocab, nseg, sets, sums);
-  ls::k_beam_pick<<<groups, 1024, 0, st>>>(logits, scores, ended, beams, vocab, k, eos, nseg, nseg_inv, sets, sums, rows, tokens, scores_out);
+  ls::k_beam_rows<<<dim3(n, nseg), 256, 0, st>>>(logits, ended, vocab, nseg, bits, sets, sums);
+  ls::k_beam_pick<<<groups, 1024, 0, st>>>(logits, scores, ended, beams, vocab, k, eos, nseg, nseg_inv, bits, sets, sums, rows, tokens, scores_out);
   return launched(who);
 }
 

@@ -175,3 +175,22 @@ def test_calls_on_streams_of_their_own():
         assert all(torch.equal(x, y) for x, y in zip(want, got))
         moved = k[:, want[0].view(-1).long().cpu()]
         assert torch.equal(gk.cpu(), moved) and torch.equal(gv.cpu(), moved)
+
+
+@pytest.mark.parametrize("vocab", [16, 1023, 8200, 33000])
+@pytest.mark.parametrize("k", [1, 15, 16, 17])
+def test_sets_of_one_thread_and_of_four(k, vocab):
+    """Up to 16 candidates and more, whose sets of tokens differ; equal logits within and across sets; the end token anywhere."""
+    from paper_2502_09922_amd import beam_select
+
+    g = torch.Generator().manual_seed(vocab + k)
+    for i in range(6):
+        logits = torch.randn(12, vocab, generator=g) * 3
+        logits = logits.round() if i % 2 else logits
+        scores, ended = -torch.rand(12, generator=g), (torch.rand(12, generator=g) < 0.25).int()
+        eos = int(torch.randint(vocab, (1,), generator=g))
+        got = [t.cpu() for t in beam_select(logits.cuda(), scores.cuda(), beams=6, k=k, ended=ended.cuda(), eos=eos)]
+        want = plain.select(logits, scores, ended, 6, k, eos)
+        assert torch.equal(got[0], want[0].int()) and torch.equal(got[1], want[1].int())
+        # the sum: 32 terms, each off by 2^-22 (difference, product, exponential), added in 32 bits; its logarithm; the output's rounding
+        assert ((got[2].double() - want[2]).abs() <= 2.0**-18 + 2.0**-23 * want[2].abs()).all()
