@@ -322,7 +322,7 @@ size_t ls_tree_attention_scratch_bytes(const ls_heads* heads, const ls_tree* tre
  *             beyond max_seq is LS_ERR_KV_OVERFLOW.  An understated bound costs speed, never keys.
  *   scratch   16-byte aligned, or NULL: holds partial results of contexts that several workgroups share; less than
  *             ls_tree_attention_scratch_bytes, or none, costs speed.  Nothing in it outlasts the call.
- * Scores, softmax and sums are fp32.  A sequence whose tree finds no room behind seq_lens[b] on the device keeps its cache, and its
+ * Scores, softmax and sums are fp32; products of bf16 rows take queries and weights as two bf16 each, off by 2^-15 at most.  A sequence whose tree finds no room behind seq_lens[b] on the device keeps its cache, and its
  * output rows are zeros.
  */
 ls_status ls_tree_attention(const ls_heads* heads, const ls_tree* tree, int batch, int max_ctx, const void* qkv, const float* rope,

@@ -8,7 +8,9 @@
 //   bf16: v_mfma_f32_16x16x32_bf16, steps of 32 keys.  The k index of the second product runs over keys {4g..4g+3, 16+4g..16+4g+3},
 // g = lane / 16; V^T comes out of transposing LDS reads of the row-major tile.  Queries are turned in fp32 and enter as a sum of two
 // bf16 (16 bits and more of them): rounded once they would move every score by 2^-9 of its size, which costs more than the
-// rounding of the output.  Weights are rounded to bf16 for the second product, their sums are of the rounded ones.
+// rounding of the output.  So do weights, split towards zero and with a second part that is never zero: rounded to one bf16 they moved outputs
+// by as much as the outputs' own rounding does (70B, 64 ragged trees 89 us with one part, 98 with two; fewer columns wait for memory), and parts
+// of one sign keep an infinite value what it is.
 //   fp32: v_mfma_f32_16x16x4_f32, steps of 16 keys.  The k index is lane / 16; a 16-byte read of a key's or a value's row serves four
 // products, of dims 16 j + 4 g + e of a key, and of rows 64 j + 4 (lane % 16) + e of V^T, which are the dims that a result's
 // lane holds 4 apart.
@@ -24,7 +26,7 @@
 //
 // Bound by memory where columns are few: 13B, 32 sequences of 1024 to 1087 keys, 16 nodes (723 MB of cache) 131 us, 5.5 TB/s.  With
 // many columns a tile's chain of reads, products, softmax and products is waited for, with two or three wavefronts on a SIMD: 70B, 64
-// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 88 us, the matrix cores busy for a quarter of it, the vector
+// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 98 us, the matrix cores busy for a quarter of it, the vector
 // units for a third, LDS for an eighth, no bank conflicts.  One sequence waits for its preamble (bounds, parents, table, queries:
 // 5 us) and the second launch (3 us): 7B, 3000 keys, 26 nodes 18.5 us of which 7 are the cache's reading.
 #include "tree.hpp"
@@ -45,6 +47,14 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 template <class T, int HD> __device__ __forceinline__ int key_swizzle(int key) { return HD == 128 || sizeof(T) == 4 ? key & 15 : ((key & 3) << 1) | ((key >> 2) & 1); }
 template <class T, int HD> __device__ __forceinline__ int value_swizzle(int key) {
   return sizeof(T) == 4 ? 0 : HD == 128 ? (key & 7) << 1 : ((key & 3) << 1) | ((key >> 2) & 1);
+}
+
+// v as a sum of two bf16: the first is v cut off, the second the rest, rounded, at least 2^-23 of v and of its sign.  Off by 2^-15 of v at
+// most; infinite factors take part with their sign alone (inf + 0 inf or inf - inf would be no number).  0 stays 0.
+__device__ __forceinline__ void two_parts(float v, bf16& first, bf16& second) {
+  const unsigned bits = __builtin_bit_cast(unsigned, v);
+  first = __builtin_bit_cast(bf16, (unsigned short)(bits >> 16));
+  second = (bf16)(__builtin_bit_cast(float, bits | 1u) - __builtin_bit_cast(float, bits & 0xFFFF0000u));
 }
 
 // Values that are no numbers become zeros; whether there were any.
@@ -294,10 +304,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 
   f32x4 o[DT];
   float m_run = -INFINITY;
-  f32x4 l_run{0.f, 0.f, 0.f, 0.f};  // bf16: all rows of a product alike; fp32: the first, a lane's sum
-  bf16x8 ones;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) ones[i] = (bf16)1.f;
+  float l_run = 0.f;  // of this lane's keys
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
   const float scale = 1.4426950408889634f / sqrtf((float)HD);  // score -> exponent of 2
@@ -380,16 +387,23 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     const float mc = m_run == -INFINITY ? 0.f : m_run * scale;
 #pragma unroll
     for (int i = 0; i < 4 * HALVES; ++i) s[i >> 2][i & 3] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale, -mc));
+    // four products less of 68 in fp32; in bf16 (a row of ones) the registers for it are not there
+    l_run += (s[0][0] + s[0][1]) + (s[0][2] + s[0][3]);
     if constexpr (sizeof(T) == 2) {
-      bf16x8 pf;
+      l_run += (s[1][0] + s[1][1]) + (s[1][2] + s[1][3]);
+      bf16x8 pf[2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) pf[i] = (bf16)s[i >> 2][i & 3];
-      // their sum is of the rounded ones, another row of the product: a single large weight then divides out
-      l_run = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf, l_run, 0, 0, 0);
+      for (int i = 0; i < 8; ++i) {
+        bf16 first, second;
+        two_parts(s[i >> 2][i & 3], first, second);
+        pf[0][i] = first;
+        pf[1][i] = second;
+      }
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf, o[d], 0, 0, 0);
+      for (int part = 1; part >= 0; --part)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[d], pf[part], o[d], 0, 0, 0);
     } else {
-      l_run[0] += (s[0][0] + s[0][1]) + (s[0][2] + s[0][3]);  // of this lane's keys; four products less of 68
 #pragma unroll
       for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
@@ -486,7 +500,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     }
   }
 
-  if constexpr (sizeof(T) == 4) l_run[0] = exchange<16, 32>(l_run[0], Add{});
+  l_run = exchange<16, 32>(l_run, Add{});
   if constexpr (KW > 1) {  // ---- the splits' results, in their order
     __shared__ float sm_m[KW][COLS], sm_l[KW][COLS];
     __syncthreads();  // nobody reads tiles any more
@@ -494,7 +508,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     const int at = share * 16 + lr;
     if (lg == 0) {
       sm_m[split][at] = m_run;
-      sm_l[split][at] = l_run[0];
+      sm_l[split][at] = l_run;
     }
 #pragma unroll
     for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(sm_o + (split * COLS + at) * (HD + SM_PAD) + dim_of(i)) = piece(i);
@@ -533,7 +547,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     if (at >= t.n * G) return;
     const size_t row = row_of(at);
     if (whole) {
-      const float inv = 1.0f / l_run[0];
+      const float inv = 1.0f / l_run;
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
         const f32x4 p = piece(i);
@@ -545,7 +559,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
     } else {
 #pragma unroll
       for (int i = 0; i < DT; ++i) *reinterpret_cast<f32x4*>(part_o + (pieces + row) * HD + dim_of(i)) = piece(i);
-      if (lg == 0) part_ml[pieces + row] = float2{m_run, l_run[0]};
+      if (lg == 0) part_ml[pieces + row] = float2{m_run, l_run};
     }
   }
 }
