@@ -6,11 +6,10 @@
 // A lane of a result holds column lane % 16 and rows 4 (lane / 16) + e: one column's running maximum and sum are per-lane values
 // and exchanges with lanes +-16 and +-32, and the weights that a lane has are a B operand as they are.
 //   bf16: v_mfma_f32_16x16x32_bf16, steps of 32 keys.  The k index of the second product runs over keys {4g..4g+3, 16+4g..16+4g+3},
-// g = lane / 16; V^T comes out of transposing LDS reads of the row-major tile.  Queries are turned in fp32 and enter as a sum of two
-// bf16 (16 bits and more of them): rounded once they would move every score by 2^-9 of its size, which costs more than the
-// rounding of the output.  So do weights, split towards zero and with a second part that is never zero: rounded to one bf16 they moved outputs
-// by as much as the outputs' own rounding does (70B, 64 ragged trees 89 us with one part, 98 with two; fewer columns wait for memory), and parts
-// of one sign keep an infinite value what it is.
+// g = lane / 16; V^T comes out of transposing LDS reads of the row-major tile.  Queries are turned in fp32; they and the weights enter as sums
+// of two bf16 (two_parts): rounded once, queries would move every score by 2^-9 of its size, which costs more than the rounding of the
+// output, and weights outputs by as much as that (70B, 64 ragged trees 89 us with one part of the weights, 98 with two; fewer columns wait for
+// memory).  The parts are of one sign and the second is never zero, so that infinite keys and values are what they are in one product.
 //   fp32: v_mfma_f32_16x16x4_f32, steps of 16 keys.  The k index is lane / 16; a 16-byte read of a key's or a value's row serves four
 // products, of dims 16 j + 4 g + e of a key, and of rows 64 j + 4 (lane % 16) + e of V^T, which are the dims that a result's
 // lane holds 4 apart.
@@ -294,10 +293,13 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
           u0 = w0;
           u1 = w1;
         }
-        qh[kk][2 * p] = (bf16)u0;
-        qh[kk][2 * p + 1] = (bf16)u1;
-        ql[kk][2 * p] = (bf16)(u0 - (float)qh[kk][2 * p]);
-        ql[kk][2 * p + 1] = (bf16)(u1 - (float)qh[kk][2 * p + 1]);
+        bf16 first[2], second[2];
+        two_parts(u0, first[0], second[0]);
+        two_parts(u1, first[1], second[1]);
+        qh[kk][2 * p] = first[0];
+        qh[kk][2 * p + 1] = first[1];
+        ql[kk][2 * p] = second[0];
+        ql[kk][2 * p + 1] = second[1];
       }
     }
   }

@@ -52,3 +52,33 @@ def test_infinite_cached_values_stay_what_they_are(heads, dtype, bad):
         assert (out[:12, : hq // hkv, 2] == bad).all()
         out[:12, : hq // hkv, 2] = clean[:12, : hq // hkv, 2]
         assert torch.equal(out, clean)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads", [(2, 2, 128), (4, 2, 64), (16, 1, 128), (3, 1, 96)], ids=lambda h: "%dx%dx%d" % h)
+@pytest.mark.parametrize("turn", [False, True], ids=["as they come", "turned"])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf])
+def test_infinite_keys(heads, dtype, turn, bad):
+    """A cached key with an infinite value: rows whose query is of the other sign there have it at a weight of zero, the others have no number."""
+    hq, hkv, hd = heads
+    c = make(heads, dtype, [40, 50], [12, 5], 22)
+    c["k"][0, 0, 10, 2] = bad
+    out, k, v = call(c, turn=turn)
+    out = out.double().view(-1, hq, hd)
+    rows = c["qkv"].double().view(17, -1, hd)[:, :hq]
+    pos = [c["ctxs"][b] + len(plain.path(t, i)) - 1 for b, t in enumerate(c["trees"]) for i in range(len(t))]
+    q = plain.turned(rows, c["rope"].double() if turn else None, pos)[:12]
+    at = q[:, : hq // hkv, 2]  # what the infinite value is multiplied by
+    assert (at.abs() > 1e-4).all() and ((at > 0) == (bad > 0)).any() and ((at > 0) != (bad > 0)).any()
+    got = out[:12, : hq // hkv]
+    assert (got.isnan().all(-1) == ((at > 0) == (bad > 0))).all()
+    assert torch.isfinite(out[12:]).all() and torch.isfinite(out[:12, hq // hkv :]).all()
+    want, weighted, size = plain.attend(q, k[0, :, :52].double(), v[0, :, :52].double(), 40, c["trees"][0])
+    k[0, 0, 10, 2] = 0.0  # sizes of the other scores
+    size = plain.attend(q, k[0, :, :52].double(), v[0, :, :52].double(), 40, c["trees"][0])[2][:, : hq // hkv]
+    keep = ~got.isnan()
+    # queries turned in 32 bits enter as two bf16 parts, of which the second is rounded: 2^-15 of them
+    ds = (hd + 10) * 2.0**-24 * size + (2.0**-15 * size if dtype == torch.bfloat16 else 2.0**-21)
+    weights = (2.0**-15 if dtype == torch.bfloat16 else 0.0) + 2 * ds + 70 * 2.0**-24
+    err, want = (got - want[:, : hq // hkv]).abs(), want[:, : hq // hkv]
+    assert float((err / (U[dtype] * want.abs() + 1.01 * weights * weighted[:, : hq // hkv]))[keep].max()) <= 1
