@@ -386,7 +386,7 @@ ls_status ls_beam_select(const float* logits, const float* scores, const int32_t
  * The sequences [0, batch) are groups of `group` neighbours (1..LS_BEAMS_MAX, a divisor of batch).
  *   src      int32 [batch] sequence index (the rows of ls_beam_select where k = beams); one outside b's group counts as b
  *   first    optional int32 [batch]: positions below it are the same in b and src[b] already, as a shared prompt's are
- *   max_ctx  host-side upper bound of seq_lens[b]; positions at and beyond it are not moved
+ *   max_ctx  host-side upper bound of seq_lens[b], max_seq at most; an understated bound costs speed, never positions
  */
 ls_status ls_kv_reorder(const ls_heads* heads, int layers, const int32_t* src, int batch, int group, const int32_t* first, int max_ctx,
                         const ls_kv* kv, void* hip_stream);

@@ -296,7 +296,7 @@ def beam_select(logits, scores, beams: int, k: int, ended=None, eos: int = 0):
 
 def kv_reorder(src, group: int, k, v, seq_lens, max_ctx: int, first=None):
     """Give each sequence the cache of sequence src[b] of its group, in place (ls_kv_reorder); k and v [layers, max_batch,
-    n_kv_heads, max_seq, head_dim], src and first: int32, one for each sequence."""
+    n_kv_heads, max_seq, head_dim], src and first: int32, one for each sequence; max_ctx: a bound of seq_lens."""
     device = _gpu(k)
     heads, kv = _cache(k, v, seq_lens, 5)
     _run(device, lib.ls_kv_reorder, C.byref(heads), k.shape[0], _tensor("src", src, torch.int32, device), src.numel(), group,

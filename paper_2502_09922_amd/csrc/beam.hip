@@ -407,17 +407,18 @@ __device__ __forceinline__ int source(const int32_t* __restrict__ src, int b, in
 }
 
 // The positions of a request's W sequences, W or fewer, in place: a thread has a U-sized piece of all of them in registers before
-// it writes any.  Workgroups of a (layer, kv head) walk the positions that anybody moves, which the device alone knows.
+// it writes any.  Workgroups of a (layer, kv head) walk the positions that anybody moves, which the device alone knows, however many
+// workgroups the host's bound of the lengths has made.
 // Bound by memory: 13B, 8 x 4 beams of up to 1087 positions, four layers, 4.1 GB read and written at 5.6 TB/s, where a copy of 1 GiB
 // moves 5.2.
 template <int W, class U>
 __global__ void __launch_bounds__(256, 1)
 k_reorder(const int32_t* __restrict__ src, const int32_t* __restrict__ first, const int32_t* __restrict__ seq_lens, int group, int max_batch, int hkv,
-          int max_seq, int max_ctx, int pieces, U* __restrict__ kc, U* __restrict__ vc) {
+          int max_seq, int pieces, U* __restrict__ kc, U* __restrict__ vc) {
   const int lo = blockIdx.z * group, layer = blockIdx.y / hkv, kh = blockIdx.y % hkv;
   const size_t seq = (size_t)hkv * max_seq * pieces;
   const size_t head = ((size_t)layer * max_batch * hkv + kh) * max_seq * pieces;
-  int from[W], p0[W], p1[W], start = max_ctx, end = 0;
+  int from[W], p0[W], p1[W], start = max_seq, end = 0;
 #pragma unroll
   for (int j = 0; j < W; ++j) {
     from[j] = lo + j;
@@ -426,7 +427,7 @@ k_reorder(const int32_t* __restrict__ src, const int32_t* __restrict__ first, co
       from[j] = source(src, lo + j, lo, group);
       if (from[j] != lo + j) {
         p0[j] = first ? max(first[lo + j], 0) : 0;
-        p1[j] = min(seq_lens[from[j]], max_ctx);
+        p1[j] = min(seq_lens[from[j]], max_seq);
         if (p0[j] < p1[j]) {
           start = min(start, p0[j]);
           end = max(end, p1[j]);
@@ -470,11 +471,11 @@ void launch_reorder(const int32_t* src, const int32_t* first, int32_t* seq_lens,
   // A workgroup for each 256 pieces below max_ctx where those are many, a quarter of that where it is few that have work (7B, four beams, 88
   // of 600 positions: 14.0 us, 18.1 with all; 13B, 8 x 4 beams: 760 and 735).  An odd number: ids go round the eight XCDs, and a number
   // of fours or eights leaves the few with work on some of them (10 of 100 positions, 256 heads: 12.8 us with 7, 22.5 with 8).
-  const size_t blocks = ((size_t)max_ctx * pieces + 255) / 256, heads = (size_t)layers * hkv * groups;
+  const size_t blocks = ((size_t)std::max(max_ctx, 1) * pieces + 255) / 256, heads = (size_t)layers * hkv * groups;
   const dim3 grid((unsigned)(std::min<size_t>(blocks * heads > MANY ? blocks : (blocks + 3) / 4, 1 << 20) | 1), layers * hkv, groups);
 #define LS_REORDER(w)                                                                                                                    \
   if (group <= w) {                                                                                                                      \
-    k_reorder<w, U><<<grid, 256, 0, st>>>(src, first, seq_lens, group, max_batch, hkv, max_seq, max_ctx, pieces, (U*)kc, (U*)vc);        \
+    k_reorder<w, U><<<grid, 256, 0, st>>>(src, first, seq_lens, group, max_batch, hkv, max_seq, pieces, (U*)kc, (U*)vc);                 \
     return;                                                                                                                              \
   }
   LS_REORDER(4) LS_REORDER(8) LS_REORDER(16) LS_REORDER(32) LS_REORDER(64)
@@ -542,14 +543,12 @@ ls_status ls_kv_reorder(const ls_heads* h, int layers, const int32_t* src, int b
   const size_t row = (size_t)h->head_dim * (h->dtype == LS_DTYPE_F32 ? 4 : 2);
   const bool wide = row % 16 == 0 && (((uintptr_t)kv->k | (uintptr_t)kv->v) & 15) == 0;
   if (group == 1) return LS_OK;
-  if (max_ctx > 0) {
-    if (wide)
-      ls::launch_reorder<ls::u32x4>(src, first, kv->seq_lens, batch / group, group, layers, (int)h->max_batch, (int)h->n_kv_heads, (int)h->max_seq, max_ctx,
-                                (int)(row / 16), kv->k, kv->v, st);
-    else
-      ls::launch_reorder<uint32_t>(src, first, kv->seq_lens, batch / group, group, layers, (int)h->max_batch, (int)h->n_kv_heads, (int)h->max_seq,
-                                   max_ctx, (int)(row / 4), kv->k, kv->v, st);
-  }
+  if (wide)
+    ls::launch_reorder<ls::u32x4>(src, first, kv->seq_lens, batch / group, group, layers, (int)h->max_batch, (int)h->n_kv_heads, (int)h->max_seq, max_ctx,
+                                  (int)(row / 16), kv->k, kv->v, st);
+  else
+    ls::launch_reorder<uint32_t>(src, first, kv->seq_lens, batch / group, group, layers, (int)h->max_batch, (int)h->n_kv_heads, (int)h->max_seq,
+                                 max_ctx, (int)(row / 4), kv->k, kv->v, st);
   ls::k_reorder_lens<<<batch / group, 64, 0, st>>>(src, group, kv->seq_lens);
   return launched(who);
 }
