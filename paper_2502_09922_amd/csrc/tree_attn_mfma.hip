@@ -567,7 +567,7 @@ k_tree_mfma(const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens
 }
 
 // Rows of sequences of several chunks: the chunks' results in chunk order, four dims to a thread.  They are asked for before it is known
-// whose row this is, and how many of them there are.
+// whose row this is, and how many of them there are.  Whose it is all sequences are asked: bounds that only the device knows need not rise.
 template <class T, int HD>
 __global__ void __launch_bounds__(256)
 k_tree_merge(const float* __restrict__ part_o, const float2* __restrict__ part_ml, const int32_t* __restrict__ cu, const int32_t* __restrict__ seq_lens,
@@ -587,14 +587,15 @@ k_tree_merge(const float* __restrict__ part_o, const float2* __restrict__ part_m
     }
   };
   load(0);
-  int b = 0, end = batch;  // the sequence with cu[b] <= r < cu[b + 1]
-  while (end - b > 1) {
-    const int mid = (b + end) >> 1;
-    if (cu[mid] <= r) b = mid;
-    else end = mid;
-  }
+  __shared__ int whose;
+  if (threadIdx.x == 0) whose = batch;
+  __syncthreads();
   TreeSeq t;
-  if (!tree_seq(cu, seq_lens, b, rows, most, max_seq, t) || r < t.row0 || r >= t.row0 + t.n) return;
+  for (int b = threadIdx.x; b < batch; b += 256)
+    if (tree_seq(cu, seq_lens, b, rows, most, max_seq, t) && r >= t.row0 && r < t.row0 + t.n) atomicMin(&whose, b);
+  __syncthreads();
+  if (whose == batch) return;
+  tree_seq(cu, seq_lens, whose, rows, most, max_seq, t);
   const int n = min((t.ctx + t.n + chunk_keys - 1) / chunk_keys, nchunk);
   if (n == 1) return;  // the first pass wrote these rows
   const float scale = 1.4426950408889634f / sqrtf((float)HD);
