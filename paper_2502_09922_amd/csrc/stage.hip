@@ -143,6 +143,16 @@ constexpr size_t TILED_SCRATCH_MAX = 64u << 20;
 // most rows of a pass with the norms inside its GEMMs: a generation step's, or a few nodes of trees
 size_t fused_rows(const ls_cfg* c) { return std::max(c->max_batch, std::min(c->max_tokens, 16u)); }
 
+// Rows that the workspace has logits for: a generation step's, or 64 nodes of a tree for each sequence, but no more than 64 MiB hold
+// (a multiple of four rows, so that logits of an odd width start on 16 bytes piece by piece).  A pass over more nodes reads the head again for
+// each so many, with logits_out too: what is said does not depend on it.
+constexpr size_t HEAD_LOGITS_MAX = 64u << 20;
+int head_rows(const ls_cfg* c) {
+  const size_t fit = HEAD_LOGITS_MAX / (sizeof(float) * std::max(c->vocab, 1u));
+  const size_t trees = std::min({(size_t)c->max_tokens, (size_t)c->max_batch * LS_TREE_MAX, fit});
+  return (int)((std::max((size_t)c->max_batch, trees) + 3) / 4 * 4);
+}
+
 Carve carve(const ls_cfg* c, int lo, int hi) {
   Carve w{};
   const size_t e = isz(c), T = c->max_tokens, B = c->max_batch, d = c->hidden;
@@ -156,7 +166,7 @@ Carve carve(const ls_cfg* c, int lo, int hi) {
   w.qkv = take(T * qkv_cols * e);
   w.attn = take(T * (size_t)c->n_q_heads * c->head_dim * e);
   w.h = take(T * (size_t)c->ffn * e);
-  w.logits = take(last ? B * (size_t)c->vocab * sizeof(float) : 0);
+  w.logits = take(last ? (size_t)head_rows(c) * c->vocab * sizeof(float) : 0);
   w.row_seq = take(T * sizeof(int32_t));
   w.row_pos = take(T * sizeof(int32_t));
   w.last_rows = take(B * sizeof(int32_t));
@@ -644,9 +654,9 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
                      (trees || attn_decode_supported(hq, hkv, hd) || attn_decode_gqa_supported(hq, hkv, hd)) &&
                      gemm_decode_fusable(rows, qkv_cols, d) && gemm_decode_fusable(rows, d, hq * hd) &&
                      gemm_decode_fusable(rows, F, d) && gemm_decode_fusable(rows, d, F);
-  // rows of the head: the sequences' last ones, or all nodes, which without logits_out go max_batch at a time, as many as the
-  // workspace has logits for
-  const int heads = trees ? rows : batch, heads_at_once = logits_out ? heads : std::min(heads, (int)c.max_batch);
+  // rows of the head: the sequences' last ones, or all nodes, as many at a time as the workspace has logits for
+  const int heads = trees ? rows : batch, heads_at_once = std::min(heads, head_rows(&c));
+  auto logits_of = [&](int r0) { return logits_out ? logits_out + (size_t)r0 * c.vocab : (float*)(ws + s->w.logits); };
   auto attend_trees = [&](const void* qkv, char* kc, char* vc, void* attn) {
     TreeAttn a = *trees;
     a.qkv = qkv; a.cs = cs; a.kc = kc; a.vc = vc; a.out = attn;
@@ -723,8 +733,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     }
     if (s->last) {
       LS_HIP(gate(*hb, st));
-      float* logits = logits_out ? logits_out : (float*)(ws + s->w.logits);
       if (head_folds) {
+        float* logits = logits_of(0);
         SkinnyFusion f_head;
         f_head.ss_in = ss_a; f_head.n_part = d / 16; f_head.eps = c.rms_eps;
         launch_gemm(dt, EPI_F32, xb, head + head_sp[1].off, heads, c.vocab, d, logits, nullptr, st, &gsc, &f_head);
@@ -732,6 +742,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       } else {
         for (int r0 = 0; r0 < heads; r0 += heads_at_once) {
           const int n = std::min(heads_at_once, heads - r0);
+          float* logits = logits_of(r0);
           launch_rmsnorm(dt, x + (size_t)r0 * d, head + head_sp[0].off, y, n, d, c.rms_eps, trees ? nullptr : last_rows, st);
           launch_gemm(dt, EPI_F32, y, head + head_sp[1].off, n, c.vocab, d, logits, nullptr, st, &gsc);
           launch_argmax(logits, n, c.vocab, (int32_t*)out + r0, st);
@@ -958,7 +969,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       const int n = std::min(heads_at_once, heads - r0);
       const int32_t* map = trees ? nullptr : last_rows;
       const float* xr = x + (size_t)r0 * d;
-      float* logits = logits_out ? logits_out : (float*)(ws + s->w.logits);
+      float* logits = logits_of(r0);
       const TiledPlan p_head = (dt == F32 || n > (d > 4096 ? 8 : 16)) && ((uintptr_t)logits & 15) == 0
                                    ? gemm_tiled_plan(dt, TILED_PART, n, (int)c.vocab, d, false, 0, nullptr, s->w.parts_bytes)
                                    : TiledPlan{};
