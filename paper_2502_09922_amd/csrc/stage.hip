@@ -806,8 +806,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   // The tiled GEMM takes every fp32 projection it supports, and the bf16 ones of all but few rows
   // where it is estimated faster than the 256 x 256 tiles.
   // Partial tiles of a generation step fit the static scratch too, so that both entry points take
-  // the same plans.
-  const size_t part_bytes = prefill || gsc.bytes < LS_STATIC_SCRATCH_BYTES ? gsc.bytes : LS_STATIC_SCRATCH_BYTES;
+  // the same plans.  Passes over trees have one entry point and as many rows as prompt passes.
+  const size_t part_bytes = prefill || trees || gsc.bytes < LS_STATIC_SCRATCH_BYTES ? gsc.bytes : LS_STATIC_SCRATCH_BYTES;
   auto plan = [&](int epi, int N, int K) {
     if (few_rows) return TiledPlan{};
     float us = 0.f;
