@@ -440,17 +440,33 @@ class Stage:
 
     def tree(self, inp, parents, cu_nodes, cu_nodes_host, max_ctx: int, stream=None, want_logits=False):
         """ls_stage_tree: the pass over the nodes of draft trees (see tree_attention for their arguments); inp, parents and
-        cu_nodes are on the stage's device.  tree_accept says which nodes to keep, tree_keep makes them positions of caches()."""
-        torch = self.torch
-        tree, batch, rows, host = _trees(parents, cu_nodes, cu_nodes_host, self.slab.device)
+        cu_nodes are on the stage's device.  tree_accept says which nodes to keep, tree_keep makes them positions of caches().
+        stream=None is torch's current stream, as for those two; prefill and decode take it for the null stream, which this pass
+        therefore runs behind, and later work on it behind this pass.  Not so tree_keep: where another stream is current, prefill and decode
+        behind it need stream=torch.cuda.current_stream()."""
+        torch, device = self.torch, self.slab.device
+        if torch.cuda.current_device() != device.index:
+            with torch.cuda.device(device):
+                return self.tree(inp, parents, cu_nodes, cu_nodes_host, max_ctx, stream, want_logits)
+        tree, batch, rows, host = _trees(parents, cu_nodes, cu_nodes_host, device)
+        x = _tensor("inp", inp, torch.int32 if self.first else self.tdtype, device, rows if self.first else rows * self.shape.hidden)
+        null, current = None, _current_stream(device.index)
+        if stream is None and current:
+            stream = torch.cuda.current_stream(device)
+            if not torch.cuda.is_current_stream_capturing():  # nothing on the null stream belongs into a graph
+                null = torch.cuda.default_stream(device)
+                stream.wait_stream(null)
+        elif stream is not None and stream.cuda_stream != current:  # the pass may outlive the caller's hold on them
+            for t in (inp, parents, cu_nodes):
+                t.record_stream(stream)
         with torch.cuda.stream(stream):  # outputs belong to the stream that writes them
-            out = (torch.empty(rows, dtype=torch.int32, device=self.device) if self.last
-                   else torch.empty(rows, self.shape.hidden, dtype=self.tdtype, device=self.device))
-            logits = torch.empty(rows, self.shape.vocab, dtype=torch.float32, device=self.device) if (want_logits and self.last) else None
-        check(lib.ls_stage_tree(self.handle, _tensor("inp", inp, torch.int32 if self.first else self.tdtype, self.slab.device,
-                                                     rows if self.first else rows * self.shape.hidden),
-                                C.byref(tree), batch, max_ctx, C.byref(self.kv), out.data_ptr(), logits.data_ptr() if logits is not None else None,
-                                self._stream_ptr(stream)))
+            out = (torch.empty(rows, dtype=torch.int32, device=device) if self.last
+                   else torch.empty(rows, self.shape.hidden, dtype=self.tdtype, device=device))
+            logits = torch.empty(rows, self.shape.vocab, dtype=torch.float32, device=device) if (want_logits and self.last) else None
+        check(lib.ls_stage_tree(self.handle, x, C.byref(tree), batch, max_ctx, C.byref(self.kv), out.data_ptr(),
+                                logits.data_ptr() if logits is not None else None, self._stream_ptr(stream)))
+        if null is not None:
+            null.wait_stream(stream)
         return (out, logits) if want_logits else out
 
     def workspace_region(self, which: int, rows: int):
