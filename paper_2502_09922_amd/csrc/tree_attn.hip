@@ -88,8 +88,11 @@ k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int3
   }
   const T* kb = kc + ((size_t)b * hkv + kh) * max_seq * hd;
   const T* vb = vc + ((size_t)b * hkv + kh) * max_seq * hd;
-  float m = -INFINITY, l = 0.f;
-  for (int key0 = 0; key0 < t.ctx + t.n; key0 += AT_ONCE) {
+  // Sums of AT_ONCE keys go into sums of NEAR times that, and those into the whole ones: one by one, equal weights next to a long sum are all
+  // rounded the same way (60000 keys: off by 7e-4).
+  constexpr int NEAR = 64;
+  float m = -INFINITY, l = 0.f, far_l = 0.f, far0[MAXP] = {}, far1[MAXP] = {};
+  for (int key0 = 0, turns = 1; key0 < t.ctx + t.n; key0 += AT_ONCE, ++turns) {
     T2 kr[AT_ONCE][MAXP], vr[AT_ONCE][MAXP];
     bool seen[AT_ONCE];
     float s[AT_ONCE], mn = m;
@@ -118,21 +121,35 @@ k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int3
     for (int j = 0; j < AT_ONCE; ++j)
       if (seen[j]) mn = fmaxf(mn, s[j]);
     const float corr = mn == -INFINITY ? 1.f : __expf(m - mn);
-    l *= corr;
-#pragma unroll
-    for (int i = 0; i < MAXP; ++i) {
-      a0[i] *= corr;
-      a1[i] *= corr;
-    }
+    float near_l = 0.f, near0[MAXP] = {}, near1[MAXP] = {};
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) {
       if (!seen[j]) continue;
       const float w = s[j] == -INFINITY ? 0.f : __expf(s[j] - mn);
-      l += w;
+      near_l += w;
 #pragma unroll
       for (int i = 0; i < MAXP; ++i) {
-        a0[i] = fmaf(w, to_f(vr[j][i][0]), a0[i]);
-        a1[i] = fmaf(w, to_f(vr[j][i][1]), a1[i]);
+        near0[i] = fmaf(w, to_f(vr[j][i][0]), near0[i]);
+        near1[i] = fmaf(w, to_f(vr[j][i][1]), near1[i]);
+      }
+    }
+    l = fmaf(l, corr, near_l);
+    far_l *= corr;
+#pragma unroll
+    for (int i = 0; i < MAXP; ++i) {
+      a0[i] = fmaf(a0[i], corr, near0[i]);
+      a1[i] = fmaf(a1[i], corr, near1[i]);
+      far0[i] *= corr;
+      far1[i] *= corr;
+    }
+    if (turns % NEAR == 0) {
+      far_l += l;
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i) {
+        far0[i] += a0[i];
+        far1[i] += a1[i];
+        a0[i] = a1[i] = 0.f;
       }
     }
     m = mn;
@@ -141,8 +158,8 @@ k_tree_attn(const T* __restrict__ qkv, const float2* __restrict__ cs, const int3
   for (int i = 0; i < MAXP; ++i) {
     const int p = lane + 64 * i;
     if (p < half) {
-      o[2 * p] = from_f<T>(a0[i] / l);
-      o[2 * p + 1] = from_f<T>(a1[i] / l);
+      o[2 * p] = from_f<T>((far0[i] + a0[i]) / (far_l + l));
+      o[2 * p + 1] = from_f<T>((far1[i] + a1[i]) / (far_l + l));
     }
   }
 }

@@ -82,3 +82,23 @@ def test_infinite_keys(heads, dtype, turn, bad):
     weights = (2.0**-15 if dtype == torch.bfloat16 else 0.0) + 2 * ds + 70 * 2.0**-24
     err, want = (got - want[:, : hq // hkv]).abs(), want[:, : hq // hkv]
     assert float((err / (U[dtype] * want.abs() + 1.01 * weights * weighted[:, : hq // hkv]))[keep].max()) <= 1
+
+
+@pytest.mark.parametrize("hd", [96, 128])
+@pytest.mark.parametrize("ctx,s", [(40000, 1.0), (60000, 1.2), (60000, 2.0)])
+def test_long_sums_of_equal_weights(hd, ctx, s):
+    """One key above, all others equal, half of them of value one: added up one by one, each step rounds a weight the same way next to a long
+    sum (4e-4 to 7e-4 of it).  Eight weights at a time, 64 times that, and those: 8 + 64 + ctx / 512 roundings of both sums; the
+    matrix cores' kernel has shorter ones."""
+    k, v = torch.zeros(1, 1, ctx + 1, hd), torch.zeros(1, 1, ctx + 1, hd)
+    c = dict(heads=(1, 1, hd), ctxs=[ctx], trees=[[-1]], cu=torch.tensor([0, 1], dtype=torch.int32).numpy(), qkv=torch.zeros(1, 3 * hd), k=k, v=v,
+             rope=torch.zeros(ctx + 1, hd // 2, 2), lens=torch.tensor([ctx], dtype=torch.int32), parents=torch.tensor([-1], dtype=torch.int32))
+    c["qkv"][0, 0] = math.sqrt(hd)
+    c["qkv"][0, hd] = -s
+    k[0, 0, 1:ctx, 0] = -s
+    v[0, 0, 1:ctx:2] = 1.0
+    out, k, v = call(c, turn=False)
+    want, weighted, size = wanted(c, k, v)
+    weights = 2 * (8 + 64 + ctx / 512 + 16) * 2.0**-24 + 2 * ((hd + 8) * 2.0**-24 * size + 2.0**-21)
+    err = (out.double().view(want.shape) - want).abs()
+    assert float((err / (weights * weighted + U[torch.float32] * want)).max()) <= 1
