@@ -8,7 +8,7 @@
 //   bf16: v_mfma_f32_16x16x32_bf16, steps of 32 keys.  The k index of the second product runs over keys {4g..4g+3, 16+4g..16+4g+3},
 // g = lane / 16; V^T comes out of transposing LDS reads of the row-major tile.  Queries are turned in fp32; they and the weights enter as sums
 // of two bf16 (two_parts): rounded once, queries would move every score by 2^-9 of its size, which costs more than the rounding of the
-// output, and weights outputs by as much as that (70B, 64 ragged trees 89 us with one part of the weights, 98 with two; fewer columns wait for
+// output, and weights outputs by as much as that (70B, 64 ragged trees 89 us with one part of the weights, 101 with two; fewer columns wait for
 // memory).  The parts are of one sign and the second is never zero, so that infinite keys and values are what they are in one product.
 //   fp32: v_mfma_f32_16x16x4_f32, steps of 16 keys.  The k index is lane / 16; a 16-byte read of a key's or a value's row serves four
 // products, of dims 16 j + 4 g + e of a key, and of rows 64 j + 4 (lane % 16) + e of V^T, which are the dims that a result's
@@ -25,7 +25,7 @@
 //
 // Bound by memory where columns are few: 13B, 32 sequences of 1024 to 1087 keys, 16 nodes (723 MB of cache) 131 us, 5.5 TB/s.  With
 // many columns a tile's chain of reads, products, softmax and products is waited for, with two or three wavefronts on a SIMD: 70B, 64
-// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 98 us, the matrix cores busy for a quarter of it, the vector
+// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 101 us, the matrix cores busy for a quarter of it, the vector
 // units for a third, LDS for an eighth, no bank conflicts.  One sequence waits for its preamble (bounds, parents, table, queries:
 // 5 us) and the second launch (3 us): 7B, 3000 keys, 26 nodes 18.5 us of which 7 are the cache's reading.
 #include "tree.hpp"
@@ -53,7 +53,7 @@ template <class T, int HD> __device__ __forceinline__ int value_swizzle(int key)
 __device__ __forceinline__ void two_parts(float v, bf16& first, bf16& second) {
   const unsigned bits = __builtin_bit_cast(unsigned, v);
   first = __builtin_bit_cast(bf16, (unsigned short)(bits >> 16));
-  second = (bf16)(__builtin_bit_cast(float, bits | 1u) - __builtin_bit_cast(float, bits & 0xFFFF0000u));
+  second = (bf16)fmaf(v, 0x1.000002p0f, -__builtin_bit_cast(float, bits & 0xFFFF0000u));
 }
 
 // Values that are no numbers become zeros; whether there were any.
