@@ -272,7 +272,8 @@ ls_status ls_stage_decode_static(ls_stage* stage, const void* in, int batch, int
  *
  * Trees of drafted tokens (speculative decoding) and beams.  But for ls_stage_tree these calls need no stage handle: they
  * work on a cache of any span of layers, one layer's for the attention, with the conventions above.  Buffers are device memory unless "host"
- * is said, 4-byte aligned at least (bf16 rows: 2); caches, rows and outputs on 16 bytes take the faster kernels.
+ * is said, aligned to their type, rope and kept to 8 bytes, the caches of ls_tree_keep and ls_kv_reorder to 4 for bf16 too; caches, rows and
+ * outputs on 16 bytes take the faster kernels.
  */
 
 /* Shape of the attention heads and of the cache they work on. */
@@ -322,8 +323,8 @@ size_t ls_tree_attention_scratch_bytes(const ls_heads* heads, const ls_tree* tre
  *             beyond max_seq is LS_ERR_KV_OVERFLOW.  An understated bound costs speed, never keys.
  *   scratch   16-byte aligned, or NULL: holds partial results of contexts that several workgroups share; less than
  *             ls_tree_attention_scratch_bytes, or none, costs speed.  Nothing in it outlasts the call.
- * Scores, softmax and sums are fp32; products of bf16 rows take queries and weights as two bf16 each, off by 2^-15 at most.  A sequence whose tree finds no room behind seq_lens[b] on the device keeps its cache, and its
- * output rows are zeros.
+ * Scores, softmax and sums are fp32; products of bf16 rows take queries and weights as two bf16 each, off by 2^-15 at most.  A sequence whose
+ * tree finds no room behind seq_lens[b] on the device keeps its cache, and its output rows are zeros.
  */
 ls_status ls_tree_attention(const ls_heads* heads, const ls_tree* tree, int batch, int max_ctx, const void* qkv, const float* rope,
                             const ls_kv* layer, void* out, void* scratch, size_t scratch_bytes, void* hip_stream);
@@ -338,7 +339,9 @@ ls_status ls_tree_attention(const ls_heads* heads, const ls_tree* tree, int batc
  *               token); otherwise [nodes, hidden].   logits_out: optional fp32 [nodes, vocab], last stage only; on 16 bytes it does
  *               not change what is said.
  * The head's weights are read once for as many nodes as the workspace has logits for: max_batch, or 64 for each sequence as far as
- * max_tokens and 64 MiB of logits go.  Rows of no sequence are computed too, from what lies there: nobody else's values depend on them.
+ * max_tokens and 64 MiB of logits go.  Rows of no sequence (bounds on the device that leave some out) are computed from what lies there;
+ * but for roundings nobody else's values depend on them.  ls_pipeline_run has prompts and generation steps alone: the stages of a pipeline are called
+ * one after the other.
  * max_ctx and sequences without room as in ls_tree_attention; the rest as in ls_stage_decode.  The probe does not see it.
  */
 ls_status ls_stage_tree(ls_stage* stage, const void* in, const ls_tree* tree, int batch, int max_ctx, const ls_kv* kv, void* out, float* logits_out,
@@ -369,8 +372,8 @@ ls_status ls_tree_keep(const ls_heads* heads, int layers, const ls_tree* tree, i
  * The k best continuations of each of `groups` requests with `beams` beams (k and beams 1..LS_BEAMS_MAX, at most 2^24 - 1 rows and 2^22 - 1
  * requests, vocab at most 2^24): row g * beams + b is beam b
  * of request g, candidate (b, token) scores scores[row] + logits[row][token] - log(sum(exp(logits[row]))).  Best first; equal
- * scores go by the lower beam, then the larger logit, then the lower token.  Scores are compared in 64 bits (the sums of
- * exponentials are of fp32 terms) and rounded to fp32 on output.  A beam whose score is not finite has no candidates but at -inf,
+ * scores go by the lower beam, then the larger logit, then the lower token.  Scores are compared in 64 bits, but for the sums of
+ * exponentials, which are of fp32 terms (two beams' candidates closer than 2^-18 may change places), and rounded to fp32 on output.  A beam whose score is not finite has no candidates but at -inf,
  * and so has one without a finite sum, all of its logits -inf, or one of them NaN or +inf; where candidates above -inf do not
  * suffice, those come in the order of beam and token.
  *   logits [groups * beams, vocab] fp32, as ls_stage_prefill and ls_stage_decode write them;  scores [groups * beams]

@@ -6,7 +6,7 @@
 // Here the kernels for every shape (the fast ones: tree_attn_mfma.hip): one rotates and appends the nodes' keys and values, one
 // attends, a wavefront to a (row, query head), a lane to one or two pairs of dims, eight keys and values on their way at once.
 // Bound by a wavefront's instructions, of which the sums over its lanes are half: 32 heads of 96 dims over 8, four sequences of 600
-// keys, 12 nodes each 115 us in bf16, 106 in fp32 (a key at a time 253 and 335; sixteen at once 116 and 109).  The same of 128 dims
+// keys, 12 nodes each 114 us in bf16, 110 in fp32 (a key at a time 253 and 335; sixteen at once no better).  The same of 128 dims
 // takes 20 on the matrix cores.
 #include "tree.hpp"
 
@@ -177,8 +177,8 @@ void launch_any(const TreeAttn& a, hipStream_t st) {
 // along the keys until each CU has one, in pieces of 128 keys at least: 7B, one sequence of 3000 keys, 26 nodes 18.3 us for 256
 // workgroups, 20.0 for 512; 8 of 900 keys 33.3 and 35.9; 600 keys, 5 nodes in pieces of 128 10.3, of 256 11.4.  With more columns,
 // whose wavefronts wait for each other, until all three places of a CU are taken, but not beyond: 70B, 16 ragged sequences of up to
-// 3000 keys, 16 nodes 53 us for 768 workgroups, 59 for 512, 63 for 1536; 13B, 16 of 1000 keys, 64 nodes (640 workgroups) 89, cut in
-// two 110.  As more rows are joined their pieces have 256 keys: 70B, 4000 keys, 8 nodes 16.8, in pieces of 128 20.2.
+// 3000 keys, 16 nodes 58 us for 768 workgroups, 59 for 512 and 58 for 1536; 13B, 16 of 1000 keys, 64 nodes (640 workgroups) 90, cut in
+// two 110; 70B, one of 4000 keys, 64 nodes 33, in smaller pieces 39.  As more rows are joined their pieces have 256 keys: 70B, 4000 keys, 8 nodes 16.8, in pieces of 128 20.2.
 TreeChunks chunks_for(const TreeAttn& a) {
   TreeChunks p;
   const int cols = a.max_nodes * (a.hq / a.hkv), wide = cols <= 16 ? 16 : cols <= 32 ? 32 : 64;

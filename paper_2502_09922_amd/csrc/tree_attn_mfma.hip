@@ -23,11 +23,12 @@
 // before it reads them: blocks of columns write the same bytes, and none depends on another workgroup's.  Only in the tiles of
 // those slots columns see different keys.
 //
-// Bound by memory where columns are few: 13B, 32 sequences of 1024 to 1087 keys, 16 nodes (723 MB of cache) 131 us, 5.5 TB/s.  With
+// Bound by memory where columns are few: 13B, 32 sequences of 1024 to 1087 keys, 16 nodes (723 MB of cache) 130 us, 5.5 TB/s.  With
 // many columns a tile's chain of reads, products, softmax and products is waited for, with two or three wavefronts on a SIMD: 70B, 64
-// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 101 us, the matrix cores busy for a quarter of it, the vector
-// units for a third, LDS for an eighth, no bank conflicts.  One sequence waits for its preamble (bounds, parents, table, queries:
-// 5 us) and the second launch (3 us): 7B, 3000 keys, 26 nodes 18.5 us of which 7 are the cache's reading.
+// trees of 4 to 16 nodes over 128 to 2287 keys (128 columns) 97 to 101 us, the matrix cores busy for 35 % of it, the vector
+// units for 38 %, LDS for 18 %, no bank conflicts; the longest context has 72 tiles, and 44 are the average of the places for workgroups.
+// One sequence waits for its preamble (bounds, parents, table, queries:
+// 5 us) and the second launch (4 us): 7B, 3000 keys, 26 nodes 19 us of which 7 are the cache's reading.
 #include "tree.hpp"
 
 #include <algorithm>
@@ -105,8 +106,8 @@ constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds 
 constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
 constexpr float FOLLOW = 8.f;
 constexpr int CUS = 256;
-// CW = 4 lives with two tiles and 168 registers, so that three workgroups fit a CU: 13B, 16 trees of 64 nodes over 1000 keys 89 us, with
-// two (four tiles, 170 registers) 96; fp32, 4 such trees 69 and 82.  CW = 2 in 168 registers gains nothing (148 and 151 us for 13B, 32
+// CW = 4 lives with two tiles and 168 registers, so that three workgroups fit a CU: 13B, 16 trees of 64 nodes over 1000 keys 89 us (90 since
+// weights have two parts), with two (four tiles, 170 registers) 96; fp32, 4 such trees 82 either way.  CW = 2 in 168 registers gains nothing (148 and 151 us of kernel for 13B, 32
 // x 26 nodes): its tiles leave room for two.
 template <int CW> constexpr int PER_CU = CW == 4 ? 3 : 2;  // workgroups on a CU, wavefronts on a SIMD
 template <class T> constexpr int TILE_KEYS = sizeof(T) == 2 ? 32 : 16;  // 16 KB of keys and values of 128 dims
@@ -645,8 +646,9 @@ void launch(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
 
 // Wavefronts share keys where columns are too many for one, as few as do.  7B, one sequence of 3000 keys, 26 nodes: 18.5 us with two 16-
 // column tiles in each pair of wavefronts, 23 with both in every wavefront, keys of its own.  Blocks of 64 columns at most, which read the cache
-// again, out of L2: blocks of 128, two tiles to a wavefront and two workgroups to a CU, took 92 us instead of 88 for 70B, 64 ragged
-// trees, 58 instead of 53 for 16 of them, 34 instead of 30 for one of 64 nodes over 4000 keys.
+// again, four fifths of it out of L2: blocks of 128, two tiles to a wavefront and two workgroups to a CU, took 92 us instead of 88 for 70B, 64
+// ragged trees, 58 instead of 53 for 16 of them, 34 instead of 30 for one of 64 nodes over 4000 keys (with weights of one part; the latter are
+// 101, 58 and 33 now).
 template <class T, int HD>
 void launch_hd(const TreeAttn& a, const TreeChunks& p, hipStream_t st) {
   const int cols = a.max_nodes * (a.hq / a.hkv);
