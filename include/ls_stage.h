@@ -397,6 +397,92 @@ ls_status ls_beam_select(const float* logits, const float* scores, const int32_t
 ls_status ls_kv_reorder(const ls_heads* heads, int layers, const int32_t* src, int batch, int group, const int32_t* first, int max_ctx,
                         const ls_kv* kv, void* hip_stream);
 
+/* ---- a cache in pages --------------------------------------------------------------------
+ *
+ * Sequences whose cached rows lie in pages of a pool, so that each holds as much memory as it needs, and may be cut down to a
+ * budget of slots by what attention gives them.  Slot i of sequence b is row i % page of page table[b][i / page]; a slot holds the key
+ * and value of one token, rotated at that token's own position, and which token that is may differ from kv head to kv head once
+ * slots have been evicted.  The conventions above; buffers are aligned to their type, rope to 8 bytes; pools, rows and outputs on 16 bytes take
+ * the faster kernels.  In ls_heads max_batch stands for the rows of table, lens and positions, and max_seq for the positions that
+ * tokens may have (the rows of rope).  A call takes 65535 sequences at most.
+ */
+typedef struct {
+  void* k; /* [layers][pages][n_kv_heads][page][head_dim], dtype                                                         */
+  void* v;
+  float* weights;           /* optional [layers][pages][n_kv_heads][page]: attention weight that a slot has got so far     */
+  int32_t* places;          /* with weights: position of the slot's token                                                  */
+  int32_t* lens;            /* [max_batch] slots that are filled, the first ones; below 0: the sequence takes no part      */
+  int32_t* positions;       /* optional [max_batch]: position of the sequence's next token; NULL: lens, for nothing is evicted */
+  const int32_t* table;     /* [max_batch][columns] pages; an entry outside [0, pages) names none                          */
+  uint32_t pages;           /* pages of the pool                                                                           */
+  uint32_t page;            /* slots of a page: a power of two from 8 to 1024                                              */
+  uint32_t columns;         /* columns * page: most slots of a sequence, 2^24 at most                                      */
+} ls_pages;
+
+/* Device bytes of scratch for an ls_paged_attention call of these arguments: with weights it has to be there, without it cuts long
+ * contexts into as many pieces as pay.  0 if the call needs none or would be refused. */
+size_t ls_paged_attention_scratch_bytes(const ls_heads* heads, const ls_pages* layer, int batch, int max_ctx);
+
+/*
+ * Attention of one layer for one new token of each sequence.  Its key and value go into slot lens[b], rotated by its position and rounded
+ * to dtype, and it attends to the slots 0..lens[b].  lens and positions are not changed (all layers of a step see the same; the
+ * caller adds one to both behind them, ls_stage_paged does).
+ *   qkv      [batch, (n_q_heads + 2 n_kv_heads) * head_dim]: query heads, key heads, value heads side by side
+ *   rope     fp32 [max_seq][head_dim/2][2], cos and sin (see ls_tree_attention), or NULL: rows come turned
+ *   layer    one layer's pools.  With weights, every slot's weight grows by what the query heads of its kv head give it (the softmax's values,
+ *            summed over those heads), the new slot's starts with that, and its place is the token's position.
+ *   out      [batch, n_q_heads * head_dim]
+ *   max_ctx  host-side upper bound of lens[b]; max_ctx + 1 beyond columns * page is LS_ERR_KV_OVERFLOW, and beyond max_seq too where
+ *            rope is given and positions are not.  Without weights an understated bound costs speed, never slots; with
+ *            weights a sequence of more slots counts as one without room.
+ *   scratch  16-byte aligned; with weights less than ls_paged_attention_scratch_bytes is LS_ERR_OOM, without, less or NULL costs speed.
+ * Slots whose page the table does not name are not there: nobody attends to them.  A sequence without room (lens[b] negative, or beyond the
+ * table, slot lens[b] without a page, or a position that is negative or that rope does not have) keeps its cache, and its output row is zeros.  Pages may be shared
+ * by sequences (a common prompt) as long as no slot lens[b] lies in them and there are no weights: rows of one slot that several sequences
+ * write, or weights that they add to, are not ordered.  Scores, softmax, sums and weights are fp32; products as in ls_tree_attention.
+ */
+ls_status ls_paged_attention(const ls_heads* heads, const ls_pages* layer, int batch, int max_ctx, const void* qkv, const float* rope,
+                             void* out, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/*
+ * A prompt's cache into pages: in all layers, positions 0..n-1 of sequence src[b] of `from`, n = from->seq_lens[src[b]], become the slots
+ * 0..n-1 of sequence b, and lens[b] and positions[b] become n.
+ *   from      cache as ls_stage_prefill writes it, k, v [layers][from_batch][n_kv_heads][from_seq][head_dim]
+ *   src       int32 [batch]; a sequence whose entry lies outside [0, from_batch) is left alone, as is one whose n lies outside
+ *             [0, min(from_seq, columns * page)]
+ *   weights   optional fp32 [layers][from_batch][n_kv_heads][from_seq]: what the slots' weights become (where the pools have them); NULL:
+ *             zeros.  Places are the positions.
+ *   max_len   host-side upper bound of n; an understated one costs speed, never positions
+ * Slots without a page are left out.  Caches on 4 bytes for bf16 too.
+ */
+ls_status ls_paged_fill(const ls_heads* heads, int layers, const ls_kv* from, int from_batch, int from_seq, const int32_t* src, const float* weights,
+                        int max_len, const ls_pages* pages, int batch, void* hip_stream);
+
+/*
+ * Cut sequences down to `keep` slots: of a sequence with more, each layer's each kv head keeps the slots of tokens at positions below `first` or
+ * from positions[b] - recent on, and of the others those of the largest weights; equal ones go by the lower slot, and a weight that
+ * is no number is below all others.  (Where more than `keep` slots are of such positions, the lowest slots of them.)  Kept slots below `keep` stay
+ * where they are; the kept ones behind, in order, go to the slots below `keep` that are not kept, in order: key, value, weight and
+ * place.  lens[b] becomes keep; what lies behind is left as it is, so pages behind slot keep - 1 are the caller's again.
+ *   pages    with weights and places; all layers.  positions NULL: lens, as far as nothing has been evicted.
+ *   keep     at least 1;  first, recent: at least 0, first + recent at most keep
+ *   max_len  host-side upper bound of lens[b]; a sequence with more is left alone
+ *   scratch  of ls_paged_evict_scratch_bytes (0: invalid sizes), 16-byte aligned; nothing in it outlasts the call
+ * A sequence with a page below lens[b] that the table does not name is left alone.  Pages of a sequence that is cut down are its own.
+ */
+size_t ls_paged_evict_scratch_bytes(const ls_heads* heads, int layers, int batch, int keep, int max_len);
+ls_status ls_paged_evict(const ls_heads* heads, int layers, const ls_pages* pages, int batch, int keep, int first, int recent, int max_len,
+                         void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/*
+ * The stage's generation step over a cache in pages: ls_stage_decode whose attention is ls_paged_attention in every layer, the pools those
+ * of all of the stage's layers.  lens[b] and positions[b] of sequences with room grow by one behind the last layer.  max_seq of the stage is the
+ * positions that tokens may have.  Rows of sequences without room are computed from zeros as attention; nobody else's depend on them.
+ * max_ctx and scratch as in ls_paged_attention (the query with the stage's heads), the rest as in ls_stage_decode.  The probe does not see it.
+ */
+ls_status ls_stage_paged(ls_stage* stage, const void* in, int batch, int max_ctx, const ls_pages* pages, void* out, float* logits_out,
+                         void* scratch, size_t scratch_bytes, void* hip_stream);
+
 /* ---- measurement ---------------------------------------------------------------------*/
 
 /* With profiling on, ls_stage_load_block brackets each copy and ls_stage_prefill brackets

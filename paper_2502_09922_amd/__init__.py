@@ -6,7 +6,7 @@ imported on first use, so that `python -m paper_2502_09922_amd.build` can run be
 library exists; a missing library is an ImportError, never a fallback.
 """
 _LAZY = ("binding", "Stage", "Pipeline", "MicroBatch", "LsError", "ls_cfg", "ls_kv", "ls_microbatch", "make_cfg", "pack_block",
-         "tree_attention", "tree_accept", "tree_keep", "beam_select", "kv_reorder")
+         "tree_attention", "tree_accept", "tree_keep", "beam_select", "kv_reorder", "PagedCache", "paged_attention", "paged_fill", "paged_evict")
 
 
 def __getattr__(name):

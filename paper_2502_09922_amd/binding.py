@@ -61,6 +61,11 @@ class ls_tree(C.Structure):
     _fields_ = [("parents", C.c_void_p), ("cu_nodes", C.c_void_p), ("cu_nodes_host", C.c_void_p)]
 
 
+class ls_pages(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "weights", "places", "lens", "positions", "table")] + [
+        (n, C.c_uint32) for n in ("pages", "page", "columns")]
+
+
 class ls_microbatch(C.Structure):
     _fields_ = [
         ("in_", C.c_void_p), ("cu_seqlens_dev", C.c_void_p), ("cu_seqlens_host", C.POINTER(C.c_int32)),
@@ -122,6 +127,12 @@ _SIGS = {
     "ls_beam_select_scratch_bytes": (C.c_size_t, [C.c_int] * 4),
     "ls_beam_select": (C.c_int, [_P, _P, _P] + [C.c_int] * 5 + [_P, _P, _P, _P, C.c_size_t, _P]),
     "ls_kv_reorder": (C.c_int, [C.POINTER(ls_heads), C.c_int, _P, C.c_int, C.c_int, _P, C.c_int, C.POINTER(ls_kv), _P]),
+    "ls_paged_attention_scratch_bytes": (C.c_size_t, [C.POINTER(ls_heads), C.POINTER(ls_pages), C.c_int, C.c_int]),
+    "ls_paged_attention": (C.c_int, [C.POINTER(ls_heads), C.POINTER(ls_pages), C.c_int, C.c_int, _P, _P, _P, _P, C.c_size_t, _P]),
+    "ls_paged_fill": (C.c_int, [C.POINTER(ls_heads), C.c_int, C.POINTER(ls_kv), C.c_int, C.c_int, _P, _P, C.c_int, C.POINTER(ls_pages), C.c_int, _P]),
+    "ls_paged_evict_scratch_bytes": (C.c_size_t, [C.POINTER(ls_heads)] + [C.c_int] * 4),
+    "ls_paged_evict": (C.c_int, [C.POINTER(ls_heads), C.c_int, C.POINTER(ls_pages)] + [C.c_int] * 5 + [_P, C.c_size_t, _P]),
+    "ls_stage_paged": (C.c_int, [_P, _P, C.c_int, C.c_int, C.POINTER(ls_pages), _P, _P, _P, C.c_size_t, _P]),
     "ls_last_error": (C.c_char_p, []),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -303,6 +314,110 @@ def kv_reorder(src, group: int, k, v, seq_lens, max_ctx: int, first=None):
          None if first is None else _tensor("first", first, torch.int32, device, src.numel()), max_ctx, C.byref(kv))
 
 
+# ---- a cache in pages: include/ls_stage.h says what each call does -------------------------------------------------------------
+class PagedCache:
+    """Tensors of a cache in pages (ls_pages), checked once.  k, v [layers, pages, n_kv_heads, page, head_dim], float32 or bfloat16;
+    table [sequences, columns], lens and positions [sequences] int32; weights (float32) and places (int32) [layers, pages, n_kv_heads,
+    page], both or none.  positions None: nothing is ever evicted.  The tensors are the caller's, who fills table and may write
+    the others between calls; the attributes stay the tensors that were given."""
+
+    __slots__ = ("_t", "_layers", "_all", "_heads", "device", "batch")
+
+    def __init__(self, k, v, table, lens, positions=None, weights=None, places=None):
+        device = _gpu(k)
+        if k.dim() != 5 or k.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("k: a float32 or bfloat16 cache [layers, pages, n_kv_heads, page, head_dim] is wanted")
+        if v.shape != k.shape:
+            raise ValueError("v: the shape of k is wanted")
+        if table.dim() != 2 or lens.dim() != 1 or lens.numel() != table.shape[0]:
+            raise ValueError("table [sequences, columns] and lens [sequences] are wanted")
+        if (weights is None) != (places is None):
+            raise ValueError("weights and places come together")
+        layers, pages, hkv, page, hd = k.shape
+        at = [_tensor("k", k, k.dtype, device), _tensor("v", v, k.dtype, device)]
+        for name, t, dtype in (("weights", weights, torch.float32), ("places", places, torch.int32)):
+            if t is not None and t.shape != k.shape[:4]:
+                raise ValueError("%s: [layers, pages, n_kv_heads, page] of k is wanted" % name)
+            at.append(None if t is None else _tensor(name, t, dtype, device))
+        at.append(_tensor("lens", lens, torch.int32, device))
+        at.append(None if positions is None else _tensor("positions", positions, torch.int32, device, lens.numel()))
+        at.append(_tensor("table", table, torch.int32, device))
+        slots = pages * hkv * page
+        rows = (slots * hd * k.element_size(),) * 2 + (slots * 4,) * 2
+        # one for each layer, and for all
+        self._layers = [ls_pages(*[p if p is None or i > 3 else p + n * rows[i] for i, p in enumerate(at)], pages, page, table.shape[1]) for n in range(layers)]
+        self._all = ls_pages(*at, pages, page, table.shape[1])
+        self._t = dict(k=k, v=v, table=table, lens=lens, positions=positions, weights=weights, places=places)
+        self._heads, self.device, self.batch = {}, device, table.shape[0]
+
+    def __getattr__(self, name):
+        try:
+            return object.__getattribute__(self, "_t")[name]
+        except KeyError:
+            raise AttributeError(name) from None
+
+    def heads(self, n_q_heads: int, max_seq: int) -> ls_heads:
+        """ls_heads of a call with these pools."""
+        h = self._heads.get((n_q_heads, max_seq))
+        if h is None:
+            k = self._t["k"]
+            h = ls_heads(LS_DTYPE_F32 if k.dtype == torch.float32 else LS_DTYPE_BF16, n_q_heads, k.shape[2], k.shape[4], self.batch, max_seq)
+            self._heads[(n_q_heads, max_seq)] = h
+        return h
+
+
+def _scratch(nb, device):
+    return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+
+
+def paged_attention(cache: PagedCache, qkv, rope, max_ctx: int, layer: int = 0, out=None):
+    """Attention of one layer for a new token of each sequence (ls_paged_attention), which takes slot lens[b] of the cache; qkv [sequences,
+    (n_q_heads + 2 n_kv_heads) * head_dim]; rope: float32 [positions, head_dim/2, 2] or None; max_ctx: a bound of lens.  lens and
+    positions stay: add one to both behind the last layer.  Returns [sequences, n_q_heads * head_dim]."""
+    device, k = cache.device, cache._t["k"]
+    hkv, hd, rows = k.shape[2], k.shape[4], cache.batch
+    if qkv.dim() != 2 or qkv.shape[0] != rows or qkv.shape[1] % hd or qkv.shape[1] // hd <= 2 * hkv:
+        raise ValueError("qkv: [%d, (n_q_heads + %d) * %d] is wanted" % (rows, 2 * hkv, hd))
+    if not 0 <= layer < k.shape[0]:
+        raise ValueError("layer: one of %d is wanted" % k.shape[0])
+    hq = qkv.shape[1] // hd - 2 * hkv
+    heads, pages = cache.heads(hq, 1 << 24 if rope is None else rope.shape[0]), cache._layers[layer]
+    q = _tensor("qkv", qkv, k.dtype, device)
+    turn = None if rope is None else _tensor("rope", rope, torch.float32, device, rope.shape[0] * hd)
+    if out is None:
+        out = torch.empty(rows, hq * hd, dtype=k.dtype, device=device)
+    to = _tensor("out", out, k.dtype, device, rows * hq * hd)
+    nb = lib.ls_paged_attention_scratch_bytes(heads, pages, rows, max_ctx)
+    scratch = _scratch(nb, device)
+    _run(device, lib.ls_paged_attention, heads, pages, rows, max_ctx, q, turn, to, scratch.data_ptr() if nb else None, nb)
+    return out
+
+
+def paged_fill(cache: PagedCache, k, v, seq_lens, src, max_len: int, weights=None):
+    """A prompt pass's cache into pages (ls_paged_fill): sequence b of `cache` gets that of sequence src[b] (int32, on the GPU) of k and v [layers,
+    max_batch, n_kv_heads, max_seq, head_dim] with seq_lens (Stage.caches() and Stage.seq_lens); weights: float32 [layers, max_batch,
+    n_kv_heads, max_seq] or None, for zeros; max_len: a bound of the lengths."""
+    device, to = cache.device, cache._t["k"]
+    _, kv = _cache(k, v, seq_lens, 5)
+    if k.dtype != to.dtype or (k.shape[0], k.shape[2], k.shape[4]) != (to.shape[0], to.shape[2], to.shape[4]) or k.device != device:
+        raise ValueError("k: a cache of the pools' type, layers, heads and device is wanted")
+    if weights is not None and (cache._t["weights"] is None or weights.shape != k.shape[:4]):
+        raise ValueError("weights: [layers, max_batch, n_kv_heads, max_seq] of k is wanted, and a cache that has some")
+    w = None if weights is None else _tensor("weights", weights, torch.float32, device)
+    _run(device, lib.ls_paged_fill, cache.heads(k.shape[2], 1 << 24), k.shape[0], kv, k.shape[1], k.shape[3],
+         _tensor("src", src, torch.int32, device, cache.batch), w, max_len, cache._all, cache.batch)
+
+
+def paged_evict(cache: PagedCache, keep: int, recent: int, max_len: int, first: int = 0):
+    """Cut sequences down to `keep` slots (ls_paged_evict): the first `first` positions and the newest `recent` stay, and of the others those
+    of the largest weights; max_len: a bound of lens."""
+    device = cache.device
+    heads, layers = cache.heads(cache._t["k"].shape[2], 1 << 24), cache._t["k"].shape[0]
+    nb = lib.ls_paged_evict_scratch_bytes(heads, layers, cache.batch, keep, max_len)
+    scratch = _scratch(nb, device)
+    _run(device, lib.ls_paged_evict, heads, layers, cache._all, cache.batch, keep, first, recent, max_len, scratch.data_ptr() if nb else None, nb)
+
+
 class Stage:
     """One ls_stage plus the device buffers it needs, allocated with PyTorch."""
 
@@ -450,6 +565,33 @@ class Stage:
                 return self.tree(inp, parents, cu_nodes, cu_nodes_host, max_ctx, stream, want_logits)
         tree, batch, rows, host = _trees(parents, cu_nodes, cu_nodes_host, device)
         x = _tensor("inp", inp, torch.int32 if self.first else self.tdtype, device, rows if self.first else rows * self.shape.hidden)
+        return self._rows_pass(rows, (inp, parents, cu_nodes), stream, want_logits, lambda out, logits, st: lib.ls_stage_tree(
+            self.handle, x, C.byref(tree), batch, max_ctx, C.byref(self.kv), out, logits, st))
+
+    def paged(self, inp, cache: PagedCache, max_ctx: int, stream=None, want_logits=False):
+        """ls_stage_paged: a generation step of the cache's sequences (a row each; the pools of all of the stage's layers).  inp is on the
+        stage's device; max_ctx: a bound of the cache's lens, which grow by one.  Streams as for tree."""
+        torch, device = self.torch, self.slab.device
+        if torch.cuda.current_device() != device.index:
+            with torch.cuda.device(device):
+                return self.paged(inp, cache, max_ctx, stream, want_logits)
+        k, rows = cache.k, cache.batch
+        if (k.dtype != self.tdtype or k.device != device or
+                (k.shape[0], k.shape[2], k.shape[4]) != (self.hi - self.lo, self.cfg.n_kv_heads, self.cfg.head_dim)):
+            raise ValueError("cache: pools of the stage's type, layers, heads and device are wanted")
+        x = _tensor("inp", inp, torch.int32 if self.first else self.tdtype, device, rows if self.first else rows * self.shape.hidden)
+        heads = cache.heads(self.cfg.n_q_heads, self.cfg.max_seq)
+        nb = lib.ls_paged_attention_scratch_bytes(heads, cache._all, rows, max_ctx)
+
+        def call(out, logits, st):
+            scratch = _scratch(nb, device)
+            return lib.ls_stage_paged(self.handle, x, rows, max_ctx, cache._all, out, logits, scratch.data_ptr() if nb else None, nb, st)
+        return self._rows_pass(rows, (inp, *[t for t in cache._t.values() if t is not None]), stream, want_logits, call)
+
+    def _rows_pass(self, rows, tensors, stream, want_logits, call):
+        """A pass that says something for each of its rows: call(out, logits, stream), behind the null stream and in front of its later
+        work where the stream is torch's current one; `tensors` are what it reads or writes."""
+        torch, device = self.torch, self.slab.device
         null, current = None, _current_stream(device.index)
         if stream is None and current:
             stream = torch.cuda.current_stream(device)
@@ -457,14 +599,13 @@ class Stage:
                 null = torch.cuda.default_stream(device)
                 stream.wait_stream(null)
         elif stream is not None and stream.cuda_stream != current:  # the pass may outlive the caller's hold on them
-            for t in (inp, parents, cu_nodes):
+            for t in tensors:
                 t.record_stream(stream)
-        with torch.cuda.stream(stream):  # outputs belong to the stream that writes them
+        with torch.cuda.stream(stream):  # outputs and scratch belong to the stream that writes them
             out = (torch.empty(rows, dtype=torch.int32, device=device) if self.last
                    else torch.empty(rows, self.shape.hidden, dtype=self.tdtype, device=device))
             logits = torch.empty(rows, self.shape.vocab, dtype=torch.float32, device=device) if (want_logits and self.last) else None
-        check(lib.ls_stage_tree(self.handle, x, C.byref(tree), batch, max_ctx, C.byref(self.kv), out.data_ptr(),
-                                logits.data_ptr() if logits is not None else None, self._stream_ptr(stream)))
+            check(call(out.data_ptr(), logits.data_ptr() if logits is not None else None, self._stream_ptr(stream)))
         if null is not None:
             null.wait_stream(stream)
         return (out, logits) if want_logits else out

@@ -1,0 +1,383 @@
+// A cache in pages: the entry points of include/ls_stage.h, the filling of pages from a prompt pass's cache and the eviction of slots.
+#include "entry.hpp"
+#include "paged.hpp"
+
+#include <algorithm>
+
+namespace ls {
+
+namespace {
+
+// ---- filling -----------------------------------------------------------------------------------------------------------------
+struct FillArgs {
+  PageMap map;
+  const int32_t *src, *from_lens;
+  int batch, from_batch, from_seq, hkv, heads, pieces, slots;  // heads: layer * hkv + kv head; pieces of a row
+};
+
+__device__ __forceinline__ int fill_len(const FillArgs& a, int b, int& src) {
+  src = a.src[b];
+  if ((unsigned)src >= (unsigned)a.from_batch) return -1;
+  const int n = a.from_lens[src];
+  return n <= a.from_seq && n <= a.slots ? n : -1;
+}
+
+// A workgroup to 64 slots of a (sequence, layer, kv head), a thread to a U-sized piece of a row.
+template <class U>
+__global__ void __launch_bounds__(256)
+k_paged_fill(FillArgs a, const U* __restrict__ fk, const U* __restrict__ fv, const float* __restrict__ fw, U* __restrict__ kc, U* __restrict__ vc,
+             float* __restrict__ weights, int32_t* __restrict__ places, int blocks) {
+  const int b = blockIdx.y, head = blockIdx.x / blocks, block = blockIdx.x % blocks, layer = head / a.hkv, kh = head % a.hkv;
+  int src;
+  const int n = fill_len(a, b, src);
+  const int lo = block * 64, hi = block == blocks - 1 ? n : min(lo + 64, n);  // the last one takes what is left
+  const size_t from = (((size_t)layer * a.from_batch + src) * a.hkv + kh) * a.from_seq;
+  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
+  auto row_of = [&](int slot, size_t& row) {
+    const int page = entries[slot >> a.map.shift];
+    row = page_row0((int)0, a.hkv, kh, a.map.shift) + (((size_t)layer * a.map.pages + page) * a.hkv << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
+    return (unsigned)page < (unsigned)a.map.pages;
+  };
+  for (int64_t i = threadIdx.x; i < (int64_t)(hi - lo) * a.pieces; i += 256) {
+    const int slot = lo + (int)(i / a.pieces), piece = (int)(i % a.pieces);
+    size_t row;
+    if (!row_of(slot, row)) continue;
+    const size_t at = (from + slot) * a.pieces + piece;
+    const U k = fk[at], v = fv[at];
+    kc[row * a.pieces + piece] = k;
+    vc[row * a.pieces + piece] = v;
+  }
+  if (!weights) return;
+  for (int slot = lo + threadIdx.x; slot < hi; slot += 256) {
+    size_t row;
+    if (!row_of(slot, row)) continue;
+    weights[row] = fw ? fw[from + slot] : 0.f;
+    places[row] = slot;
+  }
+}
+
+__global__ void __launch_bounds__(256) k_paged_fill_lens(FillArgs a, int32_t* lens, int32_t* positions) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= a.batch) return;
+  int src;
+  const int n = fill_len(a, b, src);
+  if (n < 0) return;
+  lens[b] = n;
+  if (positions) positions[b] = n;
+}
+
+// ---- eviction ----------------------------------------------------------------------------------------------------------------
+struct EvictArgs {
+  PageMap map;
+  int batch, hkv, layers, keep, first, recent, max_len, most;  // most: moves of a (layer, sequence, kv head)
+  const float* weights;
+  const int32_t* places;
+  int32_t* count;  // [units] moves, -1 for a sequence that is left alone
+  int2* moves;     // [units][most]: to slot x from slot y
+};
+
+// Greater keys stay.  A weight that is no number has 0, equal weights equal keys.
+__device__ __forceinline__ unsigned stay_key(float w, int place, int first, int from) {
+  if (place < first || place >= from) return 0xFFFFFFFFu;
+  const unsigned bits = __builtin_bit_cast(unsigned, w + 0.f);  // -0 is 0
+  return w != w ? 0u : bits ^ (bits >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+
+__device__ __forceinline__ size_t slot_row(const EvictArgs& a, const int32_t* entries, int layer, int kh, int slot) {
+  return page_row0(0, a.hkv, kh, a.map.shift) + (((size_t)layer * a.map.pages + entries[slot >> a.map.shift]) * a.hkv << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
+}
+
+// Which slots of a (layer, sequence, kv head) move where.  The key of which `keep` or more slots have as much is searched for bit by bit: as many
+// rounds of counting as it takes until one has exactly `keep`, or all 32.
+__global__ void __launch_bounds__(256) k_evict_choose(EvictArgs a) {
+  const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
+  const int n = a.map.lens[b], pos = a.map.positions ? a.map.positions[b] : n;
+  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
+  __shared__ int sums[4], bad;
+  if (threadIdx.x == 0) bad = n <= a.keep || n > a.max_len || (n - 1) >> a.map.shift >= a.map.columns;
+  __syncthreads();
+  if (!bad)
+    for (int i = threadIdx.x; i <= (n - 1) >> a.map.shift; i += 256)
+      if ((unsigned)entries[i] >= (unsigned)a.map.pages) bad = 1;
+  __syncthreads();
+  if (bad) {
+    if (threadIdx.x == 0) a.count[unit] = -1;
+    return;
+  }
+  const int from = pos < a.recent ? 0 : pos - a.recent;
+  auto key_of = [&](int slot) {
+    const size_t row = slot_row(a, entries, layer, kh, slot);
+    return stay_key(a.weights[row], a.places[row], a.first, from);
+  };
+  auto total = [&](int mine) {  // over the workgroup
+    for (int off = 32; off; off >>= 1) mine += __shfl_xor(mine, off);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    return sums[0] + sums[1] + sums[2] + sums[3];
+  };
+  unsigned key = 0;
+  int reach = n;
+  for (int bit = 31; bit >= 0 && reach != a.keep; --bit) {
+    const unsigned higher = key | 1u << bit;
+    int mine = 0;
+    for (int slot = threadIdx.x; slot < n; slot += 256) mine += key_of(slot) >= higher;
+    const int got = total(mine);
+    if (got >= a.keep) {
+      key = higher;
+      reach = got;
+    }
+  }
+  int above = a.keep;  // slots whose key is above `key`; of those at it as many stay as are wanted yet
+  if (reach != a.keep) {
+    int mine = 0;
+    for (int slot = threadIdx.x; slot < n; slot += 256) mine += key_of(slot) > key;
+    above = total(mine);
+  }
+  const bool ties = reach != a.keep;
+  int equal0 = 0, to0 = 0, from0 = 0;  // of the slots before
+  __shared__ int pre[4][3];
+  int2* moves = a.moves + (size_t)unit * a.most;
+  for (int slot0 = 0; slot0 < n; slot0 += 256) {
+    const int slot = slot0 + threadIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const unsigned mine = slot < n ? key_of(slot) : 0;
+    const uint64_t below = (1ull << lane) - 1;
+    const uint64_t eq = __ballot(slot < n && ties && mine == key);
+    __syncthreads();
+    if (lane == 0) pre[wave][0] = __popcll(eq);
+    __syncthreads();
+    int rank = equal0 + __popcll(eq & below);
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) rank += pre[w][0];
+      equal0 += pre[w][0];
+    }
+    const bool kept = slot < n && (ties ? mine > key || (mine == key && rank < a.keep - above) : mine >= key);
+    const bool hole = slot < a.keep && !kept, mover = slot < n && slot >= a.keep && kept;
+    const uint64_t holes = __ballot(hole), movers = __ballot(mover);
+    if (lane == 0) {
+      pre[wave][1] = __popcll(holes);
+      pre[wave][2] = __popcll(movers);
+    }
+    __syncthreads();
+    int to = to0 + __popcll(holes & below), fr = from0 + __popcll(movers & below);
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) {
+        to += pre[w][1];
+        fr += pre[w][2];
+      }
+      to0 += pre[w][1];
+      from0 += pre[w][2];
+    }
+    if (hole) moves[to].x = slot;
+    if (mover) moves[fr].y = slot;
+  }
+  if (threadIdx.x == 0) a.count[unit] = from0;
+}
+
+// The moves: a thread to a U-sized piece of a row.  The lengths, which the launch before reads, are set by one workgroup of a sequence.
+template <class U>
+__global__ void __launch_bounds__(256)
+k_evict_move(EvictArgs a, U* __restrict__ kc, U* __restrict__ vc, float* __restrict__ weights, int32_t* __restrict__ places, int32_t* __restrict__ lens, int pieces) {
+  const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
+  const int count = a.count[unit];
+  if (count < 0) return;
+  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
+  if (layer == 0 && kh == 0 && blockIdx.y == 0 && threadIdx.x == 0) lens[b] = a.keep;
+  const int2* moves = a.moves + (size_t)unit * a.most;
+  for (int64_t i = blockIdx.y * 256 + threadIdx.x; i < (int64_t)count * pieces; i += gridDim.y * 256) {
+    const int2 m = moves[i / pieces];
+    const int piece = (int)(i % pieces);
+    const size_t to = slot_row(a, entries, layer, kh, m.x), fr = slot_row(a, entries, layer, kh, m.y);
+    const U k = kc[fr * pieces + piece], v = vc[fr * pieces + piece];
+    kc[to * pieces + piece] = k;
+    vc[to * pieces + piece] = v;
+    if (piece == 0) {
+      weights[to] = weights[fr];
+      places[to] = places[fr];
+    }
+  }
+}
+
+// ---- arguments ---------------------------------------------------------------------------------------------------------------
+const char* pages_error(const ls_heads* h, const ls_pages* p, int batch) {
+  if (!p || !p->k || !p->v || !p->lens || !p->table) return "NULL ls_pages or pointer inside it";
+  if (p->page < 8 || p->page > 1024 || (p->page & (p->page - 1))) return "page has to be a power of two from 8 to 1024";
+  if (!p->pages || p->pages > (1u << 24)) return "pages outside [1, 2^24]";
+  if (!p->columns || (uint64_t)p->columns * p->page > (1u << 24)) return "columns * page outside [1, 2^24]";
+  if (!p->weights != !p->places) return "weights and places come together";
+  if (batch < 1 || batch > (int)h->max_batch || batch > 65535) return "batch outside [1, max_batch], or beyond 65535";
+  const uintptr_t size = h->dtype == LS_DTYPE_F32 ? 4 : 2;
+  if (((uintptr_t)p->k | (uintptr_t)p->v) & (size - 1)) return "a pool is not aligned to its type";
+  if (((uintptr_t)p->weights | (uintptr_t)p->places | (uintptr_t)p->lens | (uintptr_t)p->positions | (uintptr_t)p->table) & 3) return "a buffer is not aligned to its type";
+  return nullptr;
+}
+
+PageMap map_of(const ls_pages* p) {
+  PageMap m;
+  m.lens = p->lens; m.positions = p->positions; m.table = p->table;
+  m.pages = (int)p->pages; m.columns = (int)p->columns;
+  while ((1u << m.shift) < p->page) ++m.shift;
+  return m;
+}
+
+PagedAttn attn_of(const ls_heads* h, const ls_pages* p, int batch, int max_ctx) {
+  PagedAttn a;
+  a.map = map_of(p);
+  a.kc = p->k; a.vc = p->v; a.weights = p->weights; a.places = p->places;
+  a.batch = batch; a.hq = (int)h->n_q_heads; a.hkv = (int)h->n_kv_heads; a.hd = (int)h->head_dim; a.max_pos = (int)h->max_seq;
+  a.max_keys = max_ctx + 1;
+  return a;
+}
+
+// The checks of an attention call that its sizing query shares; its bounds are in reach of LS_ERR_KV_OVERFLOW.
+ls_status context_error(const char* who, const ls_heads* h, const ls_pages* p, int max_ctx, bool turns) {
+  if (max_ctx < 0) return bad(who, "max_ctx is negative");
+  if ((uint64_t)max_ctx + 1 > (uint64_t)p->columns * p->page) {
+    set_last_error("%s: context %d + 1 exceeds the table's %u pages of %u", who, max_ctx, p->columns, p->page);
+    return LS_ERR_KV_OVERFLOW;
+  }
+  if (turns && !p->positions && (uint64_t)max_ctx + 1 > h->max_seq) {
+    set_last_error("%s: context %d + 1 exceeds max_seq %u", who, max_ctx, h->max_seq);
+    return LS_ERR_KV_OVERFLOW;
+  }
+  return LS_OK;
+}
+
+}  // namespace
+
+ls_status paged_attention_args(const char* who, const ls_heads* h, const ls_pages* p, int batch, int max_ctx, bool turns, void* scratch, size_t scratch_bytes,
+                               PagedAttn* a) {
+  if (const char* e = heads_error(h)) return bad(who, e);
+  if (const char* e = pages_error(h, p, batch)) return bad(who, e);
+  const ls_status rc = context_error(who, h, p, max_ctx, turns);
+  if (rc != LS_OK) return rc;
+  *a = attn_of(h, p, batch, max_ctx);
+  if (a->weights) {
+    const size_t need = paged_attn_scratch_bytes(*a);
+    if (!scratch || scratch_bytes < need) {
+      set_last_error("%s: %zu bytes of scratch, %zu are needed", who, scratch ? scratch_bytes : 0, need);
+      return LS_ERR_OOM;
+    }
+    if ((uintptr_t)scratch & 15) return bad(who, "scratch is not aligned to 16 bytes");
+  }
+  a->scratch = ((uintptr_t)scratch & 15) ? nullptr : (float*)scratch;
+  a->scratch_bytes = scratch_bytes;
+  return LS_OK;
+}
+
+}  // namespace ls
+
+namespace {
+
+using ls::bad;
+using ls::launched;
+
+size_t evict_units(const ls_heads* h, int layers, int batch) { return (size_t)layers * batch * h->n_kv_heads; }
+
+const char* evict_error(const ls_heads* h, int layers, int batch, int keep, int max_len) {
+  if (const char* e = ls::heads_error(h)) return e;
+  if (batch < 1 || batch > (int)h->max_batch || batch > 65535) return "batch outside [1, max_batch], or beyond 65535";
+  if (layers < 1 || layers > (1 << 20) || evict_units(h, layers, batch) >= (1u << 24)) return "layers outside [1, what a launch takes]";
+  if (keep < 1) return "keep has to be at least 1";
+  if (max_len < 0 || max_len > (1 << 24)) return "max_len outside [0, 2^24]";
+  return nullptr;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ls_paged_attention_scratch_bytes(const ls_heads* h, const ls_pages* layer, int batch, int max_ctx) {
+  if (ls::heads_error(h) || ls::pages_error(h, layer, batch) || max_ctx < 0 || (uint64_t)max_ctx + 1 > (uint64_t)layer->columns * layer->page) return 0;
+  return ls::paged_attn_scratch_bytes(ls::attn_of(h, layer, batch, max_ctx));
+}
+
+ls_status ls_paged_attention(const ls_heads* h, const ls_pages* layer, int batch, int max_ctx, const void* qkv, const float* rope, void* out, void* scratch,
+                             size_t scratch_bytes, void* hip_stream) {
+  static const char* who = "ls_paged_attention";
+  ls::PagedAttn a;
+  const ls_status rc = ls::paged_attention_args(who, h, layer, batch, max_ctx, rope != nullptr, scratch, scratch_bytes, &a);
+  if (rc != LS_OK) return rc;
+  if (!qkv || !out) return bad(who, "NULL argument");
+  const uintptr_t size = h->dtype == LS_DTYPE_F32 ? 4 : 2;
+  if (((uintptr_t)qkv | (uintptr_t)out) & (size - 1)) return bad(who, "a buffer is not aligned to its type");
+  if ((uintptr_t)rope & 7) return bad(who, "rope is not aligned to 8 bytes");
+  a.qkv = qkv; a.cs = rope; a.out = out;
+  ls::launch_paged_attn(h->dtype, a, (hipStream_t)hip_stream);
+  return launched(who);
+}
+
+ls_status ls_paged_fill(const ls_heads* h, int layers, const ls_kv* from, int from_batch, int from_seq, const int32_t* src, const float* weights, int max_len,
+                        const ls_pages* pages, int batch, void* hip_stream) {
+  static const char* who = "ls_paged_fill";
+  if (const char* e = ls::heads_error(h)) return bad(who, e);
+  if (const char* e = ls::pages_error(h, pages, batch)) return bad(who, e);
+  if (!from || !from->k || !from->v || !from->seq_lens || !src) return bad(who, "NULL argument");
+  if (from_batch < 1 || from_batch >= (1 << 24) || from_seq < 1 || from_seq > (1 << 24)) return bad(who, "from_batch outside [1, 2^24) or from_seq outside [1, 2^24]");
+  const uintptr_t at = (uintptr_t)from->k | (uintptr_t)from->v | (uintptr_t)pages->k | (uintptr_t)pages->v;
+  if (at & 3) return bad(who, "a cache is not aligned to 4 bytes");
+  if (((uintptr_t)src | (uintptr_t)from->seq_lens | (uintptr_t)weights) & 3) return bad(who, "a buffer is not aligned to its type");
+  if (max_len < 0) return bad(who, "max_len is negative");
+  const size_t row = (size_t)h->head_dim * (h->dtype == LS_DTYPE_F32 ? 4 : 2);
+  const bool wide = row % 16 == 0 && (at & 15) == 0;
+  ls::FillArgs a;
+  a.map = ls::map_of(pages);
+  a.src = src; a.from_lens = from->seq_lens; a.batch = batch; a.from_batch = from_batch; a.from_seq = from_seq;
+  a.hkv = (int)h->n_kv_heads; a.pieces = (int)(row / (wide ? 16 : 4)); a.slots = (int)(pages->columns * pages->page);
+  const int most = std::max(1, std::min({max_len, from_seq, a.slots})), blocks = (most + 63) / 64;
+  if (layers < 1 || (uint64_t)layers * h->n_kv_heads * blocks >= (1u << 24)) return bad(who, "layers outside [1, what a launch takes]");
+  a.heads = layers * a.hkv;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const dim3 grid(a.heads * blocks, batch);
+  if (wide)
+    ls::k_paged_fill<ls::u32x4><<<grid, 256, 0, st>>>(a, (const ls::u32x4*)from->k, (const ls::u32x4*)from->v, weights, (ls::u32x4*)pages->k, (ls::u32x4*)pages->v,
+                                                  pages->weights, pages->places, blocks);
+  else
+    ls::k_paged_fill<uint32_t><<<grid, 256, 0, st>>>(a, (const uint32_t*)from->k, (const uint32_t*)from->v, weights, (uint32_t*)pages->k, (uint32_t*)pages->v,
+                                                     pages->weights, pages->places, blocks);
+  ls::k_paged_fill_lens<<<(batch + 255) / 256, 256, 0, st>>>(a, pages->lens, pages->positions);
+  return launched(who);
+}
+
+size_t ls_paged_evict_scratch_bytes(const ls_heads* h, int layers, int batch, int keep, int max_len) {
+  if (evict_error(h, layers, batch, keep, max_len)) return 0;
+  const size_t units = evict_units(h, layers, batch), most = std::max(0, std::min(keep, max_len - keep));
+  return (units * 4 + 15) / 16 * 16 + std::max(units * most * sizeof(int2), (size_t)16);
+}
+
+ls_status ls_paged_evict(const ls_heads* h, int layers, const ls_pages* pages, int batch, int keep, int first, int recent, int max_len, void* scratch,
+                         size_t scratch_bytes, void* hip_stream) {
+  static const char* who = "ls_paged_evict";
+  if (const char* e = evict_error(h, layers, batch, keep, max_len)) return bad(who, e);
+  if (const char* e = ls::pages_error(h, pages, batch)) return bad(who, e);
+  if (!pages->weights) return bad(who, "pages without weights and places");
+  if (first < 0 || recent < 0 || (int64_t)first + recent > keep) return bad(who, "first and recent are at least 0 and together at most keep");
+  const uintptr_t at = (uintptr_t)pages->k | (uintptr_t)pages->v;
+  if (at & 3) return bad(who, "a pool is not aligned to 4 bytes");
+  if (!scratch || scratch_bytes < ls_paged_evict_scratch_bytes(h, layers, batch, keep, max_len)) {
+    ls::set_last_error("%s: scratch is smaller than ls_paged_evict_scratch_bytes says", who);
+    return LS_ERR_OOM;
+  }
+  if ((uintptr_t)scratch & 15) return bad(who, "scratch is not aligned to 16 bytes");
+  if (max_len <= keep) return LS_OK;  // no sequence has more
+  const size_t row = (size_t)h->head_dim * (h->dtype == LS_DTYPE_F32 ? 4 : 2), units = evict_units(h, layers, batch);
+  const bool wide = row % 16 == 0 && (at & 15) == 0;
+  const int pieces = (int)(row / (wide ? 16 : 4));
+  ls::EvictArgs a;
+  a.map = ls::map_of(pages);
+  a.batch = batch; a.hkv = (int)h->n_kv_heads; a.layers = layers; a.keep = keep; a.first = first; a.recent = recent; a.max_len = max_len;
+  a.most = std::min(keep, max_len - keep);
+  a.weights = pages->weights; a.places = pages->places;
+  a.count = (int32_t*)scratch;
+  a.moves = (int2*)((char*)scratch + (units * 4 + 15) / 16 * 16);
+  hipStream_t st = (hipStream_t)hip_stream;
+  ls::k_evict_choose<<<units, 256, 0, st>>>(a);
+  const dim3 grid(units, std::min(std::max((int)(((int64_t)a.most * pieces + 1023) / 1024), 1), 64));
+  if (wide)
+    ls::k_evict_move<ls::u32x4><<<grid, 256, 0, st>>>(a, (ls::u32x4*)pages->k, (ls::u32x4*)pages->v, pages->weights, pages->places, pages->lens, pieces);
+  else
+    ls::k_evict_move<uint32_t><<<grid, 256, 0, st>>>(a, (uint32_t*)pages->k, (uint32_t*)pages->v, pages->weights, pages->places, pages->lens, pieces);
+  return launched(who);
+}
+
+}  // extern "C"

@@ -1,0 +1,293 @@
+// Attention of one new token a sequence over a cache in pages, with RoPE and the append.
+//
+//   s_i = q k_i / sqrt(hd) over the slots 0..n, slot n the token's own;  o = sum_i softmax(s)_i v_i
+//   weights[i] += sum over the query heads of a kv head of softmax(s)_i
+//
+// Here the kernel for every shape (the fast one: paged_attn_mfma.hip), which pieces a context is cut into, and the kernel that joins them
+// and adds the weights up.  One wavefront to a (sequence, query head, piece), a lane to one or two pairs of dims, eight keys and values on
+// their way at once; eight slots lie in one page, whose number is uniform.  Bound by a wavefront's instructions.
+#include "paged.hpp"
+
+#include <algorithm>
+
+namespace ls {
+
+namespace {
+
+// MAXP: pairs of a lane
+template <class T, int MAXP>
+__global__ void __launch_bounds__(64)
+k_paged_attn(PageMap map, const T* __restrict__ qkv, const float2* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, int32_t* __restrict__ places,
+             T* __restrict__ out, int batch, int hq, int hkv, int hd, int max_pos, int most, PagedPieces p) {
+  typedef T T2 __attribute__((ext_vector_type(2), aligned(sizeof(T))));  // a row may start anywhere
+  constexpr int AT_ONCE = 8;  // keys and values on their way
+  const int z = blockIdx.z, h = blockIdx.y, b = blockIdx.x, lane = threadIdx.x, half = hd >> 1;
+  const int G = hq / hkv, kh = h / G;
+  const size_t row = (size_t)b * hq + h;
+  T* o = out + row * hd;
+  PagedSeq t;
+  if (!paged_seq(map, b, max_pos, cs != nullptr, most, t)) {
+    if (z == 0)
+      for (int i = lane; i < hd; i += 64) o[i] = from_f<T>(0.f);
+    return;
+  }
+  const int lo = z * p.keys, keys = t.n + 1;
+  if (lo >= keys) return;
+  const int hi = z == p.n - 1 ? keys : min(lo + p.keys, keys);  // the last piece takes what is left
+  const T* rows = qkv + (size_t)b * (hq + 2 * hkv) * hd;
+  const bool own = hi == keys;  // the new token is among this piece's
+  float q0[MAXP], q1[MAXP], k0[MAXP], k1[MAXP], v0[MAXP], v1[MAXP], a0[MAXP], a1[MAXP];
+#pragma unroll
+  for (int i = 0; i < MAXP; ++i) {
+    const int at = lane + 64 * i;
+    a0[i] = a1[i] = q0[i] = q1[i] = k0[i] = k1[i] = v0[i] = v1[i] = 0.f;
+    if (at < half) {
+      const float2 turn = cs ? cs[(size_t)t.pos * half + at] : float2{1.f, 0.f};
+      auto turned = [&](const T* r, float& w0, float& w1) {
+        const float u0 = to_f(r[2 * at]), u1 = to_f(r[2 * at + 1]);
+        w0 = cs ? turn0(u0, u1, turn) : u0;
+        w1 = cs ? turn1(u0, u1, turn) : u1;
+      };
+      turned(rows + (size_t)h * hd, q0[i], q1[i]);
+      if (own) {
+        turned(rows + (size_t)(hq + kh) * hd, k0[i], k1[i]);
+        const T c0 = from_f<T>(k0[i]), c1 = from_f<T>(k1[i]);
+        const T d0 = rows[(size_t)(hq + hkv + kh) * hd + 2 * at], d1 = rows[(size_t)(hq + hkv + kh) * hd + 2 * at + 1];
+        k0[i] = to_f(c0);
+        k1[i] = to_f(c1);
+        v0[i] = to_f(d0);
+        v1[i] = to_f(d1);
+        if (h % G == 0) {
+          const size_t to = (page_row0(t.page, hkv, kh, map.shift) + (t.n & ((1 << map.shift) - 1))) * hd + 2 * at;
+          kc[to] = c0;
+          kc[to + 1] = c1;
+          vc[to] = d0;
+          vc[to + 1] = d1;
+        }
+      }
+    }
+  }
+  if (places && own && h % G == 0 && lane == 0) places[page_row0(t.page, hkv, kh, map.shift) + (t.n & ((1 << map.shift) - 1))] = t.pos;
+  const float scale = 1.4426950408889634f / sqrtf((float)hd);  // q k -> exponent of 2
+  const int32_t* entries = map.table + (size_t)b * map.columns;
+  // Sums of AT_ONCE keys go into sums of NEAR times that, and those into the whole ones: one by one, equal weights next to a long sum
+  // are all rounded the same way.
+  constexpr int NEAR = 64;
+  float m = -INFINITY, l = 0.f, far_l = 0.f, far0[MAXP] = {}, far1[MAXP] = {};
+  for (int key0 = lo, turns = 1; key0 < hi; key0 += AT_ONCE, ++turns) {
+    T2 kr[AT_ONCE][MAXP], vr[AT_ONCE][MAXP];
+    const int page = entries[key0 >> map.shift];
+    const bool there = (unsigned)page < (unsigned)map.pages;
+    const size_t base = (page_row0(there ? page : 0, hkv, kh, map.shift) + (key0 & ((1 << map.shift) - 1))) * hd;
+    bool seen[AT_ONCE];
+    float s[AT_ONCE], mn = m;
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      seen[j] = there && key0 + j < hi;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i) {
+        const size_t at = base + (size_t)j * hd + 2 * min(lane + 64 * i, half - 1);
+        kr[j][i] = *reinterpret_cast<const T2*>(kc + at);
+        vr[j][i] = *reinterpret_cast<const T2*>(vc + at);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      s[j] = 0.f;
+      const bool new_one = own && key0 + j == t.n;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i)
+        if (lane + 64 * i < half) s[j] = fmaf(q0[i], new_one ? k0[i] : to_f(kr[j][i][0]), fmaf(q1[i], new_one ? k1[i] : to_f(kr[j][i][1]), s[j]));
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) s[j] = wave_sum(s[j]);
+    if (p.scores) {
+      float mine = 0.f;
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) mine = lane == j ? s[j] : mine;
+      if (lane < AT_ONCE && key0 + lane < hi) p.scores[row * p.stride + key0 + lane] = mine;
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (seen[j]) mn = fmaxf(mn, s[j]);
+    const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * scale);
+    float near_l = 0.f, near0[MAXP] = {}, near1[MAXP] = {};
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      if (!seen[j]) continue;
+      const bool new_one = own && key0 + j == t.n;
+      const float w = s[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s[j] - mn) * scale);
+      near_l += w;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i) {
+        near0[i] = fmaf(w, new_one ? v0[i] : to_f(vr[j][i][0]), near0[i]);
+        near1[i] = fmaf(w, new_one ? v1[i] : to_f(vr[j][i][1]), near1[i]);
+      }
+    }
+    l = fmaf(l, corr, near_l);
+    far_l *= corr;
+#pragma unroll
+    for (int i = 0; i < MAXP; ++i) {
+      a0[i] = fmaf(a0[i], corr, near0[i]);
+      a1[i] = fmaf(a1[i], corr, near1[i]);
+      far0[i] *= corr;
+      far1[i] *= corr;
+    }
+    if (turns % NEAR == 0) {
+      far_l += l;
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < MAXP; ++i) {
+        far0[i] += a0[i];
+        far1[i] += a1[i];
+        a0[i] = a1[i] = 0.f;
+      }
+    }
+    m = mn;
+  }
+  l += far_l;
+  const bool whole = p.n == 1 || keys <= p.keys;
+  const size_t at = (size_t)z * batch * hq + row;
+  if ((!whole || p.scores) && lane == 0) p.ml[at] = float2{m, l};
+#pragma unroll
+  for (int i = 0; i < MAXP; ++i) {
+    const int pair = lane + 64 * i;
+    if (pair >= half) continue;
+    const float n0 = far0[i] + a0[i], n1 = far1[i] + a1[i];
+    if (whole) {
+      o[2 * pair] = from_f<T>(n0 / l);
+      o[2 * pair + 1] = from_f<T>(n1 / l);
+    } else {
+      p.o[at * hd + 2 * pair] = n0;
+      p.o[at * hd + 2 * pair + 1] = n1;
+    }
+  }
+}
+
+// Maximum and sum of a (sequence, query head) over its pieces, in their order.
+__device__ __forceinline__ float2 joined(const float2* __restrict__ ml, size_t step, int n, float scale) {
+  float m = -INFINITY, den = 0.f;
+  for (int z = 0; z < n; ++z) m = fmaxf(m, ml[z * step].x);
+  for (int z = 0; z < n; ++z) {
+    const float2 v = ml[z * step];
+    den += v.y * (v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((v.x - m) * scale));  // a sum without a maximum is 0, or no number
+  }
+  return float2{m, den};
+}
+
+// The pieces' results, and the slots' weights.  Workgroups [0, out_blocks) of a sequence take its output, 256 dims each, the others a kv
+// head's 256 slots each.
+template <class T>
+__global__ void __launch_bounds__(256)
+k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int batch, int hq, int hkv, int hd, int max_pos, bool turns, int most, PagedPieces p,
+             int out_blocks) {
+  const int b = blockIdx.y;
+  PagedSeq t;
+  if (!paged_seq(map, b, max_pos, turns, most, t)) return;
+  const int keys = t.n + 1, n = min((keys + p.keys - 1) / p.keys, p.n);
+  const size_t step = (size_t)batch * hq;
+  const float scale = 1.4426950408889634f / sqrtf((float)hd);
+  if ((int)blockIdx.x < out_blocks) {
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (n == 1 || i >= hq * hd) return;  // one piece writes the output itself
+    const size_t row = (size_t)b * hq + i / hd;
+    const float2 all = joined(p.ml + row, step, n, scale);
+    float num = 0.f;
+    for (int z = 0; z < n; ++z) {
+      const float mz = p.ml[row + z * step].x;
+      num += p.o[(row + z * step) * hd + i % hd] * (mz == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mz - all.x) * scale));
+    }
+    out[row * hd + i % hd] = from_f<T>(num / all.y);
+    return;
+  }
+  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, slot = item % blocks * 256 + threadIdx.x, G = hq / hkv;
+  if (item % blocks * 256 >= keys) return;
+  float got = 0.f;
+  for (int g = 0; g < G; ++g) {
+    const size_t row = (size_t)b * hq + kh * G + g;
+    const float2 all = joined(p.ml + row, step, n, scale);
+    if (slot < keys) got += __builtin_amdgcn_exp2f((p.scores[row * p.stride + slot] - (all.x == -INFINITY ? 0.f : all.x)) * scale) / all.y;
+  }
+  if (slot >= keys) return;
+  const int page = map.table[(size_t)b * map.columns + (slot >> map.shift)];
+  if ((unsigned)page >= (unsigned)map.pages) return;
+  const size_t at = page_row0(page, hkv, kh, map.shift) + (slot & ((1 << map.shift) - 1));
+  weights[at] = slot == t.n ? got : weights[at] + got;
+}
+
+template <class T>
+void launch_any(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
+  auto attn = a.hd <= 128 ? k_paged_attn<T, 1> : k_paged_attn<T, 2>;
+  attn<<<dim3(a.batch, a.hq, p.n), 64, 0, st>>>(a.map, (const T*)a.qkv, (const float2*)a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.batch, a.hq, a.hkv, a.hd,
+                                                a.max_pos, most, p);
+}
+
+bool fast(const PagedAttn&) { return false; }
+
+PagedPieces pieces_for(const PagedAttn& a) {
+  PagedPieces p;
+  const long base = (long)a.batch * a.hq, want = std::min(std::max(4096 / base, 1l), (a.max_keys + 127l) / 128);
+  p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
+  p.n = (a.max_keys + p.keys - 1) / p.keys;
+  return p;
+}
+
+// Bytes of the partial results of n pieces, and of the scores in front of them.
+size_t piece_bytes(const PagedAttn& a, int n) { return (size_t)n * a.batch * a.hq * (a.hd + 2) * sizeof(float); }
+int score_stride(const PagedAttn& a) { return (a.max_keys + 31) / 32 * 32; }
+size_t score_bytes(const PagedAttn& a) { return a.weights ? (size_t)a.batch * a.hq * score_stride(a) * sizeof(float) : 0; }
+
+}  // namespace
+
+size_t paged_attn_scratch_bytes(const PagedAttn& a) {
+  const PagedPieces p = pieces_for(a);
+  return p.n > 1 || a.weights ? score_bytes(a) + piece_bytes(a, p.n) : 0;
+}
+
+void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st) {
+  PagedPieces p = pieces_for(a);
+  const int most = a.weights ? a.max_keys : INT32_MAX;
+  if (!a.weights && p.n > 1 && (!a.scratch || piece_bytes(a, p.n) > a.scratch_bytes)) {  // as many as there is room for
+    const int fit = a.scratch ? (int)(a.scratch_bytes / piece_bytes(a, 1)) : 0;
+    p.keys = ((a.max_keys + std::max(fit, 1) - 1) / std::max(fit, 1) + 63) / 64 * 64;
+    p.n = (a.max_keys + p.keys - 1) / p.keys;
+  }
+  if (a.scratch && (a.weights || p.n > 1)) {
+    float* at = a.scratch;
+    if (a.weights) {
+      p.scores = at;
+      p.stride = score_stride(a);
+      at += (size_t)a.batch * a.hq * p.stride;
+    }
+    p.o = at;
+    p.ml = (float2*)(at + (size_t)p.n * a.batch * a.hq * a.hd);
+  }
+  if (dt == F32) launch_any<float>(a, p, most, st);
+  else launch_any<bf16>(a, p, most, st);
+  if (p.n == 1 && !a.weights) return;
+  const int out_blocks = p.n > 1 ? (a.hq * a.hd + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;
+  const dim3 grid(out_blocks + slots, a.batch);
+  if (dt == F32)
+    k_paged_join<float><<<grid, 256, 0, st>>>(a.map, (float*)a.out, a.weights, a.batch, a.hq, a.hkv, a.hd, a.max_pos, a.cs != nullptr, most, p, out_blocks);
+  else
+    k_paged_join<bf16><<<grid, 256, 0, st>>>(a.map, (bf16*)a.out, a.weights, a.batch, a.hq, a.hkv, a.hd, a.max_pos, a.cs != nullptr, most, p, out_blocks);
+}
+
+namespace {
+
+__global__ void __launch_bounds__(256)
+k_paged_next(PageMap map, int32_t* lens, int32_t* positions, int batch, int max_pos, int most) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  PagedSeq t;
+  if (b >= batch || !paged_seq(map, b, max_pos, true, most, t)) return;
+  lens[b] = t.n + 1;
+  if (positions) positions[b] = t.pos + 1;
+}
+
+}  // namespace
+
+void launch_paged_next(const PagedAttn& a, int32_t* lens, int32_t* positions, hipStream_t st) {
+  k_paged_next<<<(a.batch + 255) / 256, 256, 0, st>>>(a.map, lens, positions, a.batch, a.max_pos, a.weights ? a.max_keys : INT32_MAX);
+}
+
+}  // namespace ls

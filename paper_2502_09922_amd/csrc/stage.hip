@@ -3,6 +3,7 @@
 // is a kernel launched through kernels.hpp.
 #include "entry.hpp"
 #include "kernels.hpp"
+#include "paged.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -596,10 +597,11 @@ bool own_memory(const ls_stage* s, const void* p) {
   return false;
 }
 
-// `gsc`: where GEMM kernels that split K across workgroups put their partial tiles.  `trees`: the rows are nodes of draft trees,
-// of which every one gets logits and a next token; rows keep no maps then and seq_lens stays.
+// `gsc`: where GEMM kernels that split K across workgroups put their partial tiles.  `trees`, `paged`: the rows are nodes of draft trees, or
+// sequences over a cache in pages (kv holds nothing then); every row gets logits and a next token, rows keep no maps and seq_lens stays.
 ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_dev, int batch, int rows, int max_len,
-                  const ls_kv* kv, void* out, float* logits_out, hipStream_t st, const ls::GemmScratch& gsc, const ls::TreeAttn* trees = nullptr) {
+                  const ls_kv* kv, void* out, float* logits_out, hipStream_t st, const ls::GemmScratch& gsc, const ls::TreeAttn* trees = nullptr,
+                  const ls::PagedAttn* paged = nullptr) {
   using namespace ls;
   const ls_cfg& c = s->cfg;
   const uint32_t dt = c.dtype;
@@ -618,7 +620,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   int32_t* row_pos = (int32_t*)(ws + s->w.row_pos);
   int32_t* last_rows = (int32_t*)(ws + s->w.last_rows);
   const bool timed = s->profiling && prefill;
-  const bool probing = !trees && s->probe_op != LS_OP_NONE && s->probe_phase == (prefill ? 0 : 1) && !s->probe_a.empty();
+  const bool mapped = !trees && !paged;  // rows find their sequences and positions by maps
+  const bool probing = mapped && s->probe_op != LS_OP_NONE && s->probe_phase == (prefill ? 0 : 1) && !s->probe_a.empty();
 
   // PROBE(op, launch): bracket the launch with an event pair if this (op, layer) is probed
 #define PROBE(op, launch)                                                        \
@@ -651,13 +654,25 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
 
   // ---- decode step with the RMSNorms folded into the weight-streaming GEMMs
   const bool fused = !prefill && dt == BF16 && (size_t)rows <= fused_rows(&c) && d % 16 == 0 && (few_rows || !rows_supported(d)) &&
-                     (trees || attn_decode_supported(hq, hkv, hd) || attn_decode_gqa_supported(hq, hkv, hd)) &&
+                     (!mapped || attn_decode_supported(hq, hkv, hd) || attn_decode_gqa_supported(hq, hkv, hd)) &&
                      gemm_decode_fusable(rows, qkv_cols, d) && gemm_decode_fusable(rows, d, hq * hd) &&
                      gemm_decode_fusable(rows, F, d) && gemm_decode_fusable(rows, d, F);
   // rows of the head: the sequences' last ones, or all nodes, as many at a time as the workspace has logits for
-  const int heads = trees ? rows : batch, heads_at_once = std::min(heads, head_rows(&c));
+  const int heads = mapped ? batch : rows, heads_at_once = std::min(heads, head_rows(&c));
   auto logits_of = [&](int r0) { return logits_out ? logits_out + (size_t)r0 * c.vocab : (float*)(ws + s->w.logits); };
-  auto attend_trees = [&](const void* qkv, char* kc, char* vc, void* attn) {
+  auto attend = [&](int li, const void* qkv, char* kc, char* vc, void* attn) {
+    if (paged) {
+      PagedAttn a = *paged;
+      const size_t rows_before = (size_t)li * a.map.pages * hkv << a.map.shift;
+      a.qkv = qkv; a.cs = cs; a.out = attn;
+      a.kc = (char*)a.kc + rows_before * hd * e; a.vc = (char*)a.vc + rows_before * hd * e;
+      if (a.weights) {
+        a.weights += rows_before;
+        a.places += rows_before;
+      }
+      launch_paged_attn(dt, a, st);
+      return;
+    }
     TreeAttn a = *trees;
     a.qkv = qkv; a.cs = cs; a.kc = kc; a.vc = vc; a.out = attn;
     // the GEMMs' partial tiles are added up by now, their room is the larger one mostly
@@ -699,7 +714,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     }
     const bool head_folds = hb && rows <= 16 && heads_at_once == heads && gemm_decode_fusable(rows, (int)c.vocab, d);
     LS_HIP(gate(s->blocks[s->layer0], st));  // the gate of the first layer
-    launch_decode_prologue(dt, table, in, trees ? nullptr : kv->seq_lens, rows, c.max_seq, d, c.vocab, row_seq, row_pos, last_rows, x,
+    launch_decode_prologue(dt, table, in, mapped ? kv->seq_lens : nullptr, rows, c.max_seq, d, c.vocab, row_seq, row_pos, last_rows, x,
                            xb, ss_a, gain(0, 0), st);
     for (int li = 0; li < n_layers; ++li) {
       Block& b = s->blocks[s->layer0 + li];
@@ -718,8 +733,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
       f_dn.xb_out = (!more && !s->last) ? (__bf16*)out : xb; f_dn.ss_out = ss_a;
       f_dn.gamma_out = more ? gain(li + 1, 0) : head_folds ? (const __bf16*)(head + head_sp[0].off) : nullptr;
       PROBE(LS_OP_GEMM_QKV, launch_gemm(dt, EPI_STORE, xb, base + sp[1].off, rows, qkv_cols, d, qkv, nullptr, st, &gsc, &f_qkv));
-      if (trees)
-        attend_trees(qkv, kc, vc, attn);
+      if (!mapped)
+        attend(li, qkv, kc, vc, attn);
       else
         PROBE(LS_OP_ATTENTION, launch_attention_block(dt, nullptr, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
                                                       hq, hkv, hd, c.max_seq, attn, st,
@@ -743,7 +758,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
         for (int r0 = 0; r0 < heads; r0 += heads_at_once) {
           const int n = std::min(heads_at_once, heads - r0);
           float* logits = logits_of(r0);
-          launch_rmsnorm(dt, x + (size_t)r0 * d, head + head_sp[0].off, y, n, d, c.rms_eps, trees ? nullptr : last_rows, st);
+          launch_rmsnorm(dt, x + (size_t)r0 * d, head + head_sp[0].off, y, n, d, c.rms_eps, mapped ? last_rows : nullptr, st);
           launch_gemm(dt, EPI_F32, y, head + head_sp[1].off, n, c.vocab, d, logits, nullptr, st, &gsc);
           launch_argmax(logits, n, c.vocab, (int32_t*)out + r0, st);
         }
@@ -754,7 +769,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   }
 
   // ---- generation steps of few rows of a small fp32 model: one launch, once every block has landed
-  if (!prefill && !trees && dt == F32 && s->step_places.xch && !probing) {
+  if (!prefill && mapped && dt == F32 && s->step_places.xch && !probing) {
     SmallStep a;
     TensorSpan sp[6];
     const Block& b0 = s->blocks[s->layer0];
@@ -806,8 +821,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   // The tiled GEMM takes every fp32 projection it supports, and the bf16 ones of all but few rows
   // where it is estimated faster than the 256 x 256 tiles.
   // Partial tiles of a generation step fit the static scratch too, so that both entry points take
-  // the same plans.  Passes over trees have one entry point and as many rows as prompt passes.
-  const size_t part_bytes = prefill || trees || gsc.bytes < LS_STATIC_SCRATCH_BYTES ? gsc.bytes : LS_STATIC_SCRATCH_BYTES;
+  // the same plans.  Passes over trees or pages have one entry point, and those over trees as many rows as prompt passes.
+  const size_t part_bytes = prefill || !mapped || gsc.bytes < LS_STATIC_SCRATCH_BYTES ? gsc.bytes : LS_STATIC_SCRATCH_BYTES;
   auto plan = [&](int epi, int N, int K) {
     if (few_rows) return TiledPlan{};
     float us = 0.f;
@@ -819,7 +834,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
   };
   // attention without a fused kernel, and that of a prompt pass, wants rotated rows and a filled cache
   const bool attn_rotates =
-      trees || (!prefill && (attn_decode_supported(hq, hkv, hd) || (dt == BF16 && attn_decode_gqa_supported(hq, hkv, hd))));
+      !mapped || (!prefill && (attn_decode_supported(hq, hkv, hd) || (dt == BF16 && attn_decode_gqa_supported(hq, hkv, hd))));
   const bool rope_tiles = !attn_rotates && hd % 16 == 0;  // a 16-column fragment inside one head
   const TiledPlan p_qkv = attn_rotates ? plan(TILED_STORE, qkv_cols, d) : rope_tiles ? plan(TILED_ROPE, qkv_cols, d) : TiledPlan{};
   const TiledPlan p_o = rows_one_pass && gsc.splitk ? plan(TILED_PART, d, hq * hd) : TiledPlan{};
@@ -844,7 +859,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     RowsArgs ra;
     ra.rows = rows; ra.d = d; ra.x = x; ra.in = in; ra.table = table; ra.vocab = c.vocab;
     ra.cu = prefill ? cu_dev : nullptr; ra.batch = batch; ra.max_seq = c.max_seq;
-    ra.row_seq = row_seq; ra.row_pos = row_pos; ra.last_rows = last_rows; ra.seq_lens = trees ? nullptr : kv->seq_lens;
+    ra.row_seq = row_seq; ra.row_pos = row_pos; ra.last_rows = last_rows; ra.seq_lens = mapped ? kv->seq_lens : nullptr;
     Block& b0 = s->blocks[s->layer0];
     if (landed(b0) && !norm_alone(b0) && !(few_pieces && folds_norm(p_qkv, qkv_cols))) {
       ra.gamma = tensor(b0, 0); ra.y = y; ra.eps = c.rms_eps;
@@ -859,7 +874,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     launch_rows(dt, s->first ? ROWS_EMBED : ROWS_HIDDEN, ra, st);
   } else {
     if (prefill) launch_row_index_prefill(cu_dev, batch, rows, row_seq, row_pos, last_rows, st);
-    else if (!trees) launch_row_index_decode(kv->seq_lens, batch, c.max_seq, row_seq, row_pos, last_rows, st);
+    else if (mapped) launch_row_index_decode(kv->seq_lens, batch, c.max_seq, row_seq, row_pos, last_rows, st);
     if (s->first) launch_embed(dt, table, (const int32_t*)in, x, rows, d, c.vocab, st);
     else launch_load_hidden(dt, in, x, (size_t)rows * d, st);
   }
@@ -929,8 +944,8 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     } else {
       PROBE(LS_OP_GEMM_QKV, launch_gemm(dt, EPI_STORE, y, tensor(b, 1), rows, qkv_cols, d, qkv, nullptr, st, &gsc));
     }
-    if (trees) {
-      attend_trees(qkv, kc, vc, attn);
+    if (!mapped) {
+      attend(li, qkv, kc, vc, attn);
     } else {
       PROBE(LS_OP_ATTENTION, launch_attention_block(dt, cu_dev, batch, max_len, qkv, cs, kc, vc, row_seq, row_pos, rows,
                                                     hq, hkv, hd, c.max_seq, attn, st,
@@ -967,7 +982,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
     LS_HIP(gate(*hb, st));  // gate: head block has landed
     for (int r0 = 0; r0 < heads; r0 += heads_at_once) {
       const int n = std::min(heads_at_once, heads - r0);
-      const int32_t* map = trees ? nullptr : last_rows;
+      const int32_t* map = mapped ? last_rows : nullptr;
       const float* xr = x + (size_t)r0 * d;
       float* logits = logits_of(r0);
       const TiledPlan p_head = (dt == F32 || n > (d > 4096 ? 8 : 16)) && ((uintptr_t)logits & 15) == 0
@@ -988,7 +1003,7 @@ ls_status forward(ls_stage* s, bool prefill, const void* in, const int32_t* cu_d
 
   if (!rows_one_pass) {
     if (prefill) launch_seq_lens_set(cu_dev, batch, kv->seq_lens, st);
-    else if (!trees) launch_seq_lens_inc(batch, c.max_seq, kv->seq_lens, st);
+    else if (mapped) launch_seq_lens_inc(batch, c.max_seq, kv->seq_lens, st);
   }
   if (timed) LS_HIP(hipEventRecord(s->pass_end, st));
   LS_HIP(hipGetLastError());
@@ -1136,6 +1151,26 @@ ls_status ls_stage_tree(ls_stage* s, const void* in, const ls_tree* tree, int ba
   a.max_keys = std::min(max_ctx + a.max_nodes, (int)s->cfg.max_seq);
   a.hq = (int)s->cfg.n_q_heads; a.hkv = (int)s->cfg.n_kv_heads; a.hd = (int)s->cfg.head_dim; a.max_seq = (int)s->cfg.max_seq;
   return forward(s, false, in, nullptr, batch, a.rows, a.max_keys, kv, out, logits_out, (hipStream_t)hip_stream, workspace_scratch(s), &a);
+}
+
+ls_status ls_stage_paged(ls_stage* s, const void* in, int batch, int max_ctx, const ls_pages* pages, void* out, float* logits_out, void* scratch,
+                         size_t scratch_bytes, void* hip_stream) {
+  static const char* who = "ls_stage_paged";
+  ls_status rc = check_state(who, s, batch);
+  if (rc != LS_OK) return rc;
+  if (!in || !out) return fail(LS_ERR_INVALID_ARG, "%s: NULL argument", who);
+  if (logits_out && !s->last) return fail(LS_ERR_INVALID_ARG, "%s: logits_out given but the stage has no LM head", who);
+  const ls_cfg& c = s->cfg;
+  const ls_heads heads{c.dtype, c.n_q_heads, c.n_kv_heads, c.head_dim, c.max_batch, c.max_seq};
+  ls::PagedAttn a;
+  rc = ls::paged_attention_args(who, &heads, pages, batch, max_ctx, true, scratch, scratch_bytes, &a);
+  if (rc != LS_OK) return rc;
+  const ls_kv none{};
+  rc = forward(s, false, in, nullptr, batch, batch, max_ctx + 1, &none, out, logits_out, (hipStream_t)hip_stream, workspace_scratch(s), nullptr, &a);
+  if (rc != LS_OK) return rc;
+  ls::launch_paged_next(a, pages->lens, pages->positions, (hipStream_t)hip_stream);
+  LS_HIP(hipGetLastError());
+  return LS_OK;
 }
 
 ls_status ls_stage_decode_static(ls_stage* s, const void* in, int batch, int max_ctx, const ls_kv* kv, void* out,
