@@ -1,0 +1,26 @@
+// What the matrix-core kernels of attention over a cache share: tiles' layout in LDS, bf16 operands in two parts.
+#pragma once
+#include "device_util.hpp"
+
+namespace ls {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// 16-byte chunks of a row of a tile are permuted by its key, so that 16 rows' equal chunks (keys) and 4 rows' 32 bytes (values,
+// transposing) lie in different banks.
+template <class T, int HD> __device__ __forceinline__ int key_swizzle(int key) { return HD == 128 || sizeof(T) == 4 ? key & 15 : ((key & 3) << 1) | ((key >> 2) & 1); }
+template <class T, int HD> __device__ __forceinline__ int value_swizzle(int key) {
+  return sizeof(T) == 4 ? 0 : HD == 128 ? (key & 7) << 1 : ((key & 3) << 1) | ((key >> 2) & 1);
+}
+
+// v as a sum of two bf16: the first is v cut off, the second the rest, rounded, at least 2^-23 of v and of its sign.  Off by 2^-15 of v at
+// most; infinite factors take part with their sign alone (inf + 0 inf or inf - inf would be no number).  0 stays 0.
+__device__ __forceinline__ void two_parts(float v, bf16& first, bf16& second) {
+  const unsigned bits = __builtin_bit_cast(unsigned, v);
+  first = __builtin_bit_cast(bf16, (unsigned short)(bits >> 16));
+  second = (bf16)fmaf(v, 0x1.000002p0f, -__builtin_bit_cast(float, bits & 0xFFFF0000u));
+}
+
+}  // namespace ls

@@ -36,7 +36,7 @@ struct PagedPieces {
   float* scores = nullptr;  // [row * hq + head][stride] q k of every slot, where weights are wanted
   int stride = 0;
 };
-void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
+void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
 
 struct PagedSeq {
   int n, pos, page;  // slot and position of the new token, the slot's page

@@ -222,11 +222,17 @@ void launch_any(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t 
                                                 a.max_pos, most, p);
 }
 
-bool fast(const PagedAttn&) { return false; }
+bool fast(const PagedAttn& a) {
+  const uintptr_t at = (uintptr_t)a.qkv | (uintptr_t)a.kc | (uintptr_t)a.vc | (uintptr_t)a.out | (uintptr_t)a.cs;
+  return (a.hd == 64 || a.hd == 128) && (at & 15) == 0 && a.hq <= 65535;
+}
 
+// Pieces of a call's contexts.
 PagedPieces pieces_for(const PagedAttn& a) {
   PagedPieces p;
-  const long base = (long)a.batch * a.hq, want = std::min(std::max(4096 / base, 1l), (a.max_keys + 127l) / 128);
+  const bool mfma = fast(a);
+  const long base = mfma ? (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) : (long)a.batch * a.hq, target = mfma ? 512 : 4096;
+  const long want = std::min(std::max(target / base, 1l), (a.max_keys + 127l) / 128);
   p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
   p.n = (a.max_keys + p.keys - 1) / p.keys;
   return p;
@@ -247,9 +253,10 @@ size_t paged_attn_scratch_bytes(const PagedAttn& a) {
 void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st) {
   PagedPieces p = pieces_for(a);
   const int most = a.weights ? a.max_keys : INT32_MAX;
-  if (!a.weights && p.n > 1 && (!a.scratch || piece_bytes(a, p.n) > a.scratch_bytes)) {  // as many as there is room for
-    const int fit = a.scratch ? (int)(a.scratch_bytes / piece_bytes(a, 1)) : 0;
-    p.keys = ((a.max_keys + std::max(fit, 1) - 1) / std::max(fit, 1) + 63) / 64 * 64;
+  const size_t room = a.scratch ? a.scratch_bytes - score_bytes(a) : 0;  // with weights there is room for one piece at least
+  if (p.n > 1 && piece_bytes(a, p.n) > room) {                            // as many as there is room for
+    const int fit = std::max((int)(room / piece_bytes(a, 1)), 1);
+    p.keys = ((a.max_keys + fit - 1) / fit + 63) / 64 * 64;
     p.n = (a.max_keys + p.keys - 1) / p.keys;
   }
   if (a.scratch && (a.weights || p.n > 1)) {
@@ -262,7 +269,8 @@ void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st) {
     p.o = at;
     p.ml = (float2*)(at + (size_t)p.n * a.batch * a.hq * a.hd);
   }
-  if (dt == F32) launch_any<float>(a, p, most, st);
+  if (fast(a)) launch_paged_attn_mfma(dt, a, p, most, st);
+  else if (dt == F32) launch_any<float>(a, p, most, st);
   else launch_any<bf16>(a, p, most, st);
   if (p.n == 1 && !a.weights) return;
   const int out_blocks = p.n > 1 ? (a.hq * a.hd + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;

@@ -1,0 +1,439 @@
+// Attention of one new token a sequence over a cache in pages, on the matrix cores (head_dim 64 and 128).
+//
+// The query heads of a kv head are the columns of both products:
+//   S^T[key][column] = K Q^T        A = 16 key rows, B = 16 columns
+//   O^T[dim][column] += V^T P^T     A = V^T, B = P^T
+// with the operand layouts, the split of bf16 queries and weights into two parts and the softmax of the attention of draft trees
+// (tree_attn_mfma.hip): a lane of a result holds column lane % 16 and rows 4 (lane / 16) + e.
+//
+// A workgroup is a (sequence, kv head, block of 16 columns, piece of the slots); its wavefronts take the piece's tiles in turn, each through a ring of
+// LDS of its own that is filled straight from memory, so there are no barriers and what is on its way needs no registers: bound by memory, what
+// counts is how many bytes a CU has asked for.  A page's number is a scalar (pages have at least eight slots, a wavefront's load covers
+// eight rows at most) that is fetched a tile ahead.  The wavefronts' results are joined through LDS, those of pieces by a second
+// kernel, both in order.
+//
+// The new token's row is put into its tile in LDS by the wavefront that has that tile, and into the cache: nobody waits for memory there.
+#include "attn_mfma.hpp"
+#include "paged.hpp"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace ls {
+
+namespace {
+
+constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns' equal dims in different banks
+constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds in registers
+constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
+constexpr float FOLLOW = 8.f;
+constexpr int CUS = 256;
+
+// TK: keys of a tile; NW: wavefronts; NB: tiles of a ring, a power of two
+template <class T, int HD, int TK, int NW, int NB, bool WEIGH>
+__global__ void __launch_bounds__(64 * NW, 2)
+k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, int32_t* __restrict__ places,
+             T* __restrict__ out, int hq, int hkv, int max_pos, int most, int half, int batch, PagedPieces p) {
+  constexpr int THREADS = 64 * NW;
+  constexpr int ROWB = HD * sizeof(T), EPC = 16 / sizeof(T);
+  constexpr int CPR = HD / EPC;    // 16-byte chunks of a row
+  constexpr int RPI = 64 / CPR;    // rows that a wavefront's load covers
+  constexpr int NL = TK / RPI;     // loads of a tile's keys, as many of its values
+  constexpr int UNITS = TK / 8;    // parts of a tile that lie in one page whatever the page's size
+  constexpr int TILE = TK * ROWB;
+  constexpr int DT = HD / 16, HALVES = TK / 16;
+  constexpr int STORES = WEIGH ? HALVES : 0;  // of a tile's scores
+  static_assert(RPI <= 8 && (NB & (NB - 1)) == 0, "");
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+
+  const int G = hq / hkv, blocks = (G + 15) / 16;
+  const int kh = blockIdx.y / blocks, cb = blockIdx.y % blocks, z = blockIdx.z, cols = min(16, G - cb * 16);
+  int b = blockIdx.x, len_of_b;
+  // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest
+  if (half) {
+    const int rank = b < half ? b : batch - 1 - (b - half);
+    b = batch <= 64 ? row_by_length<1, true>(map.lens, batch, rank, 1 << 24, len_of_b) : row_by_length<ORDERED / 64, true>(map.lens, batch, rank, 1 << 24, len_of_b);
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const size_t row0 = (size_t)b * hq + kh * G + cb * 16;  // output row of column 0
+  PagedSeq t;
+  if (!paged_seq(map, b, max_pos, cs != nullptr, most, t)) {  // the rows hold zeros
+    if (z == 0)
+      for (int i = threadIdx.x; i < cols * HD; i += THREADS) out[row0 * HD + i] = from_f<T>(0.f);
+    return;
+  }
+  const int keys = t.n + 1, ntile = (keys + TK - 1) / TK, per = p.keys / TK;
+  const int t_lo = z * per;
+  if (t_lo >= ntile) return;
+  const int t_hi = z == p.n - 1 ? ntile : min(t_lo + per, ntile);  // the last piece takes what is left
+  const int count = max(0, (t_hi - t_lo - wave + NW - 1) / NW);    // tiles of this wavefront: t_lo + wave, NW further each time
+  const int mask = (1 << map.shift) - 1, last_entry = t.n >> map.shift;
+  // Nothing in the launch writes the table: scalar loads, which do not queue behind the tiles on their way.
+  typedef const __attribute__((address_space(4))) int32_t entry;
+  const entry* entries = (const entry*)(uintptr_t)(map.table + (size_t)b * map.columns);
+  const int lrow = lane / CPR, lchunk = lane % CPR;
+
+  // ---- the ring
+  int page[UNITS];  // of the tile that is filled next
+  auto look_up = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) page[u] = entries[min(((t_lo + wave + i * NW) * TK + 8 * u) >> map.shift, last_entry)];
+  };
+  unsigned koff[NL], voff[NL];  // a row's piece from the first of its eight rows
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int r = i * RPI + lrow;
+    koff[i] = (r & 7) * ROWB + ((lchunk ^ key_swizzle<T, HD>(r)) << 4);
+    voff[i] = (r & 7) * ROWB + ((lchunk ^ value_swizzle<T, HD>(r)) << 4);
+  }
+  const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char*)smem + wave * (NB * 2 * TILE);
+  int next = 0;                 // tiles that have been asked for
+  uint64_t gone = 0;            // whose parts have no page: UNITS bits for each of the last tiles asked for
+  // Written in assembly: of the builtin the compiler knows that it writes LDS but not where, and would wait for the fills on their way
+  // before it reads what has arrived.  (m0 is reserved, of which the compiler warns.)
+  auto fill = [&] {
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    auto piece = [](const T* base, unsigned off, unsigned to) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+    };
+#pragma clang diagnostic pop
+    const int key0 = (t_lo + wave + next * NW) * TK;
+    const unsigned to = lds0 + (next & (NB - 1)) * (2 * TILE);
+    const T *kt[UNITS], *vt[UNITS];
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int at = key0 + 8 * u;
+      const bool there = (unsigned)page[u] < (unsigned)map.pages;  // others read some page, and count as not seen
+      gone = gone << 1 | (at <= t.n && !there);
+      const size_t row = page_row0(there ? page[u] : 0, hkv, kh, map.shift) + (at & mask);
+      kt[u] = kc + row * HD;
+      vt[u] = vc + row * HD;
+    }
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      piece(kt[i * RPI / 8], koff[i], to + i * 1024);
+      piece(vt[i * RPI / 8], voff[i], to + TILE + i * 1024);
+    }
+    ++next;
+    look_up(next);
+  };
+  look_up(0);
+
+  // ---- queries: this wavefront's 16 columns, those behind the last are its copies
+  constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a row
+  const T* rows = qkv + (size_t)b * (hq + 2 * hkv) * HD;
+  const T* q = rows + (size_t)(kh * G + cb * 16 + min(lr, cols - 1)) * HD;
+  const float* turn = cs + (size_t)t.pos * HD;
+  u32x4 raw[KS];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) raw[kk] = *reinterpret_cast<const u32x4*>(q + (kk * 4 + lg) * EPC);
+  f32x4 angles[KS][EPC / 4];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+    for (int e = 0; e < EPC / 4; ++e) angles[kk][e] = cs ? reinterpret_cast<const f32x4*>(turn + (kk * 4 + lg) * EPC)[e] : f32x4{1.f, 0.f, 1.f, 0.f};
+  // the new token's row, a 16-byte piece to a lane: keys, and values behind them
+  const bool mine = count > 0 && t_lo + wave + (count - 1) * NW == ntile - 1;
+  const int nc = lane % CPR;
+  const bool nv = lane >= CPR;
+  u32x4 fresh{};
+  f32x4 nturn[EPC / 4] = {};
+  if (mine) {
+    fresh = *reinterpret_cast<const u32x4*>(rows + (size_t)(hq + (nv ? hkv : 0) + kh) * HD + nc * EPC);
+    if (cs)
+#pragma unroll
+      for (int e = 0; e < EPC / 4; ++e) nturn[e] = reinterpret_cast<const f32x4*>(turn + nc * EPC)[e];
+  }
+  while (next < min(count, NB)) fill();
+
+  typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Q;
+  Q qh[KS], ql[sizeof(T) == 2 ? KS : 1];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) {
+    const Q u = __builtin_bit_cast(Q, raw[kk]);
+    float w[EPC];
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) w[e] = to_f(u[e]);
+    if (cs)
+#pragma unroll
+      for (int e = 0; e < EPC; e += 2) {
+        const float2 c2{angles[kk][e / 4][e % 4], angles[kk][e / 4][e % 4 + 1]};
+        const float w0 = turn0(w[e], w[e + 1], c2), w1 = turn1(w[e], w[e + 1], c2);
+        w[e] = w0;
+        w[e + 1] = w1;
+      }
+#pragma unroll
+    for (int e = 0; e < EPC; ++e) {
+      if constexpr (sizeof(T) == 2) {
+        bf16 first, second;
+        two_parts(w[e], first, second);
+        qh[kk][e] = first;
+        ql[kk][e] = second;
+      } else {
+        qh[kk][e] = w[e];
+      }
+    }
+  }
+  if (mine) {
+    if (cs && !nv) {
+      Q u = __builtin_bit_cast(Q, fresh);
+#pragma unroll
+      for (int e = 0; e < EPC; e += 2) {
+        const float2 c2{nturn[e / 4][e % 4], nturn[e / 4][e % 4 + 1]};
+        const float u0 = to_f(u[e]), u1 = to_f(u[e + 1]);
+        u[e] = from_f<T>(turn0(u0, u1, c2));
+        u[e + 1] = from_f<T>(turn1(u0, u1, c2));
+      }
+      fresh = __builtin_bit_cast(u32x4, u);
+    }
+    if (cb == 0) {  // of blocks of columns one writes it
+      const size_t slot = page_row0(t.page, hkv, kh, map.shift) + (t.n & mask);
+      if (lane < 2 * CPR) *reinterpret_cast<u32x4*>((nv ? vc : kc) + slot * HD + nc * EPC) = fresh;
+      if (WEIGH && lane == 0) places[slot] = t.pos;
+    }
+  }
+
+  f32x4 o[DT];
+  float m_run = -INFINITY, l_run = 0.f;  // l_run: of this lane's keys
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const float scale = 1.4426950408889634f / sqrtf((float)HD);  // q k -> exponent of 2
+  // four neighbouring dims that a lane holds of a column: i of DT such, from dim_of(i) on
+  auto dim_of = [&](int i) { return sizeof(T) == 2 ? i * 16 + 4 * lg : (i >> 2) * 64 + 16 * lg + 4 * (i & 3); };
+  auto out_at = [&](int i, int e) -> float& {
+    float* at = reinterpret_cast<float*>(&o[0]);
+    return sizeof(T) == 2 ? at[i * 4 + e] : at[((i & ~3) + e) * 4 + (i & 3)];
+  };
+
+  for (int i = 0; i < count; ++i) {
+    const int key0 = (t_lo + wave + i * NW) * TK;
+    unsigned char* ks = smem + wave * (NB * 2 * TILE) + (i & (NB - 1)) * (2 * TILE);
+    unsigned char* vs = ks + TILE;
+    // Tile i has landed: behind its fills are those of the tiles asked for since, and the stores of the scores since then.
+    if (next - i == NB && i >= NB - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((NB - 1) * (2 * NL + STORES)));
+    else wait_vm((next - 1 - i) * 2 * NL + min(i, NB - 1) * STORES);
+    asm volatile("" ::: "memory");
+    const unsigned units = (unsigned)(gone >> ((next - 1 - i) * UNITS)) & ((1u << UNITS) - 1);  // the highest bit is the first part's
+    const bool masked = units || key0 + TK > keys, last = mine && i == count - 1;
+    unsigned seen = 0xFFFFFFFFu;
+    if (masked) {
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u)
+        if (units >> (UNITS - 1 - u) & 1) seen &= ~(0xFFu << (8 * u));
+      if (key0 + TK > keys) seen &= (1u << (keys - key0)) - 1;
+      // values that nobody sees may be anything: zero times that has to be zero
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+        if (!(seen >> (j * RPI + lrow) & 1)) *reinterpret_cast<u32x4*>(vs + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+    }
+    if (last && lane < 2 * CPR) {  // the new token's row
+      const int r = t.n - key0;
+      *reinterpret_cast<u32x4*>((nv ? vs : ks) + r * ROWB + ((nc ^ (nv ? value_swizzle<T, HD>(r) : key_swizzle<T, HD>(r))) << 4)) = fresh;
+    }
+    if (masked || last) asm volatile("" ::: "memory");
+
+    // ---- scores: all of a tile's keys are asked for at once, and all of its values before the softmax
+    f32x4 s[HALVES];
+    Q kf[HALVES][KS];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      const int kl = h * 16 + lr;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) kf[h][kk] = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
+      s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], part ? qh[kk] : ql[kk], s[h], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][kk][e], qh[kk][e], s[h], 0, 0, 0);
+      }
+    }
+    // bf16: the k index of the second product runs over keys {4g..4g+3} of each half, g = lane / 16, fp32: row 4g + e, dims 16-byte chunk by chunk
+    s16x4 vt[HALVES][sizeof(T) == 2 ? DT : 1];
+    Q vf[HALVES][sizeof(T) == 2 ? 1 : DT];
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      if constexpr (sizeof(T) == 2) {
+        const int k0 = h * 16 + 4 * lg + (lr >> 2), within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const int ch = d * 2 + ((lr & 3) >> 1);
+          vt[h][d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<T, HD>(k0)) << 4) + within));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < HD / 64; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vf[h][j * 4 + e] = *reinterpret_cast<const Q*>(vs + (h * 16 + 4 * lg + e) * ROWB + (j * 16 + lr) * 16);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (WEIGH) {
+      if (lr < cols)
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>(p.scores + (row0 + lr) * p.stride + key0 + h * 16 + 4 * lg) = s[h];
+    }
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 4 * HALVES; ++j) s[j >> 2][j & 3] = seen >> ((j >> 2) * 16 + 4 * lg + (j & 3)) & 1u ? s[j >> 2][j & 3] : -INFINITY;
+    }
+    // ---- softmax.  A NaN score makes its weight NaN, and the sums with it, whatever the maximum is.
+    float mx = s[0][0];
+#pragma unroll
+    for (int j = 1; j < 4 * HALVES; ++j) mx = __builtin_elementwise_maximum(mx, s[j >> 2][j & 3]);
+    // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: weights above one are as exact as below.
+    auto far = [&] { return (mx - m_run) * scale > FOLLOW; };  // false for (-inf, -inf)
+    if (__builtin_amdgcn_ballot_w64(far()) != 0) {             // lanes of a column exchange their maxima only then
+      mx = exchange<16, 32>(mx, Max{});
+      const bool moved = far();  // the others keep their bits
+      const float m_new = fmaxf(m_run, mx);
+      const float corr = moved ? __builtin_amdgcn_exp2f((m_run - m_new) * scale) : 1.f;
+      l_run *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= corr;
+      m_run = moved ? m_new : m_run;
+    }
+    const float mc = m_run == -INFINITY ? 0.f : m_run * scale;
+#pragma unroll
+    for (int j = 0; j < 4 * HALVES; ++j) s[j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], scale, -mc));
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) l_run += (s[h][0] + s[h][1]) + (s[h][2] + s[h][3]);
+    // ---- output
+    if constexpr (sizeof(T) == 2) {
+      bf16x4 pf[2][HALVES];
+#pragma unroll
+      for (int j = 0; j < 4 * HALVES; ++j) {
+        bf16 first, second;
+        two_parts(s[j >> 2][j & 3], first, second);
+        pf[0][j >> 2][j & 3] = first;
+        pf[1][j >> 2][j & 3] = second;
+      }
+#pragma unroll
+      for (int part = 1; part >= 0; --part)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          if constexpr (HALVES == 1) {
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt[0][d], __builtin_bit_cast(s16x4, pf[part][0]), o[d], 0, 0, 0);
+          } else {
+            const bf16x8 both = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0][d], vt[HALVES - 1][d], 0, 1, 2, 3, 4, 5, 6, 7));
+            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, __builtin_shufflevector(pf[part][0], pf[part][HALVES - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[d], 0, 0, 0);
+          }
+        }
+    } else {
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int j = 0; j < HD / 64; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) o[j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[h][j * 4 + e][d], s[h][e], o[j * 4 + d], 0, 0, 0);
+    }
+    if (next < count) {  // over this tile, of which every read has its value by now
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      fill();
+    }
+  }
+
+  // ---- the wavefronts' results, in their order
+  l_run = exchange<16, 32>(l_run, Add{});
+  __shared__ float sm_m[NW][16], sm_l[NW][16];
+  __syncthreads();  // nobody reads tiles any more
+  float* sm_o = reinterpret_cast<float*>(smem);
+  if (lg == 0) {
+    sm_m[wave][lr] = m_run;
+    sm_l[wave][lr] = l_run;
+  }
+  if (lr < cols)
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+      *reinterpret_cast<f32x4*>(sm_o + (wave * 16 + lr) * (HD + SM_PAD) + dim_of(i)) = f32x4{out_at(i, 0), out_at(i, 1), out_at(i, 2), out_at(i, 3)};
+  __syncthreads();
+  const bool whole = ntile <= per || p.n == 1;  // the sequence is this one piece: its output rows go out
+  const size_t pieces = (size_t)z * batch * hq;
+  for (int i = threadIdx.x; i < cols * (HD / 4); i += THREADS) {
+    const int c = i / (HD / 4), d = i % (HD / 4) * 4;
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, sm_m[w][c]);
+    f32x4 num{0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      // sums without a maximum are zeros, or no numbers
+      const float mw = sm_m[w][c], wt = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mw - m) * scale);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(sm_o + (w * 16 + c) * (HD + SM_PAD) + d);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) num[e] += v[e] * wt;
+      den += sm_l[w][c] * wt;
+    }
+    const size_t row = row0 + c;
+    if (whole) {
+      T4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = from_f<T>(num[e] / den);
+      *reinterpret_cast<T4*>(out + row * HD + d) = v;
+    } else {
+      *reinterpret_cast<f32x4*>(p.o + (pieces + row) * HD + d) = num;
+    }
+    if ((WEIGH || !whole) && d == 0) p.ml[pieces + row] = float2{m, den};
+  }
+}
+
+template <class T, int HD, int TK, int NW, int NB, bool WEIGH>
+void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
+  constexpr int TILES = NW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = NW * 16 * (HD + SM_PAD) * 4;
+  constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
+  static std::atomic<uint64_t> lds_allowed{0};
+  auto kernel = k_paged_mfma<T, HD, TK, NW, NB, WEIGH>;
+  allow_dynamic_lds((const void*)kernel, SMEM, lds_allowed);
+  const int heads = a.hkv * ((a.hq / a.hkv + 15) / 16);
+  int half = 0;
+  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = (long)heads * a.batch <= 2 * CUS ? std::max(1, CUS / heads) : a.batch;
+  kernel<<<dim3(a.batch, heads, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
+                                                           a.batch, p);
+}
+
+#ifndef LS_PAGED_TK
+#define LS_PAGED_TK 16
+#endif
+#ifndef LS_PAGED_NW
+#define LS_PAGED_NW 4
+#endif
+#ifndef LS_PAGED_NB
+#define LS_PAGED_NB 2
+#endif
+
+template <class T, int HD>
+void launch_hd(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
+  constexpr int TK = sizeof(T) == 4 ? 16 : LS_PAGED_TK, NB = LS_PAGED_NB;
+  if (a.weights) launch_kernel_of<T, HD, TK, LS_PAGED_NW, NB, true>(a, p, most, st);
+  else launch_kernel_of<T, HD, TK, LS_PAGED_NW, NB, false>(a, p, most, st);
+}
+
+}  // namespace
+
+void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
+  if (dt == F32) {
+    if (a.hd == 128) launch_hd<float, 128>(a, p, most, st);
+    else launch_hd<float, 64>(a, p, most, st);
+  } else {
+    if (a.hd == 128) launch_hd<bf16, 128>(a, p, most, st);
+    else launch_hd<bf16, 64>(a, p, most, st);
+  }
+}
+
+}  // namespace ls
