@@ -26,10 +26,14 @@ __device__ __forceinline__ int fill_len(const FillArgs& a, int b, int& src) {
 template <class U>
 __global__ void __launch_bounds__(256)
 k_paged_fill(FillArgs a, const U* __restrict__ fk, const U* __restrict__ fv, const float* __restrict__ fw, U* __restrict__ kc, U* __restrict__ vc,
-             float* __restrict__ weights, int32_t* __restrict__ places, int blocks) {
+             float* __restrict__ weights, int32_t* __restrict__ places, int32_t* __restrict__ lens, int32_t* __restrict__ positions, int blocks) {
   const int b = blockIdx.y, head = blockIdx.x / blocks, block = blockIdx.x % blocks, layer = head / a.hkv, kh = head % a.hkv;
   int src;
   const int n = fill_len(a, b, src);
+  if (blockIdx.x == 0 && threadIdx.x == 0 && n >= 0) {  // nobody in this launch reads them
+    lens[b] = n;
+    if (positions) positions[b] = n;
+  }
   const int lo = block * 64, hi = block == blocks - 1 ? n : min(lo + 64, n);  // the last one takes what is left
   const size_t from = (((size_t)layer * a.from_batch + src) * a.hkv + kh) * a.from_seq;
   const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
@@ -56,16 +60,6 @@ k_paged_fill(FillArgs a, const U* __restrict__ fk, const U* __restrict__ fv, con
   }
 }
 
-__global__ void __launch_bounds__(256) k_paged_fill_lens(FillArgs a, int32_t* lens, int32_t* positions) {
-  const int b = blockIdx.x * 256 + threadIdx.x;
-  if (b >= a.batch) return;
-  int src;
-  const int n = fill_len(a, b, src);
-  if (n < 0) return;
-  lens[b] = n;
-  if (positions) positions[b] = n;
-}
-
 // ---- eviction ----------------------------------------------------------------------------------------------------------------
 struct EvictArgs {
   PageMap map;
@@ -87,24 +81,188 @@ __device__ __forceinline__ size_t slot_row(const EvictArgs& a, const int32_t* en
   return page_row0(0, a.hkv, kh, a.map.shift) + (((size_t)layer * a.map.pages + entries[slot >> a.map.shift]) * a.hkv << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
 }
 
-// Which slots of a (layer, sequence, kv head) move where.  The key of which `keep` or more slots have as much is searched for bit by bit: as many
-// rounds of counting as it takes until one has exactly `keep`, or all 32.
-__global__ void __launch_bounds__(256) k_evict_choose(EvictArgs a) {
-  const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
-  const int n = a.map.lens[b], pos = a.map.positions ? a.map.positions[b] : n;
+// Slots and positions of a unit's sequence; false if it is left alone, whose entries all threads of the workgroup look at.
+__device__ __forceinline__ bool evict_seq(const EvictArgs& a, int b, int threads, int* bad, int& n, int& from) {
+  n = a.map.lens[b];
+  const int pos = a.map.positions ? a.map.positions[b] : n;
+  from = pos < a.recent ? 0 : pos - a.recent;
+  if (n <= a.keep || n > a.max_len || (n - 1) >> a.map.shift >= a.map.columns) return false;
   const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
-  __shared__ int sums[4], bad;
-  if (threadIdx.x == 0) bad = n <= a.keep || n > a.max_len || (n - 1) >> a.map.shift >= a.map.columns;
+  bool odd = false;
+  for (int i = threadIdx.x; i <= (n - 1) >> a.map.shift; i += threads) odd |= (unsigned)entries[i] >= (unsigned)a.map.pages;
+  if (threads == 64) return __builtin_amdgcn_ballot_w64(odd) == 0;
+  if (threadIdx.x == 0) *bad = 0;
   __syncthreads();
-  if (!bad)
-    for (int i = threadIdx.x; i <= (n - 1) >> a.map.shift; i += 256)
-      if ((unsigned)entries[i] >= (unsigned)a.map.pages) bad = 1;
+  if (odd) *bad = 1;
   __syncthreads();
-  if (bad) {
+  return *bad == 0;
+}
+
+// The moves of a (layer, sequence, kv head) whose keys fit the registers of W wavefronts, V to a lane: wavefront w has the w-th part of the slots,
+// 64 neighbours to a register.  The largest key that `keep` slots or more reach is searched for between the smallest and the largest of the
+// slots that may go, by where it lay if keys were spread evenly and by halves in turn, until exactly `keep` slots reach it or nothing is left
+// between; in the latter case the lower ones of equal keys stay.  Weights and places are read once.
+template <int W, int V>
+__global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
+  const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ int bad, sums[2][W][3];
+  int n, from, turn = 0;
+  if (!evict_seq(a, b, 64 * W, &bad, n, from)) {
     if (threadIdx.x == 0) a.count[unit] = -1;
     return;
   }
-  const int from = pos < a.recent ? 0 : pos - a.recent;
+  // over the workgroup: what each wavefront has, in order
+  auto each = [&](int x, int y, int z) {
+    turn ^= 1;
+    if (lane == 0) {
+      sums[turn][wave][0] = x;
+      sums[turn][wave][1] = y;
+      sums[turn][wave][2] = z;
+    }
+    __syncthreads();
+  };
+  auto total = [&](int x) {
+    if constexpr (W == 1) return x;
+    each(x, 0, 0);
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) all += sums[turn][w][0];
+    return all;
+  };
+  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
+  const int per = (n + 64 * W - 1) / (64 * W), slot0 = wave * per * 64 + lane, mask = (1 << a.map.shift) - 1;
+  const float* weights = a.weights + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
+  const int32_t* places = a.places + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
+  unsigned key[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    key[i] = 0;  // of no slot: below every threshold
+    const int slot = slot0 + i * 64;
+    if (i < per && slot < n) {
+      const size_t row = page_row0(entries[slot >> a.map.shift], a.hkv, kh, a.map.shift) + (slot & mask);
+      key[i] = stay_key(weights[row], places[row], a.first, from);
+    }
+  }
+  unsigned low = 0xFFFFFFFFu, high = 0;
+  int stay = 0;  // slots that stay whatever their weight
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < per) {
+      const bool there = slot0 + i * 64 < n, free = there && key[i] != 0xFFFFFFFFu;
+      low = min(low, free ? key[i] : 0xFFFFFFFFu);
+      high = max(high, free ? key[i] : 0u);
+      stay += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && !free));
+    }
+  for (int off = 32; off; off >>= 1) {
+    low = min(low, (unsigned)__shfl_xor((int)low, off));
+    high = max(high, (unsigned)__shfl_xor((int)high, off));
+  }
+  if constexpr (W > 1) {
+    each((int)low, (int)high, stay);
+    low = 0xFFFFFFFFu;
+    high = stay = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      low = min(low, (unsigned)sums[turn][w][0]);
+      high = max(high, (unsigned)sums[turn][w][1]);
+      stay += sums[turn][w][2];
+    }
+  }
+  // `reach` slots have at least `least`, `keep` or more of them; fewer than `keep`, `above`, have `beyond` or more
+  unsigned least = low, beyond = high + 1;
+  int reach = n, above = stay;
+  if (stay >= a.keep) {
+    least = 0xFFFFFFFFu;
+    reach = stay;
+    above = 0;
+  }
+  bool even = true;
+  while (reach != a.keep && beyond - least > 1 && stay < a.keep) {
+    const unsigned range = beyond - least;
+    unsigned step = range >> 1;
+    if (even) step = min(max((unsigned)((float)range * ((float)(reach - a.keep) / (float)(reach - above))), 1u), range - 1);
+    even = !even;
+    const unsigned middle = least + step;
+    int got = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < per) got += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] >= middle));
+    got = total(got);
+    if (got >= a.keep) {
+      least = middle;
+      reach = got;
+    } else {
+      beyond = middle;
+      above = got;
+    }
+  }
+  // ---- holes and movers in the order of slots
+  const bool ties = reach != a.keep;  // of the slots of key `least`, keep - above stay
+  int rank = 0;
+  if (ties) {
+    int equal = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < per) equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(slot0 + i * 64 < n && key[i] == least));
+    if constexpr (W > 1) {
+      each(equal, 0, 0);
+      for (int w = 0; w < wave; ++w) rank += sums[turn][w][0];
+    }
+  }
+  const uint64_t below = (1ull << lane) - 1;
+  uint64_t kept = 0;  // bit i: slot i of this lane
+  int holes = 0, movers = 0;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < per) {
+      const int slot = slot0 + i * 64;
+      bool stays = slot < n && key[i] >= least;
+      if (ties) {
+        const uint64_t equal = __builtin_amdgcn_ballot_w64(slot < n && key[i] == least);
+        if (slot < n && key[i] == least) stays = rank + __builtin_popcountll(equal & below) < a.keep - above;
+        rank += __builtin_popcountll(equal);
+      }
+      kept |= (uint64_t)stays << i;
+      holes += __builtin_popcountll(__builtin_amdgcn_ballot_w64(slot < a.keep && !stays));
+      movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(slot >= a.keep && stays));
+    }
+  int to = 0, fr = 0, all = movers;
+  if constexpr (W > 1) {
+    each(holes, movers, 0);
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      to += w < wave ? sums[turn][w][0] : 0;
+      fr += w < wave ? sums[turn][w][1] : 0;
+      all += sums[turn][w][1];
+    }
+  }
+  int2* moves = a.moves + (size_t)unit * a.most;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < per) {
+      const int slot = slot0 + i * 64;
+      const bool stays = kept >> i & 1, hole = slot < a.keep && !stays, mover = slot >= a.keep && stays;
+      const uint64_t hs = __builtin_amdgcn_ballot_w64(hole), ms = __builtin_amdgcn_ballot_w64(mover);
+      if (hole) moves[to + __builtin_popcountll(hs & below)].x = slot;
+      if (mover) moves[fr + __builtin_popcountll(ms & below)].y = slot;
+      to += __builtin_popcountll(hs);
+      fr += __builtin_popcountll(ms);
+    }
+  if (threadIdx.x == 0) a.count[unit] = all;
+}
+
+// The same for sequences of any length: keys are made again for each count, bit by bit.
+__global__ void __launch_bounds__(256) k_evict_choose_long(EvictArgs a) {
+  const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
+  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
+  __shared__ int sums[4], bad;
+  int n, from;
+  if (!evict_seq(a, b, 256, &bad, n, from)) {
+    if (threadIdx.x == 0) a.count[unit] = -1;
+    return;
+  }
   auto key_of = [&](int slot) {
     const size_t row = slot_row(a, entries, layer, kh, slot);
     return stay_key(a.weights[row], a.places[row], a.first, from);
@@ -172,6 +330,13 @@ __global__ void __launch_bounds__(256) k_evict_choose(EvictArgs a) {
     if (mover) moves[fr].y = slot;
   }
   if (threadIdx.x == 0) a.count[unit] = from0;
+}
+
+void launch_evict_choose(const EvictArgs& a, size_t units, hipStream_t st) {
+  if (a.max_len <= 64 * 32) k_evict_choose<1, 32><<<units, 64, 0, st>>>(a);
+  else if (a.max_len <= 256 * 32) k_evict_choose<4, 32><<<units, 256, 0, st>>>(a);
+  else if (a.max_len <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a);
+  else k_evict_choose_long<<<units, 256, 0, st>>>(a);
 }
 
 // The moves: a thread to a U-sized piece of a row.  The lengths, which the launch before reads, are set by one workgroup of a sequence.
@@ -331,11 +496,10 @@ ls_status ls_paged_fill(const ls_heads* h, int layers, const ls_kv* from, int fr
   const dim3 grid(a.heads * blocks, batch);
   if (wide)
     ls::k_paged_fill<ls::u32x4><<<grid, 256, 0, st>>>(a, (const ls::u32x4*)from->k, (const ls::u32x4*)from->v, weights, (ls::u32x4*)pages->k, (ls::u32x4*)pages->v,
-                                                  pages->weights, pages->places, blocks);
+                                                  pages->weights, pages->places, pages->lens, pages->positions, blocks);
   else
     ls::k_paged_fill<uint32_t><<<grid, 256, 0, st>>>(a, (const uint32_t*)from->k, (const uint32_t*)from->v, weights, (uint32_t*)pages->k, (uint32_t*)pages->v,
-                                                     pages->weights, pages->places, blocks);
-  ls::k_paged_fill_lens<<<(batch + 255) / 256, 256, 0, st>>>(a, pages->lens, pages->positions);
+                                                     pages->weights, pages->places, pages->lens, pages->positions, blocks);
   return launched(who);
 }
 
@@ -371,7 +535,7 @@ ls_status ls_paged_evict(const ls_heads* h, int layers, const ls_pages* pages, i
   a.count = (int32_t*)scratch;
   a.moves = (int2*)((char*)scratch + (units * 4 + 15) / 16 * 16);
   hipStream_t st = (hipStream_t)hip_stream;
-  ls::k_evict_choose<<<units, 256, 0, st>>>(a);
+  ls::launch_evict_choose(a, units, st);
   const dim3 grid(units, std::min(std::max((int)(((int64_t)a.most * pieces + 1023) / 1024), 1), 64));
   if (wide)
     ls::k_evict_move<ls::u32x4><<<grid, 256, 0, st>>>(a, (ls::u32x4*)pages->k, (ls::u32x4*)pages->v, pages->weights, pages->places, pages->lens, pieces);

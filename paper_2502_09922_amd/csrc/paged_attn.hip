@@ -175,44 +175,95 @@ __device__ __forceinline__ float2 joined(const float2* __restrict__ ml, size_t s
   return float2{m, den};
 }
 
-// The pieces' results, and the slots' weights.  Workgroups [0, out_blocks) of a sequence take its output, 256 dims each, the others a kv
-// head's 256 slots each.
-template <class T>
+// The pieces' results, and the slots' weights.  Workgroups [0, out_blocks) of a sequence take its output, D dims to a thread, the others 256 slots
+// of a kv head each, whose query heads' maxima and sums they join first.
+template <class T, int D>
 __global__ void __launch_bounds__(256)
 k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int batch, int hq, int hkv, int hd, int max_pos, bool turns, int most, PagedPieces p,
              int out_blocks) {
+  typedef T TD __attribute__((ext_vector_type(D), aligned(sizeof(T))));  // a row may start anywhere
+  typedef float FD __attribute__((ext_vector_type(D)));
+  constexpr int U = 8;  // pieces, or heads, on their way at once
   const int b = blockIdx.y;
-  PagedSeq t;
-  if (!paged_seq(map, b, max_pos, turns, most, t)) return;
-  const int keys = t.n + 1, n = min((keys + p.keys - 1) / p.keys, p.n);
   const size_t step = (size_t)batch * hq;
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
+  PagedSeq t;
   if ((int)blockIdx.x < out_blocks) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (n == 1 || i >= hq * hd) return;  // one piece writes the output itself
+    const int i = min((int)(blockIdx.x * 256 + threadIdx.x), hq * hd / D - 1) * D, d = i % hd;
     const size_t row = (size_t)b * hq + i / hd;
-    const float2 all = joined(p.ml + row, step, n, scale);
-    float num = 0.f;
-    for (int z = 0; z < n; ++z) {
-      const float mz = p.ml[row + z * step].x;
-      num += p.o[(row + z * step) * hd + i % hd] * (mz == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mz - all.x) * scale));
+    float2 ml[U];
+    FD v[U];
+    auto load = [&](int z0) {  // the first of them before it is known how many there are
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const size_t at = row + min(z0 + u, p.n - 1) * step;
+        ml[u] = p.ml[at];
+        v[u] = *reinterpret_cast<const FD*>(p.o + at * hd + d);
+      }
+    };
+    load(0);
+    if (!paged_seq(map, b, max_pos, turns, most, t)) return;
+    const int n = min((t.n + p.keys) / p.keys, p.n);
+    if (n == 1) return;  // one piece writes the output itself
+    float m = -INFINITY, den = 0.f;
+    FD num = 0.f;
+    for (int z0 = 0; z0 < n; z0 += U) {
+      if (z0) load(z0);
+      float top = m;
+#pragma unroll
+      for (int u = 0; u < U; ++u) top = z0 + u < n ? fmaxf(top, ml[u].x) : top;
+      const float corr = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale);  // sums without a maximum are zeros, or no numbers
+      den *= corr;
+      num *= corr;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (z0 + u < n) {
+          const float wt = ml[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml[u].x - top) * scale);
+#pragma unroll
+          for (int e = 0; e < D; ++e) num[e] += v[u][e] * wt;
+          den += ml[u].y * wt;
+        }
+      m = top;
     }
-    out[row * hd + i % hd] = from_f<T>(num / all.y);
+    TD w;
+#pragma unroll
+    for (int e = 0; e < D; ++e) w[e] = from_f<T>(num[e] / den);
+    *reinterpret_cast<TD*>(out + row * hd + d) = w;
     return;
   }
-  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, slot = item % blocks * 256 + threadIdx.x, G = hq / hkv;
-  if (item % blocks * 256 >= keys) return;
+  if (!paged_seq(map, b, max_pos, turns, most, t)) return;
+  const int keys = t.n + 1, n = min((t.n + p.keys) / p.keys, p.n);
+  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, first = item % blocks * 256, slot = first + threadIdx.x, G = hq / hkv;
+  if (first >= keys) return;
+  const int page = slot < keys ? map.table[(size_t)b * map.columns + (slot >> map.shift)] : -1;
+  const bool there = (unsigned)page < (unsigned)map.pages;
+  const size_t at = page_row0(there ? page : 0, hkv, kh, map.shift) + (slot & ((1 << map.shift) - 1));
+  const float had = there && slot != t.n ? weights[at] : 0.f;
+  __shared__ float2 heads[64];  // maximum, 1 / sum
   float got = 0.f;
-  for (int g = 0; g < G; ++g) {
-    const size_t row = (size_t)b * hq + kh * G + g;
-    const float2 all = joined(p.ml + row, step, n, scale);
-    if (slot < keys) got += __builtin_amdgcn_exp2f((p.scores[row * p.stride + slot] - (all.x == -INFINITY ? 0.f : all.x)) * scale) / all.y;
+  for (int g0 = 0; g0 < G; g0 += 64) {
+    const size_t row = (size_t)b * hq + kh * G + g0;
+    const int count = min(64, G - g0);
+    float s[U];
+    auto load = [&](int g) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) s[u] = p.scores[(row + min(g + u, count - 1)) * p.stride + min(slot, keys - 1)];
+    };
+    load(0);
+    if (g0) __syncthreads();
+    if ((int)threadIdx.x < count) {
+      const float2 all = joined(p.ml + row + threadIdx.x, step, n, scale);
+      heads[threadIdx.x] = float2{all.x == -INFINITY ? 0.f : all.x, 1.f / all.y};
+    }
+    __syncthreads();
+    for (int g = 0; g < count; g += U) {
+      if (g) load(g);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (g + u < count) got += __builtin_amdgcn_exp2f((s[u] - heads[g + u].x) * scale) * heads[g + u].y;
+    }
   }
-  if (slot >= keys) return;
-  const int page = map.table[(size_t)b * map.columns + (slot >> map.shift)];
-  if ((unsigned)page >= (unsigned)map.pages) return;
-  const size_t at = page_row0(page, hkv, kh, map.shift) + (slot & ((1 << map.shift) - 1));
-  weights[at] = slot == t.n ? got : weights[at] + got;
+  if (there) weights[at] = had + got;
 }
 
 template <class T>
@@ -273,12 +324,13 @@ void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st) {
   else if (dt == F32) launch_any<float>(a, p, most, st);
   else launch_any<bf16>(a, p, most, st);
   if (p.n == 1 && !a.weights) return;
-  const int out_blocks = p.n > 1 ? (a.hq * a.hd + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;
+  const int D = a.hd % 4 ? 2 : 4, out_blocks = p.n > 1 ? (a.hq * a.hd / D + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;
   const dim3 grid(out_blocks + slots, a.batch);
-  if (dt == F32)
-    k_paged_join<float><<<grid, 256, 0, st>>>(a.map, (float*)a.out, a.weights, a.batch, a.hq, a.hkv, a.hd, a.max_pos, a.cs != nullptr, most, p, out_blocks);
-  else
-    k_paged_join<bf16><<<grid, 256, 0, st>>>(a.map, (bf16*)a.out, a.weights, a.batch, a.hq, a.hkv, a.hd, a.max_pos, a.cs != nullptr, most, p, out_blocks);
+  auto join = [&](auto* kernel, auto* out) {
+    kernel<<<grid, 256, 0, st>>>(a.map, out, a.weights, a.batch, a.hq, a.hkv, a.hd, a.max_pos, a.cs != nullptr, most, p, out_blocks);
+  };
+  if (dt == F32) join(D == 4 ? k_paged_join<float, 4> : k_paged_join<float, 2>, (float*)a.out);
+  else join(D == 4 ? k_paged_join<bf16, 4> : k_paged_join<bf16, 2>, (bf16*)a.out);
 }
 
 namespace {
