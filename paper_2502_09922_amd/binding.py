@@ -321,7 +321,7 @@ class PagedCache:
     page], both or none.  positions None: nothing is ever evicted.  The tensors are the caller's, who fills table and may write
     the others between calls; the attributes stay the tensors that were given."""
 
-    __slots__ = ("_t", "_layers", "_all", "_heads", "device", "batch")
+    __slots__ = ("_t", "_layers", "_all", "_heads", "_call", "device", "batch")
 
     def __init__(self, k, v, table, lens, positions=None, weights=None, places=None):
         device = _gpu(k)
@@ -348,7 +348,7 @@ class PagedCache:
         self._layers = [ls_pages(*[p if p is None or i > 3 else p + n * rows[i] for i, p in enumerate(at)], pages, page, table.shape[1]) for n in range(layers)]
         self._all = ls_pages(*at, pages, page, table.shape[1])
         self._t = dict(k=k, v=v, table=table, lens=lens, positions=positions, weights=weights, places=places)
-        self._heads, self.device, self.batch = {}, device, table.shape[0]
+        self._heads, self._call, self.device, self.batch = {}, None, device, table.shape[0]
 
     def __getattr__(self, name):
         try:
@@ -366,6 +366,19 @@ class PagedCache:
         return h
 
 
+    def attention_call(self, columns: int, max_seq: int, max_ctx: int):
+        """(n_q_heads, ls_heads, scratch bytes) of an attention call over rows of so many columns: of one size step after step."""
+        if self._call is None or self._call[0] != (columns, max_seq, max_ctx):
+            k = self._t["k"]
+            hkv, hd = k.shape[2], k.shape[4]
+            if columns % hd or columns // hd <= 2 * hkv:
+                raise ValueError("qkv: [%d, (n_q_heads + %d) * %d] is wanted" % (self.batch, 2 * hkv, hd))
+            hq = columns // hd - 2 * hkv
+            heads = self.heads(hq, max_seq)
+            self._call = ((columns, max_seq, max_ctx), (hq, heads, lib.ls_paged_attention_scratch_bytes(heads, self._all, self.batch, max_ctx)))
+        return self._call[1]
+
+
 def _scratch(nb, device):
     return torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
 
@@ -374,22 +387,22 @@ def paged_attention(cache: PagedCache, qkv, rope, max_ctx: int, layer: int = 0, 
     """Attention of one layer for a new token of each sequence (ls_paged_attention), which takes slot lens[b] of the cache; qkv [sequences,
     (n_q_heads + 2 n_kv_heads) * head_dim]; rope: float32 [positions, head_dim/2, 2] or None; max_ctx: a bound of lens.  lens and
     positions stay: add one to both behind the last layer.  Returns [sequences, n_q_heads * head_dim]."""
-    device, k = cache.device, cache._t["k"]
-    hkv, hd, rows = k.shape[2], k.shape[4], cache.batch
-    if qkv.dim() != 2 or qkv.shape[0] != rows or qkv.shape[1] % hd or qkv.shape[1] // hd <= 2 * hkv:
-        raise ValueError("qkv: [%d, (n_q_heads + %d) * %d] is wanted" % (rows, 2 * hkv, hd))
-    if not 0 <= layer < k.shape[0]:
-        raise ValueError("layer: one of %d is wanted" % k.shape[0])
-    hq = qkv.shape[1] // hd - 2 * hkv
-    heads, pages = cache.heads(hq, 1 << 24 if rope is None else rope.shape[0]), cache._layers[layer]
+    device, k, rows = cache.device, cache._t["k"], cache.batch
+    if qkv.dim() != 2 or qkv.shape[0] != rows:
+        raise ValueError("qkv: %d rows are wanted" % rows)
+    hq, heads, nb = cache.attention_call(qkv.shape[1], 1 << 24 if rope is None else rope.shape[0], max_ctx)
+    if not 0 <= layer < len(cache._layers):
+        raise ValueError("layer: one of %d is wanted" % len(cache._layers))
+    hd = k.shape[4]
     q = _tensor("qkv", qkv, k.dtype, device)
     turn = None if rope is None else _tensor("rope", rope, torch.float32, device, rope.shape[0] * hd)
     if out is None:
         out = torch.empty(rows, hq * hd, dtype=k.dtype, device=device)
-    to = _tensor("out", out, k.dtype, device, rows * hq * hd)
-    nb = lib.ls_paged_attention_scratch_bytes(heads, pages, rows, max_ctx)
-    scratch = _scratch(nb, device)
-    _run(device, lib.ls_paged_attention, heads, pages, rows, max_ctx, q, turn, to, scratch.data_ptr() if nb else None, nb)
+        to = out.data_ptr()
+    else:
+        to = _tensor("out", out, k.dtype, device, rows * hq * hd)
+    scratch = torch.empty(nb, dtype=torch.uint8, device=device) if nb else None
+    _run(device, lib.ls_paged_attention, heads, cache._layers[layer], rows, max_ctx, q, turn, to, scratch.data_ptr() if nb else None, nb)
     return out
 
 
@@ -580,8 +593,7 @@ class Stage:
                 (k.shape[0], k.shape[2], k.shape[4]) != (self.hi - self.lo, self.cfg.n_kv_heads, self.cfg.head_dim)):
             raise ValueError("cache: pools of the stage's type, layers, heads and device are wanted")
         x = _tensor("inp", inp, torch.int32 if self.first else self.tdtype, device, rows if self.first else rows * self.shape.hidden)
-        heads = cache.heads(self.cfg.n_q_heads, self.cfg.max_seq)
-        nb = lib.ls_paged_attention_scratch_bytes(heads, cache._all, rows, max_ctx)
+        _, _, nb = cache.attention_call((self.cfg.n_q_heads + 2 * self.cfg.n_kv_heads) * self.cfg.head_dim, self.cfg.max_seq, max_ctx)
 
         def call(out, logits, st):
             scratch = _scratch(nb, device)

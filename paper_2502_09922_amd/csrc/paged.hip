@@ -135,13 +135,26 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
   const float* weights = a.weights + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
   const int32_t* places = a.places + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
   unsigned key[V];
+  constexpr int AT_ONCE = V < 16 ? V : 16;  // on their way together; slots that are not there read the last one
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    key[i] = 0;  // of no slot: below every threshold
-    const int slot = slot0 + i * 64;
-    if (i < per && slot < n) {
-      const size_t row = page_row0(entries[slot >> a.map.shift], a.hkv, kh, a.map.shift) + (slot & mask);
-      key[i] = stay_key(weights[row], places[row], a.first, from);
+  for (int i0 = 0; i0 < V; i0 += AT_ONCE) {
+    size_t row[AT_ONCE];
+    float w[AT_ONCE];
+    int place[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int slot = min(slot0 + (i0 + j) * 64, n - 1);
+      row[j] = page_row0(entries[slot >> a.map.shift], a.hkv, kh, a.map.shift) + (slot & mask);
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      w[j] = weights[row[j]];
+      place[j] = places[row[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int i = i0 + j;  // a key of 0 is below every threshold
+      key[i] = i < per && slot0 + i * 64 < n ? stay_key(w[j], place[j], a.first, from) : 0;
     }
   }
   unsigned low = 0xFFFFFFFFu, high = 0;
@@ -333,9 +346,21 @@ __global__ void __launch_bounds__(256) k_evict_choose_long(EvictArgs a) {
 }
 
 void launch_evict_choose(const EvictArgs& a, size_t units, hipStream_t st) {
-  if (a.max_len <= 64 * 32) k_evict_choose<1, 32><<<units, 64, 0, st>>>(a);
-  else if (a.max_len <= 256 * 32) k_evict_choose<4, 32><<<units, 256, 0, st>>>(a);
-  else if (a.max_len <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a);
+#ifdef LS_EVICT_FEW
+  const bool few = units <= LS_EVICT_FEW;
+#else
+  const bool few = units <= 512;
+#endif
+  const int n = a.max_len;
+  if (n <= 64 * 8) k_evict_choose<1, 8><<<units, 64, 0, st>>>(a);
+  else if (n <= 64 * 16 && !few) k_evict_choose<1, 16><<<units, 64, 0, st>>>(a);
+  else if (n <= 64 * 32 && !few) k_evict_choose<1, 32><<<units, 64, 0, st>>>(a);
+  else if (n <= 256 * 8) k_evict_choose<4, 8><<<units, 256, 0, st>>>(a);
+  else if (n <= 256 * 16) k_evict_choose<4, 16><<<units, 256, 0, st>>>(a);
+  else if (n <= 256 * 32 && !few) k_evict_choose<4, 32><<<units, 256, 0, st>>>(a);
+  else if (n <= 1024 * 8) k_evict_choose<16, 8><<<units, 1024, 0, st>>>(a);
+  else if (n <= 1024 * 16) k_evict_choose<16, 16><<<units, 1024, 0, st>>>(a);
+  else if (n <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a);
   else k_evict_choose_long<<<units, 256, 0, st>>>(a);
 }
 

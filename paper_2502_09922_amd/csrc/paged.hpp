@@ -38,6 +38,8 @@ struct PagedPieces {
 };
 void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
 
+bool paged_joins_weights(const PagedAttn& a, const PagedPieces& p);  // by itself, without a join behind it
+
 struct PagedSeq {
   int n, pos, page;  // slot and position of the new token, the slot's page
 };

@@ -10,6 +10,13 @@
 
 #include <algorithm>
 
+#ifndef LS_PAGED_WGS
+#define LS_PAGED_WGS 256
+#endif
+#ifndef LS_ONE
+#define LS_ONE 640
+#endif
+
 namespace ls {
 
 namespace {
@@ -282,8 +289,9 @@ bool fast(const PagedAttn& a) {
 PagedPieces pieces_for(const PagedAttn& a) {
   PagedPieces p;
   const bool mfma = fast(a);
-  const long base = mfma ? (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) : (long)a.batch * a.hq, target = mfma ? 512 : 4096;
-  const long want = std::min(std::max(target / base, 1l), (a.max_keys + 127l) / 128);
+  const long base = mfma ? (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) : (long)a.batch * a.hq, target = mfma ? LS_PAGED_WGS : 4096;
+  long want = std::min(std::max(target / base, 1l), (a.max_keys + 127l) / 128);
+  if (mfma && a.max_keys <= LS_ONE) want = 1;
   p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
   p.n = (a.max_keys + p.keys - 1) / p.keys;
   return p;
@@ -323,7 +331,7 @@ void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st) {
   if (fast(a)) launch_paged_attn_mfma(dt, a, p, most, st);
   else if (dt == F32) launch_any<float>(a, p, most, st);
   else launch_any<bf16>(a, p, most, st);
-  if (p.n == 1 && !a.weights) return;
+  if (p.n == 1 && (!a.weights || (fast(a) && paged_joins_weights(a, p)))) return;
   const int D = a.hd % 4 ? 2 : 4, out_blocks = p.n > 1 ? (a.hq * a.hd / D + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;
   const dim3 grid(out_blocks + slots, a.batch);
   auto join = [&](auto* kernel, auto* out) {

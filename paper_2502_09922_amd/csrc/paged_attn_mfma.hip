@@ -33,7 +33,7 @@ constexpr int CUS = 256;
 template <class T, int HD, int TK, int NW, int NB, bool WEIGH>
 __global__ void __launch_bounds__(64 * NW, 2)
 k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, int32_t* __restrict__ places,
-             T* __restrict__ out, int hq, int hkv, int max_pos, int most, int half, int batch, PagedPieces p) {
+             T* __restrict__ out, int hq, int hkv, int max_pos, int most, int half, int batch, PagedPieces p, float* __restrict__ weights) {
   constexpr int THREADS = 64 * NW;
   constexpr int ROWB = HD * sizeof(T), EPC = 16 / sizeof(T);
   constexpr int CPR = HD / EPC;    // 16-byte chunks of a row
@@ -97,8 +97,9 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   auto fill = [&] {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-    auto piece = [](const T* base, unsigned off, unsigned to) {
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+    auto piece = [](auto once, const T* base, unsigned off, unsigned to) {
+      if constexpr (decltype(once)::value) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
     };
 #pragma clang diagnostic pop
     const int key0 = (t_lo + wave + next * NW) * TK;
@@ -113,11 +114,17 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       kt[u] = kc + row * HD;
       vt[u] = vc + row * HD;
     }
+    // What one block of columns reads once does not stay in L2: 13B, 32 sequences 120 -> 106 us, 70B, 64 ragged 76 -> 66 (32 heads over one,
+    // 64 sequences of 2000 slots, which two blocks read: 21 and 24).
+    auto all = [&](auto once) {
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      piece(kt[i * RPI / 8], koff[i], to + i * 1024);
-      piece(vt[i * RPI / 8], voff[i], to + TILE + i * 1024);
-    }
+      for (int i = 0; i < NL; ++i) {
+        piece(once, kt[i * RPI / 8], koff[i], to + i * 1024);
+        piece(once, vt[i * RPI / 8], voff[i], to + TILE + i * 1024);
+      }
+    };
+    if (blocks == 1) all(std::true_type{});
+    else all(std::false_type{});
     ++next;
     look_up(next);
   };
@@ -351,6 +358,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   // ---- the wavefronts' results, in their order
   l_run = exchange<16, 32>(l_run, Add{});
   __shared__ float sm_m[NW][16], sm_l[NW][16];
+  __shared__ float2 sm_all[16];  // maximum, 1 / sum
   __syncthreads();  // nobody reads tiles any more
   float* sm_o = reinterpret_cast<float*>(smem);
   if (lg == 0) {
@@ -389,13 +397,36 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     } else {
       *reinterpret_cast<f32x4*>(p.o + (pieces + row) * HD + d) = num;
     }
-    if ((WEIGH || !whole) && d == 0) p.ml[pieces + row] = float2{m, den};
+    if (d == 0) {
+      if (WEIGH && weights) sm_all[c] = float2{m == -INFINITY ? 0.f : m, 1.f / den};
+      else if (WEIGH || !whole) p.ml[pieces + row] = float2{m, den};
+    }
+  }
+  if constexpr (WEIGH) {  // the weights of all slots, where one workgroup has all of them and all of the query heads
+    if (!weights) return;
+    __syncthreads();  // the scores of all wavefronts are in memory
+    for (int slot = threadIdx.x; slot < keys; slot += THREADS) {
+      constexpr int U = 8;  // heads on their way at once
+      const int at = map.table[(size_t)b * map.columns + (slot >> map.shift)];
+      const bool there = (unsigned)at < (unsigned)map.pages;
+      const size_t to = page_row0(there ? at : 0, hkv, kh, map.shift) + (slot & mask);
+      float got = there && slot != t.n ? weights[to] : 0.f;
+      for (int c0 = 0; c0 < cols; c0 += U) {
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = p.scores[(row0 + min(c0 + u, cols - 1)) * p.stride + slot];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c0 + u < cols) got += __builtin_amdgcn_exp2f((v[u] - sm_all[c0 + u].x) * scale) * sm_all[c0 + u].y;
+      }
+      if (there) weights[to] = got;
+    }
   }
 }
 
-template <class T, int HD, int TK, int NW, int NB, bool WEIGH>
+template <class T, int HD, int NW, int NB, bool WEIGH>
 void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
-  constexpr int TILES = NW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = NW * 16 * (HD + SM_PAD) * 4;
+  constexpr int TK = 16, TILES = NW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = NW * 16 * (HD + SM_PAD) * 4;
   constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
   static std::atomic<uint64_t> lds_allowed{0};
   auto kernel = k_paged_mfma<T, HD, TK, NW, NB, WEIGH>;
@@ -404,27 +435,41 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
   int half = 0;
   if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = (long)heads * a.batch <= 2 * CUS ? std::max(1, CUS / heads) : a.batch;
   kernel<<<dim3(a.batch, heads, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
-                                                           a.batch, p);
+                                                           a.batch, p, paged_joins_weights(a, p) ? a.weights : nullptr);
 }
 
-#ifndef LS_PAGED_TK
-#define LS_PAGED_TK 16
+#ifndef LS_BIG
+#define LS_BIG 4, 2
 #endif
-#ifndef LS_PAGED_NW
-#define LS_PAGED_NW 4
+#ifndef LS_SMALL
+#define LS_SMALL 8, 2
 #endif
-#ifndef LS_PAGED_NB
-#define LS_PAGED_NB 2
+#ifndef LS_FBIG
+#define LS_FBIG 4, 1
+#endif
+#ifndef LS_FSMALL
+#define LS_FSMALL 8, 1
+#endif
+#ifndef LS_LIMIT
+#define LS_LIMIT 256
 #endif
 
 template <class T, int HD>
 void launch_hd(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
-  constexpr int TK = sizeof(T) == 4 ? 16 : LS_PAGED_TK, NB = LS_PAGED_NB;
-  if (a.weights) launch_kernel_of<T, HD, TK, LS_PAGED_NW, NB, true>(a, p, most, st);
-  else launch_kernel_of<T, HD, TK, LS_PAGED_NW, NB, false>(a, p, most, st);
+  const bool alone = (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) * p.n <= LS_LIMIT;
+  if constexpr (sizeof(T) * HD == 512) {
+    if (a.weights) alone ? launch_kernel_of<T, HD, LS_FSMALL, true>(a, p, most, st) : launch_kernel_of<T, HD, LS_FBIG, true>(a, p, most, st);
+    else alone ? launch_kernel_of<T, HD, LS_FSMALL, false>(a, p, most, st) : launch_kernel_of<T, HD, LS_FBIG, false>(a, p, most, st);
+  } else {
+    if (a.weights) alone ? launch_kernel_of<T, HD, LS_SMALL, true>(a, p, most, st) : launch_kernel_of<T, HD, LS_BIG, true>(a, p, most, st);
+    else alone ? launch_kernel_of<T, HD, LS_SMALL, false>(a, p, most, st) : launch_kernel_of<T, HD, LS_BIG, false>(a, p, most, st);
+  }
 }
 
 }  // namespace
+
+// Whether the attention kernel adds the weights up itself.
+bool paged_joins_weights(const PagedAttn& a, const PagedPieces& p) { return a.weights && p.n == 1 && a.hq / a.hkv <= 16; }
 
 void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
   if (dt == F32) {
