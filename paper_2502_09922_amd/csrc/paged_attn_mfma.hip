@@ -59,29 +59,42 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const size_t row0 = (size_t)b * hq + kh * G + cb * 16;  // output row of column 0
+  // Nothing in the launch writes lengths, positions and table: scalar loads, which do not queue behind the tiles on their way.  The
+  // first tile's pages and the queries are asked for before the length is known.
+  typedef const __attribute__((address_space(4))) int32_t fixed;
   PagedSeq t;
-  if (!paged_seq(map, b, max_pos, cs != nullptr, most, t)) {  // the rows hold zeros
-    if (z == 0)
-      for (int i = threadIdx.x; i < cols * HD; i += THREADS) out[row0 * HD + i] = from_f<T>(0.f);
-    return;
-  }
-  const int keys = t.n + 1, ntile = (keys + TK - 1) / TK, per = p.keys / TK;
-  const int t_lo = z * per;
-  if (t_lo >= ntile) return;
-  const int t_hi = z == p.n - 1 ? ntile : min(t_lo + per, ntile);  // the last piece takes what is left
-  const int count = max(0, (t_hi - t_lo - wave + NW - 1) / NW);    // tiles of this wavefront: t_lo + wave, NW further each time
-  const int mask = (1 << map.shift) - 1, last_entry = t.n >> map.shift;
-  // Nothing in the launch writes the table: scalar loads, which do not queue behind the tiles on their way.
-  typedef const __attribute__((address_space(4))) int32_t entry;
-  const entry* entries = (const entry*)(uintptr_t)(map.table + (size_t)b * map.columns);
-  const int lrow = lane / CPR, lchunk = lane % CPR;
-
-  // ---- the ring
+  t.n = ((fixed*)(uintptr_t)map.lens)[b];
+  t.pos = map.positions ? ((fixed*)(uintptr_t)map.positions)[b] : t.n;
+  fixed* entries = (fixed*)(uintptr_t)(map.table + (size_t)b * map.columns);
+  const int per = p.keys / TK, t_lo = z * per, mask = (1 << map.shift) - 1;
   int page[UNITS];  // of the tile that is filled next
   auto look_up = [&](int i) {
 #pragma unroll
-    for (int u = 0; u < UNITS; ++u) page[u] = entries[min(((t_lo + wave + i * NW) * TK + 8 * u) >> map.shift, last_entry)];
+    for (int u = 0; u < UNITS; ++u) page[u] = entries[min(((t_lo + wave + i * NW) * TK + 8 * u) >> map.shift, map.columns - 1)];
   };
+  look_up(0);
+  constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a row
+  const T* rows = qkv + (size_t)b * (hq + 2 * hkv) * HD;
+  const T* q = rows + (size_t)(kh * G + cb * 16 + min(lr, cols - 1)) * HD;  // columns behind the last are its copies
+  u32x4 raw[KS];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk) raw[kk] = *reinterpret_cast<const u32x4*>(q + (kk * 4 + lg) * EPC);
+  auto no_room = [&] {  // the rows hold zeros
+    if (z == 0)
+      for (int i = threadIdx.x; i < cols * HD; i += THREADS) out[row0 * HD + i] = from_f<T>(0.f);
+  };
+  if (t.n < 0 || t.n >= most || t.n >> map.shift >= map.columns || t.pos < 0 || (cs && t.pos >= max_pos)) {
+    no_room();
+    return;
+  }
+  t.page = entries[t.n >> map.shift];
+  const int keys = t.n + 1, ntile = (keys + TK - 1) / TK;
+  if (t_lo >= ntile) return;
+  const int t_hi = z == p.n - 1 ? ntile : min(t_lo + per, ntile);  // the last piece takes what is left
+  const int count = max(0, (t_hi - t_lo - wave + NW - 1) / NW);    // tiles of this wavefront: t_lo + wave, NW further each time
+  const int lrow = lane / CPR, lchunk = lane % CPR;
+
+  // ---- the ring
   unsigned koff[NL], voff[NL];  // a row's piece from the first of its eight rows
 #pragma unroll
   for (int i = 0; i < NL; ++i) {
@@ -128,16 +141,12 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     ++next;
     look_up(next);
   };
-  look_up(0);
-
-  // ---- queries: this wavefront's 16 columns, those behind the last are its copies
-  constexpr int KS = sizeof(T) == 2 ? HD / 32 : HD / 16;  // reads of a row
-  const T* rows = qkv + (size_t)b * (hq + 2 * hkv) * HD;
-  const T* q = rows + (size_t)(kh * G + cb * 16 + min(lr, cols - 1)) * HD;
-  const float* turn = cs + (size_t)t.pos * HD;
-  u32x4 raw[KS];
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk) raw[kk] = *reinterpret_cast<const u32x4*>(q + (kk * 4 + lg) * EPC);
+  for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(raw[kk]));  // waited for here, not behind the tiles
+  while (next < min(count, NB)) fill();
+
+  // ---- queries: this wavefront's 16 columns, turned
+  const float* turn = cs + (size_t)t.pos * HD;
   f32x4 angles[KS][EPC / 4];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk)
@@ -155,7 +164,11 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
 #pragma unroll
       for (int e = 0; e < EPC / 4; ++e) nturn[e] = reinterpret_cast<const f32x4*>(turn + nc * EPC)[e];
   }
-  while (next < min(count, NB)) fill();
+  if ((unsigned)t.page >= (unsigned)map.pages) {
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));  // nothing is on its way into the LDS of whoever comes next
+    no_room();
+    return;
+  }
 
   typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Q;
   Q qh[KS], ql[sizeof(T) == 2 ? KS : 1];
