@@ -28,14 +28,23 @@ size_t paged_attn_scratch_bytes(const PagedAttn& a);
 void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st);
 void launch_paged_next(const PagedAttn& a, int32_t* lens, int32_t* positions, hipStream_t st);  // one more slot and position each
 
-// Pieces of the contexts that workgroups of their own take, and where they leave their results.
+// Pieces of the contexts that workgroups of their own take, and where they leave their results: piece z of the row at `at` has place at + z * step.
+// Dealt out beforehand (share == 0) a piece has `keys` slots of every sequence, at = row * hq + head, step = batch * hq.  Dealt out by the lengths
+// (matrix cores), `share` workgroups get shares of about the same size and a place for 16 columns each: step = 16.
 struct PagedPieces {
+  static constexpr int SEQUENCES = 1024;  // at most, whose lengths a wavefront holds in registers to deal them out
   int n = 1, keys = 0;      // keys of a piece: a multiple of 64
-  float* o = nullptr;       // [piece][row * hq + head][head_dim], not normalised
-  float2* ml = nullptr;     // [piece][row * hq + head]: maximum in units of q k, sum
-  float* scores = nullptr;  // [row * hq + head][stride] q k of every slot, where weights are wanted
-  int stride = 0;
+  int share = 0;
+  float* o = nullptr;       // [place][head_dim], not normalised
+  float2* ml = nullptr;     // [place]: maximum in units of q k, sum
+  int2* dealt = nullptr;    // [sequence]: first workgroup, pieces
+  float* scores = nullptr;  // q k of every slot, where weights are wanted: [sequence][kv head][slot / 16][query head of it][slot % 16]
+  int stride = 0;           // slots of a sequence, a multiple of 32
 };
+// Of query head h, G to a kv head.
+__device__ __forceinline__ size_t score_at(const PagedPieces& p, int b, int hq, int G, int h, int slot) {
+  return ((size_t)b * hq + h / G * G) * p.stride + (size_t)(slot >> 4) * (16 * G) + h % G * 16 + (slot & 15);
+}
 void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
 
 bool paged_joins_weights(const PagedAttn& a, const PagedPieces& p);  // by itself, without a join behind it

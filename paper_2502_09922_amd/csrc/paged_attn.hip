@@ -16,6 +16,9 @@
 #ifndef LS_ONE
 #define LS_ONE 640
 #endif
+#ifndef LS_LONG
+#define LS_LONG 4096
+#endif
 
 namespace ls {
 
@@ -112,7 +115,7 @@ k_paged_attn(PageMap map, const T* __restrict__ qkv, const float2* __restrict__ 
       float mine = 0.f;
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) mine = lane == j ? s[j] : mine;
-      if (lane < AT_ONCE && key0 + lane < hi) p.scores[row * p.stride + key0 + lane] = mine;
+      if (lane < AT_ONCE && key0 + lane < hi) p.scores[score_at(p, b, hq, G, h, key0 + lane)] = mine;
     }
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j)
@@ -191,26 +194,30 @@ k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int 
   typedef T TD __attribute__((ext_vector_type(D), aligned(sizeof(T))));  // a row may start anywhere
   typedef float FD __attribute__((ext_vector_type(D)));
   constexpr int U = 8;  // pieces, or heads, on their way at once
-  const int b = blockIdx.y;
-  const size_t step = (size_t)batch * hq;
+  const int b = blockIdx.y, G = hq / hkv, blocks16 = (G + 15) / 16;
+  const size_t step = p.share ? 16 : (size_t)batch * hq;
+  const int2 dealt = p.share ? p.dealt[b] : int2{0, 0};
+  auto place_of = [&](int h) {  // of a query head's first piece
+    return p.share ? ((size_t)dealt.x + (size_t)(h / G * blocks16 + h % G / 16) * dealt.y) * 16 + h % G % 16 : (size_t)b * hq + h;
+  };
   const float scale = 1.4426950408889634f / sqrtf((float)hd);
   PagedSeq t;
   if ((int)blockIdx.x < out_blocks) {
     const int i = min((int)(blockIdx.x * 256 + threadIdx.x), hq * hd / D - 1) * D, d = i % hd;
-    const size_t row = (size_t)b * hq + i / hd;
+    const size_t row = (size_t)b * hq + i / hd, place = place_of(i / hd);
     float2 ml[U];
     FD v[U];
     auto load = [&](int z0) {  // the first of them before it is known how many there are
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const size_t at = row + min(z0 + u, p.n - 1) * step;
+        const size_t at = place + min(z0 + u, (p.share ? dealt.y : p.n) - 1) * step;
         ml[u] = p.ml[at];
         v[u] = *reinterpret_cast<const FD*>(p.o + at * hd + d);
       }
     };
     load(0);
     if (!paged_seq(map, b, max_pos, turns, most, t)) return;
-    const int n = min((t.n + p.keys) / p.keys, p.n);
+    const int n = p.share ? dealt.y : min((t.n + p.keys) / p.keys, p.n);
     if (n == 1) return;  // one piece writes the output itself
     float m = -INFINITY, den = 0.f;
     FD num = 0.f;
@@ -239,8 +246,8 @@ k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int 
     return;
   }
   if (!paged_seq(map, b, max_pos, turns, most, t)) return;
-  const int keys = t.n + 1, n = min((t.n + p.keys) / p.keys, p.n);
-  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, first = item % blocks * 256, slot = first + threadIdx.x, G = hq / hkv;
+  const int keys = t.n + 1, n = p.share ? dealt.y : min((t.n + p.keys) / p.keys, p.n);
+  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, first = item % blocks * 256, slot = first + threadIdx.x;
   if (first >= keys) return;
   const int page = slot < keys ? map.table[(size_t)b * map.columns + (slot >> map.shift)] : -1;
   const bool there = (unsigned)page < (unsigned)map.pages;
@@ -249,17 +256,16 @@ k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int 
   __shared__ float2 heads[64];  // maximum, 1 / sum
   float got = 0.f;
   for (int g0 = 0; g0 < G; g0 += 64) {
-    const size_t row = (size_t)b * hq + kh * G + g0;
     const int count = min(64, G - g0);
     float s[U];
     auto load = [&](int g) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) s[u] = p.scores[(row + min(g + u, count - 1)) * p.stride + min(slot, keys - 1)];
+      for (int u = 0; u < U; ++u) s[u] = p.scores[score_at(p, b, hq, G, kh * G + g0 + min(g + u, count - 1), min(slot, keys - 1))];
     };
     load(0);
     if (g0) __syncthreads();
     if ((int)threadIdx.x < count) {
-      const float2 all = joined(p.ml + row + threadIdx.x, step, n, scale);
+      const float2 all = joined(p.ml + place_of(kh * G + g0 + threadIdx.x), step, n, scale);
       heads[threadIdx.x] = float2{all.x == -INFINITY ? 0.f : all.x, 1.f / all.y};
     }
     __syncthreads();
@@ -285,54 +291,74 @@ bool fast(const PagedAttn& a) {
   return (a.hd == 64 || a.hd == 128) && (at & 15) == 0 && a.hq <= 65535;
 }
 
-// Pieces of a call's contexts.
-PagedPieces pieces_for(const PagedAttn& a) {
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+int score_stride(const PagedAttn& a) { return (a.max_keys + 31) / 32 * 32; }
+size_t score_bytes(const PagedAttn& a) { return a.weights ? (size_t)a.batch * a.hq * score_stride(a) * sizeof(float) : 0; }
+size_t place_bytes(const PagedAttn& a) { return (size_t)(a.hd + 2) * sizeof(float); }
+// Of partial results, and of what is beside them.
+size_t piece_bytes(const PagedAttn& a, const PagedPieces& p) {
+  return p.share ? p.share * 16 * place_bytes(a) + up16(a.batch * sizeof(int2)) : (size_t)p.n * a.batch * a.hq * place_bytes(a);
+}
+
+// Pieces of a call's contexts, as far as `room` bytes go.
+PagedPieces pieces_for(const PagedAttn& a, size_t room) {
   PagedPieces p;
-  const bool mfma = fast(a);
-  const long base = mfma ? (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) : (long)a.batch * a.hq, target = mfma ? LS_PAGED_WGS : 4096;
-  long want = std::min(std::max(target / base, 1l), (a.max_keys + 127l) / 128);
-  if (mfma && a.max_keys <= LS_ONE) want = 1;
+  p.keys = (a.max_keys + 63) / 64 * 64;
+  const long units = (long)a.hkv * ((a.hq / a.hkv + 15) / 16), base = a.batch * units;
+  if (fast(a)) {
+    if (a.max_keys <= LS_ONE) return p;
+    if (a.batch > 1 && a.max_keys > LS_LONG && a.batch <= PagedPieces::SEQUENCES && base <= (1 << 16)) {
+      p.share = (int)(2 * base <= LS_PAGED_WGS ? LS_PAGED_WGS : base <= LS_PAGED_WGS ? 2 * LS_PAGED_WGS : base + 2 * LS_PAGED_WGS);
+      const size_t each = 16 * place_bytes(a), beside = up16(a.batch * sizeof(int2));
+      if (piece_bytes(a, p) > room) p.share = room > beside ? (int)((room - beside) / each) : 0;
+      if (p.share > base) return p;
+      p.share = 0;
+    }
+    const long fit = (long)std::min(room / (a.batch * a.hq * place_bytes(a)), (size_t)1 << 20);
+    const long want = std::min({std::max(LS_PAGED_WGS / base, 1l), (a.max_keys + 127l) / 128, std::max(fit, 1l)});
+    p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
+    p.n = (a.max_keys + p.keys - 1) / p.keys;
+    return p;
+  }
+  const long rows = (long)a.batch * a.hq, fit = (long)std::min(room / (rows * place_bytes(a)), (size_t)1 << 20);
+  const long want = std::min({std::max(4096 / rows, 1l), (a.max_keys + 127l) / 128, std::max(fit, 1l)});
   p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
   p.n = (a.max_keys + p.keys - 1) / p.keys;
   return p;
 }
 
-// Bytes of the partial results of n pieces, and of the scores in front of them.
-size_t piece_bytes(const PagedAttn& a, int n) { return (size_t)n * a.batch * a.hq * (a.hd + 2) * sizeof(float); }
-int score_stride(const PagedAttn& a) { return (a.max_keys + 31) / 32 * 32; }
-size_t score_bytes(const PagedAttn& a) { return a.weights ? (size_t)a.batch * a.hq * score_stride(a) * sizeof(float) : 0; }
-
 }  // namespace
 
 size_t paged_attn_scratch_bytes(const PagedAttn& a) {
-  const PagedPieces p = pieces_for(a);
-  return p.n > 1 || a.weights ? score_bytes(a) + piece_bytes(a, p.n) : 0;
+  const PagedPieces p = pieces_for(a, SIZE_MAX);
+  // with weights, room for one piece of the kernel for every shape, which buffers that are not known here may want
+  const size_t least = a.weights ? (size_t)a.batch * a.hq * place_bytes(a) : 0;
+  return score_bytes(a) + std::max(p.n > 1 || p.share ? piece_bytes(a, p) : 0, least);
 }
 
 void launch_paged_attn(uint32_t dt, const PagedAttn& a, hipStream_t st) {
-  PagedPieces p = pieces_for(a);
   const int most = a.weights ? a.max_keys : INT32_MAX;
-  const size_t room = a.scratch ? a.scratch_bytes - score_bytes(a) : 0;  // with weights there is room for one piece at least
-  if (p.n > 1 && piece_bytes(a, p.n) > room) {                            // as many as there is room for
-    const int fit = std::max((int)(room / piece_bytes(a, 1)), 1);
-    p.keys = ((a.max_keys + fit - 1) / fit + 63) / 64 * 64;
-    p.n = (a.max_keys + p.keys - 1) / p.keys;
-  }
-  if (a.scratch && (a.weights || p.n > 1)) {
+  PagedPieces p = pieces_for(a, a.scratch ? a.scratch_bytes - score_bytes(a) : 0);
+  if (a.scratch) {
     float* at = a.scratch;
     if (a.weights) {
       p.scores = at;
       p.stride = score_stride(a);
       at += (size_t)a.batch * a.hq * p.stride;
     }
+    if (p.share) {
+      p.dealt = (int2*)at;
+      at += up16(a.batch * sizeof(int2)) / sizeof(float);
+    }
     p.o = at;
-    p.ml = (float2*)(at + (size_t)p.n * a.batch * a.hq * a.hd);
+    p.ml = (float2*)(at + (p.share ? (size_t)p.share * 16 : (size_t)p.n * a.batch * a.hq) * a.hd);
   }
   if (fast(a)) launch_paged_attn_mfma(dt, a, p, most, st);
   else if (dt == F32) launch_any<float>(a, p, most, st);
   else launch_any<bf16>(a, p, most, st);
-  if (p.n == 1 && (!a.weights || (fast(a) && paged_joins_weights(a, p)))) return;
-  const int D = a.hd % 4 ? 2 : 4, out_blocks = p.n > 1 ? (a.hq * a.hd / D + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;
+  const bool cut = p.n > 1 || p.share;
+  if (!cut && (!a.weights || (fast(a) && paged_joins_weights(a, p)))) return;
+  const int D = a.hd % 4 ? 2 : 4, out_blocks = cut ? (a.hq * a.hd / D + 255) / 256 : 0, slots = a.weights ? a.hkv * ((a.max_keys + 255) / 256) : 0;
   const dim3 grid(out_blocks + slots, a.batch);
   auto join = [&](auto* kernel, auto* out) {
     kernel<<<grid, 256, 0, st>>>(a.map, out, a.weights, a.batch, a.hq, a.hkv, a.hd, a.max_pos, a.cs != nullptr, most, p, out_blocks);

@@ -25,9 +25,69 @@ namespace {
 
 constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns' equal dims in different banks
 constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds in registers
+constexpr int DEALT = PagedPieces::SEQUENCES;
 constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
 constexpr float FOLLOW = 8.f;
 constexpr int CUS = 256;
+
+__device__ __forceinline__ int wave_total(int v) {
+  return __builtin_amdgcn_readfirstlane(
+      __float_as_int(exchange<32, 1>(__int_as_float(v), [](float a, float b) { return __int_as_float(__float_as_int(a) + __float_as_int(b)); })));
+}
+
+// What workgroup `w` of `share` has to do where contexts are cut by their lengths: sequence b's piece z of `pieces` for unit `unit` of `units` (kv heads x blocks of columns).  All pieces
+// have at most `most` tiles, the fewest that make no more than `share` pieces; every wavefront finds that on its own, which takes a microsecond.  False: nothing.
+struct Piece {
+  int b, unit, z, pieces, first;  // first: workgroup of the sequence's first piece
+};
+template <int C>
+__device__ __forceinline__ bool deal(const PageMap& map, int batch, int units, int share, int w, int limit, int tile, Piece& p) {
+  const int lane = threadIdx.x & 63;
+  int tiles[C], total = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {  // a sequence without room has one, whose rows hold zeros
+    const int i = c * 64 + lane, n = map.lens[min(i, batch - 1)];
+    tiles[c] = i >= batch ? 0 : n < 0 || n >= limit || n >> map.shift >= map.columns ? 1 : n / tile + 1;
+    total += tiles[c];
+  }
+  unsigned most = (unsigned)((wave_total(total) * (int64_t)units + share - 1) / share);
+  int count[C];
+  while (true) {
+    int all = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      count[c] = (int)(((unsigned)tiles[c] + most - 1) / most);
+      all += count[c];
+    }
+    all = wave_total(all) * units;  // one for each sequence and unit in the end, for which there is room
+    if (all <= share) break;
+    most = max(most + 1, (unsigned)((uint64_t)most * (unsigned)all / (unsigned)share));
+  }
+  int before = 0;
+  bool found = false;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    int upto = count[c];
+    for (int off = 1; off < 64; off <<= 1) {
+      const int v = __shfl_up(upto, off);
+      upto += lane >= off ? v : 0;
+    }
+    const int first = (before + upto - count[c]) * units;
+    const uint64_t is = __builtin_amdgcn_ballot_w64(w >= first && w < first + count[c] * units);
+    if (is) {
+      const int at = __builtin_ctzll(is);
+      p.b = c * 64 + at;
+      p.first = __builtin_amdgcn_readlane(first, at);
+      p.pieces = __builtin_amdgcn_readlane(count[c], at);
+      found = true;
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (!found) return false;
+  p.unit = (w - p.first) / p.pieces;
+  p.z = (w - p.first) % p.pieces;
+  return true;
+}
 
 // TK: keys of a tile; NW: wavefronts; NB: tiles of a ring, a power of two
 template <class T, int HD, int TK, int NW, int NB, bool WEIGH>
@@ -48,8 +108,21 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   const int G = hq / hkv, blocks = (G + 15) / 16;
-  const int kh = blockIdx.y / blocks, cb = blockIdx.y % blocks, z = blockIdx.z, cols = min(16, G - cb * 16);
-  int b = blockIdx.x, len_of_b;
+  int b = blockIdx.x, unit = blockIdx.y, z = blockIdx.z, len_of_b;
+  Piece dealt{};
+  if (p.share) {
+    const bool any = batch <= 64 ? deal<1>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt)
+                     : batch <= 256 ? deal<4>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt)
+                                    : deal<DEALT / 64>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt);
+    if (!any) return;
+    b = dealt.b;
+    unit = dealt.unit;
+    z = dealt.z;
+    if (unit == 0 && z == 0 && threadIdx.x == 0) p.dealt[b] = int2{dealt.first, dealt.pieces};
+  }
+  unit = __builtin_amdgcn_readfirstlane(unit);
+  z = __builtin_amdgcn_readfirstlane(z);
+  const int kh = unit / blocks, cb = unit % blocks, cols = min(16, G - cb * 16);
   // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest
   if (half) {
     const int rank = b < half ? b : batch - 1 - (b - half);
@@ -66,9 +139,11 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   t.n = ((fixed*)(uintptr_t)map.lens)[b];
   t.pos = map.positions ? ((fixed*)(uintptr_t)map.positions)[b] : t.n;
   fixed* entries = (fixed*)(uintptr_t)(map.table + (size_t)b * map.columns);
-  const int per = p.keys / TK, t_lo = z * per, mask = (1 << map.shift) - 1;
+  const int mask = (1 << map.shift) - 1;
+  int t_lo = z * (p.keys / TK);
+  if (p.share && t.n >= 0) t_lo = __builtin_amdgcn_readfirstlane((t.n / TK + 1) * z / dealt.pieces);  // as even as may be (2^20 tiles, 2^10 pieces at most)
   int page[UNITS];  // of the tile that is filled next
-  auto look_up = [&](int i) {
+  auto look_up = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) page[u] = entries[min(((t_lo + wave + i * NW) * TK + 8 * u) >> map.shift, map.columns - 1)];
   };
@@ -90,7 +165,8 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   t.page = entries[t.n >> map.shift];
   const int keys = t.n + 1, ntile = (keys + TK - 1) / TK;
   if (t_lo >= ntile) return;
-  const int t_hi = z == p.n - 1 ? ntile : min(t_lo + per, ntile);  // the last piece takes what is left
+  int t_hi = z == p.n - 1 ? ntile : min(t_lo + p.keys / TK, ntile);  // the last piece takes what is left
+  if (p.share) t_hi = __builtin_amdgcn_readfirstlane(ntile * (z + 1) / dealt.pieces);
   const int count = max(0, (t_hi - t_lo - wave + NW - 1) / NW);    // tiles of this wavefront: t_lo + wave, NW further each time
   const int lrow = lane / CPR, lchunk = lane % CPR;
 
@@ -107,10 +183,10 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   uint64_t gone = 0;            // whose parts have no page: UNITS bits for each of the last tiles asked for
   // Written in assembly: of the builtin the compiler knows that it writes LDS but not where, and would wait for the fills on their way
   // before it reads what has arrived.  (m0 is reserved, of which the compiler warns.)
-  auto fill = [&] {
+  auto fill = [&]() __attribute__((always_inline)) {
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-    auto piece = [](auto once, const T* base, unsigned off, unsigned to) {
+    auto piece = [](auto once, const T* base, unsigned off, unsigned to) __attribute__((always_inline)) {
       if constexpr (decltype(once)::value) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
       else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
     };
@@ -129,7 +205,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     }
     // What one block of columns reads once does not stay in L2: 13B, 32 sequences 120 -> 106 us, 70B, 64 ragged 76 -> 66 (32 heads over one,
     // 64 sequences of 2000 slots, which two blocks read: 21 and 24).
-    auto all = [&](auto once) {
+    auto all = [&](auto once) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         piece(once, kt[i * RPI / 8], koff[i], to + i * 1024);
@@ -216,6 +292,25 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       if (WEIGH && lane == 0) places[slot] = t.pos;
     }
   }
+
+  // Slots whose weights this thread adds up below, AHEAD at a time: where they are, and what they have, on its way while tiles are (at the end they
+  // would be waited for: 13B, 32 sequences of 500 slots 65 us).
+  constexpr int AHEAD = 4;
+  size_t to[AHEAD];
+  float had[AHEAD];
+  bool there[AHEAD];
+  auto weights_of = [&](int first) {
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int slot = min(first + j * THREADS, t.n), at = map.table[(size_t)b * map.columns + (slot >> map.shift)];
+      there[j] = (unsigned)at < (unsigned)map.pages;
+      to[j] = page_row0(there[j] ? at : 0, hkv, kh, map.shift) + (slot & mask);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) had[j] = weights[to[j]];
+  };
+  if (WEIGH && weights) weights_of(threadIdx.x);
+  float* scores = WEIGH ? p.scores + ((size_t)b * hq + kh * G) * p.stride + cb * 256 : nullptr;  // of column 0
 
   f32x4 o[DT];
   float m_run = -INFINITY, l_run = 0.f;  // l_run: of this lane's keys
@@ -304,7 +399,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     if constexpr (WEIGH) {
       if (lr < cols)
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>(p.scores + (row0 + lr) * p.stride + key0 + h * 16 + 4 * lg) = s[h];
+        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>(scores + (size_t)(key0 + h * 16) * G + lr * 16 + 4 * lg) = s[h];
     }
     if (masked) {
 #pragma unroll
@@ -383,8 +478,8 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     for (int i = 0; i < DT; ++i)
       *reinterpret_cast<f32x4*>(sm_o + (wave * 16 + lr) * (HD + SM_PAD) + dim_of(i)) = f32x4{out_at(i, 0), out_at(i, 1), out_at(i, 2), out_at(i, 3)};
   __syncthreads();
-  const bool whole = ntile <= per || p.n == 1;  // the sequence is this one piece: its output rows go out
-  const size_t pieces = (size_t)z * batch * hq;
+  const bool whole = p.share ? dealt.pieces == 1 : ntile <= p.keys / TK || p.n == 1;  // the sequence is this one piece: its output rows go out
+  const size_t place0 = p.share ? (size_t)blockIdx.x * 16 : (size_t)z * batch * hq + row0;
   for (int i = threadIdx.x; i < cols * (HD / 4); i += THREADS) {
     const int c = i / (HD / 4), d = i % (HD / 4) * 4;
     float m = -INFINITY;
@@ -408,31 +503,40 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       for (int e = 0; e < 4; ++e) v[e] = from_f<T>(num[e] / den);
       *reinterpret_cast<T4*>(out + row * HD + d) = v;
     } else {
-      *reinterpret_cast<f32x4*>(p.o + (pieces + row) * HD + d) = num;
+      *reinterpret_cast<f32x4*>(p.o + (place0 + c) * HD + d) = num;
     }
     if (d == 0) {
       if (WEIGH && weights) sm_all[c] = float2{m == -INFINITY ? 0.f : m, 1.f / den};
-      else if (WEIGH || !whole) p.ml[pieces + row] = float2{m, den};
+      else if (WEIGH || !whole) p.ml[place0 + c] = float2{m, den};
     }
   }
   if constexpr (WEIGH) {  // the weights of all slots, where one workgroup has all of them and all of the query heads
     if (!weights) return;
     __syncthreads();  // the scores of all wavefronts are in memory
-    for (int slot = threadIdx.x; slot < keys; slot += THREADS) {
-      constexpr int U = 8;  // heads on their way at once
-      const int at = map.table[(size_t)b * map.columns + (slot >> map.shift)];
-      const bool there = (unsigned)at < (unsigned)map.pages;
-      const size_t to = page_row0(there ? at : 0, hkv, kh, map.shift) + (slot & mask);
-      float got = there && slot != t.n ? weights[to] : 0.f;
+    for (int first = threadIdx.x; first < keys; first += AHEAD * THREADS) {
+      constexpr int U = 4;  // heads on their way at once
+      if (first != (int)threadIdx.x) weights_of(first);
+      float got[AHEAD] = {};
       for (int c0 = 0; c0 < cols; c0 += U) {
-        float v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = p.scores[(row0 + min(c0 + u, cols - 1)) * p.stride + slot];
+        float v[U][AHEAD];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (c0 + u < cols) got += __builtin_amdgcn_exp2f((v[u] - sm_all[c0 + u].x) * scale) * sm_all[c0 + u].y;
+#pragma unroll
+          for (int j = 0; j < AHEAD; ++j) {
+            const int slot = min(first + j * THREADS, t.n);
+            v[u][j] = c0 + u < cols ? scores[(size_t)(slot & ~15) * G + (c0 + u) * 16 + (slot & 15)] : 0.f;
+          }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c0 + u < cols)
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) got[j] += __builtin_amdgcn_exp2f((v[u][j] - sm_all[c0 + u].x) * scale) * sm_all[c0 + u].y;
       }
-      if (there) weights[to] = got;
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        const int slot = first + j * THREADS;
+        if (slot < keys && there[j]) weights[to[j]] = slot == t.n ? got[j] : had[j] + got[j];
+      }
     }
   }
 }
@@ -446,8 +550,8 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
   allow_dynamic_lds((const void*)kernel, SMEM, lds_allowed);
   const int heads = a.hkv * ((a.hq / a.hkv + 15) / 16);
   int half = 0;
-  if (p.n == 1 && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = (long)heads * a.batch <= 2 * CUS ? std::max(1, CUS / heads) : a.batch;
-  kernel<<<dim3(a.batch, heads, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
+  if (p.n == 1 && !p.share && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = (long)heads * a.batch <= 2 * CUS ? std::max(1, CUS / heads) : a.batch;
+  kernel<<<p.share ? dim3(p.share) : dim3(a.batch, heads, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
                                                            a.batch, p, paged_joins_weights(a, p) ? a.weights : nullptr);
 }
 
@@ -469,7 +573,7 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
 
 template <class T, int HD>
 void launch_hd(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
-  const bool alone = (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) * p.n <= LS_LIMIT;
+  const bool alone = (p.share ? p.share : (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) * p.n) <= LS_LIMIT;
   if constexpr (sizeof(T) * HD == 512) {
     if (a.weights) alone ? launch_kernel_of<T, HD, LS_FSMALL, true>(a, p, most, st) : launch_kernel_of<T, HD, LS_FBIG, true>(a, p, most, st);
     else alone ? launch_kernel_of<T, HD, LS_FSMALL, false>(a, p, most, st) : launch_kernel_of<T, HD, LS_FBIG, false>(a, p, most, st);
@@ -482,7 +586,7 @@ void launch_hd(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t s
 }  // namespace
 
 // Whether the attention kernel adds the weights up itself.
-bool paged_joins_weights(const PagedAttn& a, const PagedPieces& p) { return a.weights && p.n == 1 && a.hq / a.hkv <= 16; }
+bool paged_joins_weights(const PagedAttn& a, const PagedPieces& p) { return a.weights && p.n == 1 && !p.share && a.hq / a.hkv <= 16; }
 
 void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
   if (dt == F32) {
