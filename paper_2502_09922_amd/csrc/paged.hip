@@ -4,11 +4,13 @@
 
 #include <algorithm>
 
+
 namespace ls {
 
 namespace {
 
 // ---- filling -----------------------------------------------------------------------------------------------------------------
+constexpr int FILL_SLOTS = 64;  // a thread of a workgroup at most to each
 struct FillArgs {
   PageMap map;
   const int32_t *src, *from_lens;
@@ -22,11 +24,12 @@ __device__ __forceinline__ int fill_len(const FillArgs& a, int b, int& src) {
   return n <= a.from_seq && n <= a.slots ? n : -1;
 }
 
-// A workgroup to 64 slots of a (sequence, layer, kv head), a thread to a U-sized piece of a row.
+// A workgroup to FILL_SLOTS slots of a (sequence, layer, kv head) at a time, a thread to a U-sized piece of a row, AT_ONCE of them on their way.
 template <class U>
 __global__ void __launch_bounds__(256)
 k_paged_fill(FillArgs a, const U* __restrict__ fk, const U* __restrict__ fv, const float* __restrict__ fw, U* __restrict__ kc, U* __restrict__ vc,
              float* __restrict__ weights, int32_t* __restrict__ places, int32_t* __restrict__ lens, int32_t* __restrict__ positions, int blocks) {
+  constexpr int AT_ONCE = 4;
   const int b = blockIdx.y, head = blockIdx.x / blocks, block = blockIdx.x % blocks, layer = head / a.hkv, kh = head % a.hkv;
   int src;
   const int n = fill_len(a, b, src);
@@ -34,29 +37,43 @@ k_paged_fill(FillArgs a, const U* __restrict__ fk, const U* __restrict__ fv, con
     lens[b] = n;
     if (positions) positions[b] = n;
   }
-  const int lo = block * 64, hi = block == blocks - 1 ? n : min(lo + 64, n);  // the last one takes what is left
-  const size_t from = (((size_t)layer * a.from_batch + src) * a.hkv + kh) * a.from_seq;
+  const size_t from = (((size_t)layer * a.from_batch + src) * a.hkv + kh) * a.from_seq, layer0 = (size_t)layer * a.map.pages * a.hkv << a.map.shift;
   const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
   auto row_of = [&](int slot, size_t& row) {
     const int page = entries[slot >> a.map.shift];
-    row = page_row0((int)0, a.hkv, kh, a.map.shift) + (((size_t)layer * a.map.pages + page) * a.hkv << a.map.shift) + (slot & ((1 << a.map.shift) - 1));
+    row = layer0 + page_row0(page, a.hkv, kh, a.map.shift) + (slot & ((1 << a.map.shift) - 1));
     return (unsigned)page < (unsigned)a.map.pages;
   };
-  for (int64_t i = threadIdx.x; i < (int64_t)(hi - lo) * a.pieces; i += 256) {
-    const int slot = lo + (int)(i / a.pieces), piece = (int)(i % a.pieces);
-    size_t row;
-    if (!row_of(slot, row)) continue;
-    const size_t at = (from + slot) * a.pieces + piece;
-    const U k = fk[at], v = fv[at];
-    kc[row * a.pieces + piece] = k;
-    vc[row * a.pieces + piece] = v;
-  }
-  if (!weights) return;
-  for (int slot = lo + threadIdx.x; slot < hi; slot += 256) {
-    size_t row;
-    if (!row_of(slot, row)) continue;
-    weights[row] = fw ? fw[from + slot] : 0.f;
-    places[row] = slot;
+  for (int lo = block * FILL_SLOTS; lo < n; lo += blocks * FILL_SLOTS) {  // more than one only where max_len is understated
+    const int slots = min(FILL_SLOTS, n - lo), items = slots * a.pieces;
+    size_t place = 0;  // of a slot to a thread: its weight is on its way with the rows
+    float weight = 0.f;
+    const bool named = weights && (int)threadIdx.x < slots && row_of(lo + threadIdx.x, place);
+    if (named && fw) weight = fw[from + lo + threadIdx.x];
+    for (int i0 = threadIdx.x; i0 < items; i0 += 256 * AT_ONCE) {
+      U k[AT_ONCE], v[AT_ONCE];
+      size_t to[AT_ONCE];
+      bool there[AT_ONCE];
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const int i = min(i0 + j * 256, items - 1), slot = lo + i / a.pieces, piece = i % a.pieces;
+        const size_t at = (from + slot) * a.pieces + piece;
+        k[j] = __builtin_nontemporal_load(fk + at);
+        v[j] = __builtin_nontemporal_load(fv + at);
+        there[j] = row_of(slot, to[j]) && i0 + j * 256 < items;
+        to[j] = to[j] * a.pieces + piece;
+      }
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j)
+        if (there[j]) {
+          __builtin_nontemporal_store(k[j], kc + to[j]);
+          __builtin_nontemporal_store(v[j], vc + to[j]);
+        }
+    }
+    if (named) {
+      weights[place] = weight;
+      places[place] = lo + threadIdx.x;
+    }
   }
 }
 
@@ -64,10 +81,13 @@ k_paged_fill(FillArgs a, const U* __restrict__ fk, const U* __restrict__ fv, con
 struct EvictArgs {
   PageMap map;
   int batch, hkv, layers, keep, first, recent, max_len, most;  // most: moves of a (layer, sequence, kv head)
-  const float* weights;
-  const int32_t* places;
-  int32_t* count;  // [units] moves, -1 for a sequence that is left alone
+  float* weights;
+  int32_t* places;
+  int32_t* count;  // [units] moves that are to be made, -1 for a sequence that is left alone
   int2* moves;     // [units][most]: to slot x from slot y
+  void *kc, *vc;
+  int pieces;      // of a row, 16 bytes each (wide) or 4
+  bool wide;
 };
 
 // Greater keys stay.  A weight that is no number has 0, equal weights equal keys.
@@ -98,15 +118,55 @@ __device__ __forceinline__ bool evict_seq(const EvictArgs& a, int b, int threads
   return *bad == 0;
 }
 
+// `count` of the moves of a (layer, kv head), by `threads` threads: a U-sized piece of a row to each, AT_ONCE of them on their way.
+template <class U>
+__device__ __forceinline__ void make_moves(const EvictArgs& a, const int32_t* entries, int layer, int kh, const int2* moves, int count, int threads) {
+  constexpr int AT_ONCE = 4;
+  U *kc = (U*)a.kc, *vc = (U*)a.vc;
+  const int items = count * a.pieces;
+  for (int i0 = threadIdx.x; i0 < items; i0 += threads * AT_ONCE) {
+    U k[AT_ONCE], v[AT_ONCE];
+    size_t to[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int i = min(i0 + j * threads, items - 1), piece = i % a.pieces;
+      const int2 m = moves[i / a.pieces];
+      const size_t fr = slot_row(a, entries, layer, kh, m.y) * a.pieces + piece;
+      to[j] = slot_row(a, entries, layer, kh, m.x) * a.pieces + piece;
+      k[j] = __builtin_nontemporal_load(kc + fr);
+      v[j] = __builtin_nontemporal_load(vc + fr);
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      if (i0 + j * threads < items) {
+        __builtin_nontemporal_store(k[j], kc + to[j]);
+        __builtin_nontemporal_store(v[j], vc + to[j]);
+      }
+  }
+  for (int i = threadIdx.x; i < count; i += threads) {
+    const int2 m = moves[i];
+    const size_t to = slot_row(a, entries, layer, kh, m.x), fr = slot_row(a, entries, layer, kh, m.y);
+    a.weights[to] = a.weights[fr];
+    a.places[to] = a.places[fr];
+  }
+}
+
+// Rows of all kv heads of a layer, whose bytes of weights and places 32-bit offsets reach.
+constexpr int64_t NARROW = 1 << 29;
+
 // The moves of a (layer, sequence, kv head) whose keys fit the registers of W wavefronts, V to a lane: wavefront w has the w-th part of the slots,
 // 64 neighbours to a register.  The largest key that `keep` slots or more reach is searched for between the smallest and the largest of the
-// slots that may go, by where it lay if keys were spread evenly and by halves in turn, until exactly `keep` slots reach it or nothing is left
-// between; in the latter case the lower ones of equal keys stay.  Weights and places are read once.
+// slots that may go, by where it lay if keys were spread evenly, until exactly `keep` slots reach it or nothing is left
+// between; in the latter case the lower ones of equal keys stay.  Weights and places are read once.  Where a unit has no more than FEW moves (`here`),
+// they are made here: another launch for one move each took 6 us for 5120 units.
+constexpr int FEW = 32, GUESSES = 12;
 template <int W, int V>
-__global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
+__global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here) {
+  constexpr int GR = V < 8 ? V : 8;  // registers at a time; those behind the slots hold keys of 0, below every threshold
   const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   __shared__ int bad, sums[2][W][3];
+  __shared__ int2 list[FEW];
   int n, from, turn = 0;
   if (!evict_seq(a, b, 64 * W, &bad, n, from)) {
     if (threadIdx.x == 0) a.count[unit] = -1;
@@ -122,55 +182,63 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
     }
     __syncthreads();
   };
-  auto total = [&](int x) {
+  __shared__ int counts[3];  // one is added to, one read, one cleared
+  if (W > 1 && threadIdx.x == 0) counts[0] = 0;
+  auto total = [&](int x, int round) {
     if constexpr (W == 1) return x;
-    each(x, 0, 0);
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < W; ++w) all += sums[turn][w][0];
-    return all;
+    if (lane == 0) atomicAdd(&counts[round % 3], x);
+    if (threadIdx.x == 0) counts[(round + 1) % 3] = 0;
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(counts[round % 3]);
   };
   const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
-  const int per = (n + 64 * W - 1) / (64 * W), slot0 = wave * per * 64 + lane, mask = (1 << a.map.shift) - 1;
+  const int per = (n + 64 * W - 1) / (64 * W), first = wave * per * 64, slot0 = first + lane, mask = (1 << a.map.shift) - 1;
   const float* weights = a.weights + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
   const int32_t* places = a.places + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
+  // the registers that may hold slots of this wavefront, GR at a time
+  auto registers = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < V; g += GR)
+      if (g < per) {
+#pragma unroll
+        for (int i = g; i < g + GR; ++i) f(i, slot0 + i * 64, i < per && slot0 + i * 64 < n);
+      }
+  };
   unsigned key[V];
-  constexpr int AT_ONCE = V < 16 ? V : 16;  // on their way together; slots that are not there read the last one
 #pragma unroll
-  for (int i0 = 0; i0 < V; i0 += AT_ONCE) {
-    size_t row[AT_ONCE];
-    float w[AT_ONCE];
-    int place[AT_ONCE];
+  for (int g = 0; g < V; g += GR) {
+    if (g < per) {
+      unsigned row[GR];
+      float w[GR];
+      int place[GR];
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const int slot = min(slot0 + (i0 + j) * 64, n - 1);
-      row[j] = page_row0(entries[slot >> a.map.shift], a.hkv, kh, a.map.shift) + (slot & mask);
-    }
+      for (int j = 0; j < GR; ++j) {
+        const int slot = min(slot0 + (g + j) * 64, n - 1);
+        row[j] = ((unsigned)(entries[slot >> a.map.shift] * a.hkv + kh) << a.map.shift) + (slot & mask);
+      }
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      w[j] = weights[row[j]];
-      place[j] = places[row[j]];
-    }
+      for (int j = 0; j < GR; ++j) {
+        w[j] = weights[row[j]];
+        place[j] = places[row[j]];
+      }
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const int i = i0 + j;  // a key of 0 is below every threshold
-      key[i] = i < per && slot0 + i * 64 < n ? stay_key(w[j], place[j], a.first, from) : 0;
+      for (int j = 0; j < GR; ++j) key[g + j] = g + j < per && slot0 + (g + j) * 64 < n ? stay_key(w[j], place[j], a.first, from) : 0;
+    } else {
+#pragma unroll
+      for (int j = 0; j < GR; ++j) key[g + j] = 0;
     }
   }
   unsigned low = 0xFFFFFFFFu, high = 0;
   int stay = 0;  // slots that stay whatever their weight
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i < per) {
-      const bool there = slot0 + i * 64 < n, free = there && key[i] != 0xFFFFFFFFu;
-      low = min(low, free ? key[i] : 0xFFFFFFFFu);
-      high = max(high, free ? key[i] : 0u);
-      stay += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && !free));
-    }
-  for (int off = 32; off; off >>= 1) {
-    low = min(low, (unsigned)__shfl_xor((int)low, off));
-    high = max(high, (unsigned)__shfl_xor((int)high, off));
-  }
+  registers([&](int i, int, bool there) __attribute__((always_inline)) {
+    const bool free = there && key[i] != 0xFFFFFFFFu;
+    low = min(low, free ? key[i] : 0xFFFFFFFFu);
+    high = max(high, free ? key[i] : 0u);
+    stay += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] == 0xFFFFFFFFu));
+  });
+  auto bits = [](float v) { return __builtin_bit_cast(unsigned, v); };
+  low = bits(exchange<32, 1>(__builtin_bit_cast(float, low), [&](float x, float y) { return __builtin_bit_cast(float, min(bits(x), bits(y))); }));
+  high = bits(exchange<32, 1>(__builtin_bit_cast(float, high), [&](float x, float y) { return __builtin_bit_cast(float, max(bits(x), bits(y))); }));
   if constexpr (W > 1) {
     each((int)low, (int)high, stay);
     low = 0xFFFFFFFFu;
@@ -182,6 +250,8 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
       stay += sums[turn][w][2];
     }
   }
+  low = __builtin_amdgcn_readfirstlane(low);
+  high = __builtin_amdgcn_readfirstlane(high);
   // `reach` slots have at least `least`, `keep` or more of them; fewer than `keep`, `above`, have `beyond` or more
   unsigned least = low, beyond = high + 1;
   int reach = n, above = stay;
@@ -190,18 +260,20 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
     reach = stay;
     above = 0;
   }
-  bool even = true;
-  while (reach != a.keep && beyond - least > 1 && stay < a.keep) {
+  for (int round = 0; reach != a.keep && beyond - least > 1 && stay < a.keep; ++round) {
     const unsigned range = beyond - least;
     unsigned step = range >> 1;
-    if (even) step = min(max((unsigned)((float)range * ((float)(reach - a.keep) / (float)(reach - above))), 1u), range - 1);
-    even = !even;
-    const unsigned middle = least + step;
+    // 16384 weights spread like exp(1.5 N(0, 1)) take 8 rounds, by halves 14, in turn 13 to 16; halves end what guesses do not
+    if (round < GUESSES) step = min(max((unsigned)((float)range * ((float)(reach - a.keep) / (float)(reach - above))), 1u), range - 1);
+    const unsigned middle = __builtin_amdgcn_readfirstlane(least + step);
     int got = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < per) got += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] >= middle));
-    got = total(got);
+    for (int g = 0; g < V; g += GR)
+      if (g < per) {
+#pragma unroll
+        for (int i = g; i < g + GR; ++i) got += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] >= middle));
+      }
+    got = total(got, round);
     if (got >= a.keep) {
       least = middle;
       reach = got;
@@ -215,31 +287,29 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
   int rank = 0;
   if (ties) {
     int equal = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < per) equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(slot0 + i * 64 < n && key[i] == least));
+    registers([&](int i, int, bool there) __attribute__((always_inline)) { equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && key[i] == least)); });
     if constexpr (W > 1) {
       each(equal, 0, 0);
       for (int w = 0; w < wave; ++w) rank += sums[turn][w][0];
     }
   }
-  const uint64_t below = (1ull << lane) - 1;
-  uint64_t kept = 0;  // bit i: slot i of this lane
+  auto before = [](uint64_t m) { return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0)); };  // lanes of m in front of this one
+  uint64_t stays = 0;  // bit i: slot i of this lane
   int holes = 0, movers = 0;
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i < per) {
-      const int slot = slot0 + i * 64;
-      bool stays = slot < n && key[i] >= least;
-      if (ties) {
-        const uint64_t equal = __builtin_amdgcn_ballot_w64(slot < n && key[i] == least);
-        if (slot < n && key[i] == least) stays = rank + __builtin_popcountll(equal & below) < a.keep - above;
-        rank += __builtin_popcountll(equal);
-      }
-      kept |= (uint64_t)stays << i;
-      holes += __builtin_popcountll(__builtin_amdgcn_ballot_w64(slot < a.keep && !stays));
-      movers += __builtin_popcountll(__builtin_amdgcn_ballot_w64(slot >= a.keep && stays));
+  registers([&](int i, int, bool there) __attribute__((always_inline)) {
+    bool is = there && key[i] >= least;
+    if (ties) {
+      const uint64_t equal = __builtin_amdgcn_ballot_w64(there && key[i] == least);
+      if (there && key[i] == least) is = rank + (int)before(equal) < a.keep - above;
+      rank += __builtin_popcountll(equal);
     }
+    stays |= (uint64_t)is << i;
+    const uint64_t all = __builtin_amdgcn_ballot_w64(is);
+    const int64_t front = (int64_t)a.keep - (first + i * 64);  // of these 64 slots below `keep`
+    const uint64_t in_front = front >= 64 ? ~0ull : front <= 0 ? 0ull : (1ull << front) - 1;
+    holes += i < per ? __builtin_popcountll(~all & in_front) : 0;
+    movers += __builtin_popcountll(all & ~in_front);
+  });
   int to = 0, fr = 0, all = movers;
   if constexpr (W > 1) {
     each(holes, movers, 0);
@@ -251,19 +321,24 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a) {
       all += sums[turn][w][1];
     }
   }
-  int2* moves = a.moves + (size_t)unit * a.most;
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i < per) {
-      const int slot = slot0 + i * 64;
-      const bool stays = kept >> i & 1, hole = slot < a.keep && !stays, mover = slot >= a.keep && stays;
-      const uint64_t hs = __builtin_amdgcn_ballot_w64(hole), ms = __builtin_amdgcn_ballot_w64(mover);
-      if (hole) moves[to + __builtin_popcountll(hs & below)].x = slot;
-      if (mover) moves[fr + __builtin_popcountll(ms & below)].y = slot;
+  int2* moves = here ? list : a.moves + (size_t)unit * a.most;
+  registers([&](int i, int slot, bool) __attribute__((always_inline)) {
+    const bool is = stays >> i & 1, hole = i < per && slot < a.keep && !is, mover = slot >= a.keep && is;
+    const uint64_t hs = __builtin_amdgcn_ballot_w64(hole), ms = __builtin_amdgcn_ballot_w64(mover);
+    if (hs) {
+      if (hole) moves[to + before(hs)].x = slot;
       to += __builtin_popcountll(hs);
+    }
+    if (ms) {
+      if (mover) moves[fr + before(ms)].y = slot;
       fr += __builtin_popcountll(ms);
     }
-  if (threadIdx.x == 0) a.count[unit] = all;
+  });
+  if (threadIdx.x == 0) a.count[unit] = here ? 0 : all;
+  if (!here) return;
+  __syncthreads();
+  if (a.wide) make_moves<u32x4>(a, entries, layer, kh, list, all, 64 * W);
+  else make_moves<uint32_t>(a, entries, layer, kh, list, all, 64 * W);
 }
 
 // The same for sequences of any length: keys are made again for each count, bit by bit.
@@ -345,47 +420,47 @@ __global__ void __launch_bounds__(256) k_evict_choose_long(EvictArgs a) {
   if (threadIdx.x == 0) a.count[unit] = from0;
 }
 
-void launch_evict_choose(const EvictArgs& a, size_t units, hipStream_t st) {
-#ifdef LS_EVICT_FEW
-  const bool few = units <= LS_EVICT_FEW;
-#else
-  const bool few = units <= 512;
-#endif
-  const int n = a.max_len;
-  if (n <= 64 * 8) k_evict_choose<1, 8><<<units, 64, 0, st>>>(a);
-  else if (n <= 64 * 16 && !few) k_evict_choose<1, 16><<<units, 64, 0, st>>>(a);
-  else if (n <= 64 * 32 && !few) k_evict_choose<1, 32><<<units, 64, 0, st>>>(a);
-  else if (n <= 256 * 8) k_evict_choose<4, 8><<<units, 256, 0, st>>>(a);
-  else if (n <= 256 * 16) k_evict_choose<4, 16><<<units, 256, 0, st>>>(a);
-  else if (n <= 256 * 32 && !few) k_evict_choose<4, 32><<<units, 256, 0, st>>>(a);
-  else if (n <= 1024 * 8) k_evict_choose<16, 8><<<units, 1024, 0, st>>>(a);
-  else if (n <= 1024 * 16) k_evict_choose<16, 16><<<units, 1024, 0, st>>>(a);
-  else if (n <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a);
-  else k_evict_choose_long<<<units, 256, 0, st>>>(a);
-}
-
-// The moves: a thread to a U-sized piece of a row.  The lengths, which the launch before reads, are set by one workgroup of a sequence.
+// The moves: a workgroup to MOVES of them at a time.  The lengths, which the launch before reads, are set by one workgroup of a sequence.
+constexpr int MOVES = 64;
 template <class U>
-__global__ void __launch_bounds__(256)
-k_evict_move(EvictArgs a, U* __restrict__ kc, U* __restrict__ vc, float* __restrict__ weights, int32_t* __restrict__ places, int32_t* __restrict__ lens, int pieces) {
+__global__ void __launch_bounds__(256) k_evict_move(EvictArgs a, int32_t* __restrict__ lens) {
   const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
   const int count = a.count[unit];
   if (count < 0) return;
-  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
   if (layer == 0 && kh == 0 && blockIdx.y == 0 && threadIdx.x == 0) lens[b] = a.keep;
   const int2* moves = a.moves + (size_t)unit * a.most;
-  for (int64_t i = blockIdx.y * 256 + threadIdx.x; i < (int64_t)count * pieces; i += gridDim.y * 256) {
-    const int2 m = moves[i / pieces];
-    const int piece = (int)(i % pieces);
-    const size_t to = slot_row(a, entries, layer, kh, m.x), fr = slot_row(a, entries, layer, kh, m.y);
-    const U k = kc[fr * pieces + piece], v = vc[fr * pieces + piece];
-    kc[to * pieces + piece] = k;
-    vc[to * pieces + piece] = v;
-    if (piece == 0) {
-      weights[to] = weights[fr];
-      places[to] = places[fr];
-    }
+  for (int lo = blockIdx.y * MOVES; lo < count; lo += gridDim.y * MOVES)
+    make_moves<U>(a, a.map.table + (size_t)b * a.map.columns, layer, kh, moves + lo, min(MOVES, count - lo), 256);
+}
+
+// Lengths alone, where the moves have been made.
+__global__ void __launch_bounds__(256) k_evict_lens(EvictArgs a, int32_t* __restrict__ lens) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b < a.batch && a.count[b * a.hkv] >= 0) lens[b] = a.keep;
+}
+
+void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t st) {
+  // More wavefronts to a unit where units do not fill the chip: 1024 units of 1025 slots 14 -> 10 us.
+  const bool few = units <= 2048;
+  const bool here = a.most <= FEW;
+  const int n = ((int64_t)a.map.pages * a.hkv << a.map.shift) < NARROW ? a.max_len : INT32_MAX;
+  if (n <= 64 * 8) k_evict_choose<1, 8><<<units, 64, 0, st>>>(a, here);
+  else if (n <= 64 * 16 && !few) k_evict_choose<1, 16><<<units, 64, 0, st>>>(a, here);
+  else if (n <= 64 * 32 && !few) k_evict_choose<1, 32><<<units, 64, 0, st>>>(a, here);
+  else if (n <= 256 * 8) k_evict_choose<4, 8><<<units, 256, 0, st>>>(a, here);
+  else if (n <= 256 * 16) k_evict_choose<4, 16><<<units, 256, 0, st>>>(a, here);
+  else if (n <= 256 * 32 && !few) k_evict_choose<4, 32><<<units, 256, 0, st>>>(a, here);
+  else if (n <= 1024 * 8) k_evict_choose<16, 8><<<units, 1024, 0, st>>>(a, here);
+  else if (n <= 1024 * 16) k_evict_choose<16, 16><<<units, 1024, 0, st>>>(a, here);
+  else if (n <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a, here);
+  else k_evict_choose_long<<<units, 256, 0, st>>>(a);
+  if (here && n <= 1024 * 32) {
+    k_evict_lens<<<(a.batch + 255) / 256, 256, 0, st>>>(a, lens);
+    return;
   }
+  const dim3 grid(units, std::min((a.most + MOVES - 1) / MOVES, 1024));
+  if (a.wide) k_evict_move<u32x4><<<grid, 256, 0, st>>>(a, lens);
+  else k_evict_move<uint32_t><<<grid, 256, 0, st>>>(a, lens);
 }
 
 // ---- arguments ---------------------------------------------------------------------------------------------------------------
@@ -514,7 +589,7 @@ ls_status ls_paged_fill(const ls_heads* h, int layers, const ls_kv* from, int fr
   a.map = ls::map_of(pages);
   a.src = src; a.from_lens = from->seq_lens; a.batch = batch; a.from_batch = from_batch; a.from_seq = from_seq;
   a.hkv = (int)h->n_kv_heads; a.pieces = (int)(row / (wide ? 16 : 4)); a.slots = (int)(pages->columns * pages->page);
-  const int most = std::max(1, std::min({max_len, from_seq, a.slots})), blocks = (most + 63) / 64;
+  const int most = std::max(1, std::min({max_len, from_seq, a.slots})), blocks = (most + ls::FILL_SLOTS - 1) / ls::FILL_SLOTS;
   if (layers < 1 || (uint64_t)layers * h->n_kv_heads * blocks >= (1u << 24)) return bad(who, "layers outside [1, what a launch takes]");
   a.heads = layers * a.hkv;
   hipStream_t st = (hipStream_t)hip_stream;
@@ -559,13 +634,8 @@ ls_status ls_paged_evict(const ls_heads* h, int layers, const ls_pages* pages, i
   a.weights = pages->weights; a.places = pages->places;
   a.count = (int32_t*)scratch;
   a.moves = (int2*)((char*)scratch + (units * 4 + 15) / 16 * 16);
-  hipStream_t st = (hipStream_t)hip_stream;
-  ls::launch_evict_choose(a, units, st);
-  const dim3 grid(units, std::min(std::max((int)(((int64_t)a.most * pieces + 1023) / 1024), 1), 64));
-  if (wide)
-    ls::k_evict_move<ls::u32x4><<<grid, 256, 0, st>>>(a, (ls::u32x4*)pages->k, (ls::u32x4*)pages->v, pages->weights, pages->places, pages->lens, pieces);
-  else
-    ls::k_evict_move<uint32_t><<<grid, 256, 0, st>>>(a, (uint32_t*)pages->k, (uint32_t*)pages->v, pages->weights, pages->places, pages->lens, pieces);
+  a.kc = pages->k; a.vc = pages->v; a.pieces = pieces; a.wide = wide;
+  ls::launch_evict(a, units, pages->lens, (hipStream_t)hip_stream);
   return launched(who);
 }
 

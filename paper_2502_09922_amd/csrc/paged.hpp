@@ -38,13 +38,9 @@ struct PagedPieces {
   float* o = nullptr;       // [place][head_dim], not normalised
   float2* ml = nullptr;     // [place]: maximum in units of q k, sum
   int2* dealt = nullptr;    // [sequence]: first workgroup, pieces
-  float* scores = nullptr;  // q k of every slot, where weights are wanted: [sequence][kv head][slot / 16][query head of it][slot % 16]
-  int stride = 0;           // slots of a sequence, a multiple of 32
+  float* scores = nullptr;  // [row * hq + head][stride] q k of every slot, where weights are wanted
+  int stride = 0;           // a multiple of 32
 };
-// Of query head h, G to a kv head.
-__device__ __forceinline__ size_t score_at(const PagedPieces& p, int b, int hq, int G, int h, int slot) {
-  return ((size_t)b * hq + h / G * G) * p.stride + (size_t)(slot >> 4) * (16 * G) + h % G * 16 + (slot & 15);
-}
 void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
 
 bool paged_joins_weights(const PagedAttn& a, const PagedPieces& p);  // by itself, without a join behind it

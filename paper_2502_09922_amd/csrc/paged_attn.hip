@@ -115,7 +115,7 @@ k_paged_attn(PageMap map, const T* __restrict__ qkv, const float2* __restrict__ 
       float mine = 0.f;
 #pragma unroll
       for (int j = 0; j < AT_ONCE; ++j) mine = lane == j ? s[j] : mine;
-      if (lane < AT_ONCE && key0 + lane < hi) p.scores[score_at(p, b, hq, G, h, key0 + lane)] = mine;
+      if (lane < AT_ONCE && key0 + lane < hi) p.scores[row * p.stride + key0 + lane] = mine;
     }
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j)
@@ -256,11 +256,12 @@ k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int 
   __shared__ float2 heads[64];  // maximum, 1 / sum
   float got = 0.f;
   for (int g0 = 0; g0 < G; g0 += 64) {
+    const size_t row = (size_t)b * hq + kh * G + g0;
     const int count = min(64, G - g0);
     float s[U];
     auto load = [&](int g) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) s[u] = p.scores[score_at(p, b, hq, G, kh * G + g0 + min(g + u, count - 1), min(slot, keys - 1))];
+      for (int u = 0; u < U; ++u) s[u] = p.scores[(row + min(g + u, count - 1)) * p.stride + min(slot, keys - 1)];
     };
     load(0);
     if (g0) __syncthreads();

@@ -310,7 +310,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     for (int j = 0; j < AHEAD; ++j) had[j] = weights[to[j]];
   };
   if (WEIGH && weights) weights_of(threadIdx.x);
-  float* scores = WEIGH ? p.scores + ((size_t)b * hq + kh * G) * p.stride + cb * 256 : nullptr;  // of column 0
+  float* scores = WEIGH ? p.scores + (row0 + lr) * p.stride : nullptr;  // of this lane's column
 
   f32x4 o[DT];
   float m_run = -INFINITY, l_run = 0.f;  // l_run: of this lane's keys
@@ -399,7 +399,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     if constexpr (WEIGH) {
       if (lr < cols)
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>(scores + (size_t)(key0 + h * 16) * G + lr * 16 + 4 * lg) = s[h];
+        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>(scores + key0 + h * 16 + 4 * lg) = s[h];
     }
     if (masked) {
 #pragma unroll
@@ -522,10 +522,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int j = 0; j < AHEAD; ++j) {
-            const int slot = min(first + j * THREADS, t.n);
-            v[u][j] = c0 + u < cols ? scores[(size_t)(slot & ~15) * G + (c0 + u) * 16 + (slot & 15)] : 0.f;
-          }
+          for (int j = 0; j < AHEAD; ++j) v[u][j] = c0 + u < cols ? p.scores[(row0 + c0 + u) * p.stride + min(first + j * THREADS, t.n)] : 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (c0 + u < cols)
