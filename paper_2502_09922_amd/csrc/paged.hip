@@ -490,7 +490,7 @@ PagedAttn attn_of(const ls_heads* h, const ls_pages* p, int batch, int max_ctx) 
   a.map = map_of(p);
   a.kc = p->k; a.vc = p->v; a.weights = p->weights; a.places = p->places;
   a.batch = batch; a.hq = (int)h->n_q_heads; a.hkv = (int)h->n_kv_heads; a.hd = (int)h->head_dim; a.max_pos = (int)h->max_seq;
-  a.max_keys = max_ctx + 1;
+  a.size = h->dtype == LS_DTYPE_F32 ? 4 : 2; a.max_keys = max_ctx + 1;
   return a;
 }
 

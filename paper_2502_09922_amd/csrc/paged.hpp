@@ -20,7 +20,7 @@ struct PagedAttn {
   void *kc = nullptr, *vc = nullptr, *out = nullptr;
   float* weights = nullptr;
   int32_t* places = nullptr;
-  int batch = 0, hq = 0, hkv = 0, hd = 0, max_pos = 0, max_keys = 0;  // max_keys: the new token's among them
+  int batch = 0, hq = 0, hkv = 0, hd = 0, size = 0, max_pos = 0, max_keys = 0;  // size: bytes of a value; max_keys: the new token's among them
   float* scratch = nullptr;
   size_t scratch_bytes = 0;
 };

@@ -5,20 +5,12 @@
 //
 // Here the kernel for every shape (the fast one: paged_attn_mfma.hip), which pieces a context is cut into, and the kernel that joins them
 // and adds the weights up.  One wavefront to a (sequence, query head, piece), a lane to one or two pairs of dims, eight keys and values on
-// their way at once; eight slots lie in one page, whose number is uniform.  Bound by a wavefront's instructions.
+// their way at once; eight slots lie in one page, whose number is uniform.  Bound by a wavefront's instructions: of 128 dims, as before
+// the matrix cores had them, 13B, 32 sequences of 1024 to 1087 slots 140 us (106 there), 70B, 64 ragged ones 699 (66): each query head
+// reads the cache for itself.
 #include "paged.hpp"
 
 #include <algorithm>
-
-#ifndef LS_PAGED_WGS
-#define LS_PAGED_WGS 256
-#endif
-#ifndef LS_ONE
-#define LS_ONE 640
-#endif
-#ifndef LS_LONG
-#define LS_LONG 4096
-#endif
 
 namespace ls {
 
@@ -301,22 +293,31 @@ size_t piece_bytes(const PagedAttn& a, const PagedPieces& p) {
   return p.share ? p.share * 16 * place_bytes(a) + up16(a.batch * sizeof(int2)) : (size_t)p.n * a.batch * a.hq * place_bytes(a);
 }
 
-// Pieces of a call's contexts, as far as `room` bytes go.
+// Pieces of a call's contexts, as far as `room` bytes go.  On the matrix cores:
+//   - Where a kv head's keys and values of a sequence are at most ONE bytes, one workgroup each and no second launch: 8 kv heads, bf16, 128 dims,
+//     600 slots 10.2 us, in pieces of 128 slots 11.7 (900 slots 12.1 and 11.7); 64 dims, 1200 slots 11.2 and 11.4; fp32, 128 dims, 300 slots 11.5
+//     and 11.8, 400 slots 13.7 and 11.8.
+//   - Where some may be longer than LONG bytes, workgroups get shares by the lengths that the device knows: of 32 sequences of 500 slots and one of 16000, 8
+//     kv heads, the long one's 8 workgroups took 153 us, shared out 30; 64 of 300 and two of 3500 73 and 29.  It costs a microsecond in
+//     front and the second launch: 64 of 5000 slots 199 us uncut, 205 shared out; 64 of 2287 93 and 103.
+//   - Otherwise in equal pieces until a CU each has one: 7B, one sequence of 3000 slots 15.3 us, 16.6 with two to a CU.
 PagedPieces pieces_for(const PagedAttn& a, size_t room) {
   PagedPieces p;
   p.keys = (a.max_keys + 63) / 64 * 64;
   const long units = (long)a.hkv * ((a.hq / a.hkv + 15) / 16), base = a.batch * units;
   if (fast(a)) {
-    if (a.max_keys <= LS_ONE) return p;
-    if (a.batch > 1 && a.max_keys > LS_LONG && a.batch <= PagedPieces::SEQUENCES && base <= (1 << 16)) {
-      p.share = (int)(2 * base <= LS_PAGED_WGS ? LS_PAGED_WGS : base <= LS_PAGED_WGS ? 2 * LS_PAGED_WGS : base + 2 * LS_PAGED_WGS);
+    constexpr long CUS = 256, ONE = 300 << 10, LONG = 1500 << 10;
+    const long bytes = (long)a.max_keys * a.hd * 2 * a.size;
+    if (bytes <= ONE) return p;
+    if (a.batch > 1 && bytes > LONG && a.batch <= PagedPieces::SEQUENCES && base <= (1 << 16)) {
+      p.share = (int)(2 * base <= CUS ? CUS : base <= CUS ? 2 * CUS : base + 2 * CUS);
       const size_t each = 16 * place_bytes(a), beside = up16(a.batch * sizeof(int2));
       if (piece_bytes(a, p) > room) p.share = room > beside ? (int)((room - beside) / each) : 0;
       if (p.share > base) return p;
       p.share = 0;
     }
     const long fit = (long)std::min(room / (a.batch * a.hq * place_bytes(a)), (size_t)1 << 20);
-    const long want = std::min({std::max(LS_PAGED_WGS / base, 1l), (a.max_keys + 127l) / 128, std::max(fit, 1l)});
+    const long want = std::min({std::max(CUS / base, 1l), (a.max_keys + 127l) / 128, std::max(fit, 1l)});
     p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
     p.n = (a.max_keys + p.keys - 1) / p.keys;
     return p;

@@ -13,6 +13,12 @@
 // kernel, both in order.
 //
 // The new token's row is put into its tile in LDS by the wavefront that has that tile, and into the cache: nobody waits for memory there.
+//
+// Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 106 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for, 106; the
+// arithmetic alone 45.  70B, 64 of 128 to 2287 slots 66 us, 5.5 TB/s (64 without arithmetic): one workgroup to each place of the chip, so its start and
+// end, 5 us, are nobody else's.  4 of 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 116, 5.6 TB/s, where a tile's
+// products take half of its time on a SIMD.  Weights: scores go out and come back, 4 bytes for each query head and slot: 64 sequences of 1000 slots, 8 query heads to a kv head
+// 56 us, 44 without, where a stored score's place among the fills makes no difference.
 #include "attn_mfma.hpp"
 #include "paged.hpp"
 
@@ -23,10 +29,9 @@ namespace ls {
 
 namespace {
 
-constexpr int SM_PAD = 4;  // floats behind a column's output in LDS: 16 columns' equal dims in different banks
-constexpr int ORDERED = 256;       // sequences whose lengths a wavefront holds in registers
-constexpr int DEALT = PagedPieces::SEQUENCES;
-constexpr int ORDERED_KEYS = 512;  // contexts are ordered only where some may be longer
+constexpr int SM_PAD = 4;          // floats behind a column's output in LDS: 16 columns' equal dims in different banks
+constexpr int ORDERED = 256;       // sequences at most that are taken by length, whose lengths a wavefront holds in registers
+constexpr int ORDERED_KEYS = 512;  // and only where some may be longer
 constexpr float FOLLOW = 8.f;
 constexpr int CUS = 256;
 
@@ -35,8 +40,9 @@ __device__ __forceinline__ int wave_total(int v) {
       __float_as_int(exchange<32, 1>(__int_as_float(v), [](float a, float b) { return __int_as_float(__float_as_int(a) + __float_as_int(b)); })));
 }
 
-// What workgroup `w` of `share` has to do where contexts are cut by their lengths: sequence b's piece z of `pieces` for unit `unit` of `units` (kv heads x blocks of columns).  All pieces
-// have at most `most` tiles, the fewest that make no more than `share` pieces; every wavefront finds that on its own, which takes a microsecond.  False: nothing.
+// What workgroup `w` of `share` has to do where contexts are cut by their lengths: piece z of `pieces` of sequence b, for one of its `units` (kv heads x
+// blocks of columns).  Pieces have at most `most` tiles, few enough of them that there are no more than `share` pieces; every wavefront finds that on
+// its own, which takes a microsecond for 64 sequences.  False: nothing.
 struct Piece {
   int b, unit, z, pieces, first;  // first: workgroup of the sequence's first piece
 };
@@ -113,7 +119,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   if (p.share) {
     const bool any = batch <= 64 ? deal<1>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt)
                      : batch <= 256 ? deal<4>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt)
-                                    : deal<DEALT / 64>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt);
+                                    : deal<PagedPieces::SEQUENCES / 64>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt);
     if (!any) return;
     b = dealt.b;
     unit = dealt.unit;
@@ -552,32 +558,15 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
                                                            a.batch, p, paged_joins_weights(a, p) ? a.weights : nullptr);
 }
 
-#ifndef LS_BIG
-#define LS_BIG 4, 2
-#endif
-#ifndef LS_SMALL
-#define LS_SMALL 8, 2
-#endif
-#ifndef LS_FBIG
-#define LS_FBIG 4, 1
-#endif
-#ifndef LS_FSMALL
-#define LS_FSMALL 8, 1
-#endif
-#ifndef LS_LIMIT
-#define LS_LIMIT 256
-#endif
-
+// Four wavefronts with two tiles each, two workgroups to a CU (fp32 of 128 dims: one tile of 16 KB), or twice the wavefronts where a CU has one
+// workgroup at most.  13B, 32 sequences 106 us; three wavefronts 110, two 116, tiles of 32 keys or rings of four tiles, which leave a CU one
+// workgroup, 7 to 8 more.  7B, 8 sequences of 1024 slots with weights: eight wavefronts 27.0, four 29.1.
 template <class T, int HD>
 void launch_hd(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
-  const bool alone = (p.share ? p.share : (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) * p.n) <= LS_LIMIT;
-  if constexpr (sizeof(T) * HD == 512) {
-    if (a.weights) alone ? launch_kernel_of<T, HD, LS_FSMALL, true>(a, p, most, st) : launch_kernel_of<T, HD, LS_FBIG, true>(a, p, most, st);
-    else alone ? launch_kernel_of<T, HD, LS_FSMALL, false>(a, p, most, st) : launch_kernel_of<T, HD, LS_FBIG, false>(a, p, most, st);
-  } else {
-    if (a.weights) alone ? launch_kernel_of<T, HD, LS_SMALL, true>(a, p, most, st) : launch_kernel_of<T, HD, LS_BIG, true>(a, p, most, st);
-    else alone ? launch_kernel_of<T, HD, LS_SMALL, false>(a, p, most, st) : launch_kernel_of<T, HD, LS_BIG, false>(a, p, most, st);
-  }
+  constexpr int NB = sizeof(T) * HD == 512 ? 1 : 2;
+  const bool alone = (p.share ? p.share : (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) * p.n) <= CUS;
+  if (a.weights) alone ? launch_kernel_of<T, HD, 8, NB, true>(a, p, most, st) : launch_kernel_of<T, HD, 4, NB, true>(a, p, most, st);
+  else alone ? launch_kernel_of<T, HD, 8, NB, false>(a, p, most, st) : launch_kernel_of<T, HD, 4, NB, false>(a, p, most, st);
 }
 
 }  // namespace

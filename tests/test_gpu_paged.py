@@ -510,3 +510,153 @@ def test_a_run_at_a_budget(heads, dtype):
         c.take(cache)
     # the third has pages for 32 slots: behind them its rows are zeros, and it is not cut down
     assert c.lens.tolist() == [keep + 1, keep + 1, 45] and c.positions.tolist() == [125, 89, 45]
+
+
+# ---- contexts that are dealt out by their lengths ----------------------------------------------------------------------------
+DEALT = pytest.mark.parametrize("heads", [(8, 2, 128), (20, 1, 64), (4, 4, 64), (34, 2, 128)], ids=lambda h: "%dx%dx%d" % h)
+
+
+@TYPES
+@WEIGHED
+@DEALT
+def test_long_and_short_contexts(heads, dtype, weighed):
+    """One long sequence among short ones, some of which take no part, have no room or lack a page."""
+    c = plain.Pages(heads, dtype, [40, 6200, 0, 300, 8, 3100, 16, 17, 90], 16, seed=51, weighed=weighed)
+    c.lens[4], c.table[6, 1], c.table[5, 7], c.table[1, 100:105] = -1, c.k.shape[1], -1, 2**31 - 1
+    c.positions[8] = 6300
+    check(c, plain.rope_table(6300, heads[2]))
+
+
+@TYPES
+@WEIGHED
+@pytest.mark.parametrize("batch", [2, 64, 65, 256, 300, 1025])
+def test_one_long_context_among_many(batch, dtype, weighed):
+    """As many sequences as one register, four and sixteen of a wavefront hold the lengths of, and more."""
+    r = random.Random(batch)
+    lens = [r.choice([0, 1, 5, 15, 16, 40]) for _ in range(batch)]
+    lens[batch // 3] = 6200
+    c = plain.Pages((2, 1, 64), dtype, lens, 32, seed=52, weighed=weighed)
+    check(c, plain.rope_table(6201, 64))
+
+
+@TYPES
+@WEIGHED
+def test_all_long_contexts(dtype, weighed):
+    """More pieces than workgroups could take with one each, and none long enough to be cut."""
+    c = plain.Pages((4, 4, 128), dtype, [3400 + 7 * i for i in range(6)], 64, seed=53, weighed=weighed)
+    check(c, None)
+
+
+@TYPES
+@DEALT
+def test_dealt_with_scratch_of_any_size(heads, dtype):
+    from paper_2502_09922_amd import binding as b
+
+    c = plain.Pages(heads, dtype, [6200, 20, 700], 64, seed=54)
+    rope, hq = plain.rope_table(6210, heads[2]).cuda(), heads[0]
+    cache, qkv = c.on_gpu(), c.qkv[0].cuda()
+    h, pages = cache.heads(hq, 6210), cache._layers[0]
+    need = b.lib.ls_paged_attention_scratch_bytes(h, pages, 3, 6200)
+    scratch = torch.empty(need + 64, dtype=torch.uint8, device="cuda")
+    for nb in (0, 16, 4096, need // 40, need // 3, need - 1, need):
+        out = torch.full((3, hq * heads[2]), math.nan, dtype=dtype, device="cuda")
+        scratch.fill_(255)  # NaN
+        assert b.lib.ls_paged_attention(h, pages, 3, 6200, qkv.data_ptr(), rope.data_ptr(), out.data_ptr(), scratch.data_ptr(), nb, 0) == 0
+        torch.cuda.synchronize()
+        assert (scratch[nb:] == 255).all()
+        got = copy.copy(c)
+        got.take(cache)
+        plain.check_attention(c, 0, rope.cpu(), got, out.cpu())
+
+
+@TYPES
+@WEIGHED
+@pytest.mark.parametrize("heads", [(20, 1, 128), (40, 2, 64), (16, 16, 64)], ids=lambda h: "%dx%dx%d" % h)
+def test_pieces_of_more_heads_than_a_block(heads, dtype, weighed):
+    c = plain.Pages(heads, dtype, [2500, 1300], 16, seed=55, weighed=weighed)
+    check(c, plain.rope_table(2501, heads[2]))
+
+
+@TYPES
+@WEIGHED
+@pytest.mark.parametrize("heads", [(4, 2, 128), (40, 2, 128)], ids=lambda h: "%dx%dx%d" % h)
+def test_a_workgroup_to_a_sequence(heads, dtype, weighed):
+    """More sequences than CUs, of which one is longer than the others by far but for being dealt out."""
+    lens = [5] * 140
+    lens[70], lens[71] = 1400 if dtype == torch.float32 else 2800, 1025
+    c = plain.Pages(heads, dtype, lens, 16, seed=56, weighed=weighed)
+    check(c, plain.rope_table(2801, heads[2]))
+
+
+@pytest.mark.parametrize("weighed", [False, True], ids=["", "weighed"])
+def test_dealt_anew_by_each_replay(weighed):
+    """A captured call whose sequences' lengths become others."""
+    from paper_2502_09922_amd import paged_attention
+
+    c = plain.Pages((8, 2, 128), torch.bfloat16, [3900, 3900, 3900], 64, seed=57, weighed=weighed)
+    cache, qkv, graph = c.on_gpu(), c.qkv[0].cuda(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = paged_attention(cache, qkv, None, 3900)
+    for lens in ([3900, 3, 100], [0, 0, 0], [-1, 3899, 2000], [3900, 3900, 3900]):
+        cache.lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        c.take(cache)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = copy.copy(c)
+        got.take(cache)
+        plain.check_attention(c, 0, None, got, out.cpu())
+        c.take(cache)
+        torch.empty(1 << 22, device="cuda").fill_(math.nan)
+
+
+# ---- eviction, further ---------------------------------------------------------------------------------------------------------
+LENGTHS = [(600, 570, 3), (1500, 1469, 20), (3000, 2999, 1), (5000, 4990, 9), (9000, 8968, 0), (12000, 4000, 64), (20000, 19995, 4), (31000, 30970, 100),
+           (32768, 5, 5), (32769, 32768, 1)]
+
+
+@pytest.mark.parametrize("batch,n,keep,recent", [(1,) + x for x in LENGTHS] + [(1100,) + x for x in LENGTHS[:3]])
+def test_all_lengths_of_sequences_that_are_cut_down(batch, n, keep, recent):
+    """Few moves and many, by one wavefront to sixteen; beside sequences that stay as they are where there are many."""
+    page, hkv = 64, 2
+    pages = (n + page - 1) // page
+    c = plain.Pages((2, hkv, 2), torch.float32, [1], page, seed=61, weighed=True)
+    g, order = torch.Generator().manual_seed(n), list(range(pages))
+    random.Random(n).shuffle(order)
+    c.table = torch.full((batch, pages), 7, dtype=torch.int32)
+    c.table[batch // 2] = torch.tensor(order, dtype=torch.int32)
+    c.lens = torch.full((batch,), min(5, keep), dtype=torch.int32)
+    c.lens[batch // 2] = n
+    c.positions = c.lens.clone()
+    c.k, c.v = (torch.randn(1, pages, hkv, page, 2, generator=g) for _ in range(2))
+    c.weights = torch.randn(1, pages, hkv, page, generator=g).exp() * (torch.rand(1, pages, hkv, page, generator=g) < 0.9)
+    c.places = torch.randint(0, n, (1, pages, hkv, page), generator=g).int()
+    want = cut(c, keep, 0, recent, n)
+    assert int(want.lens[batch // 2]) == keep
+
+
+def test_evictions_beyond_32_bits():
+    """More rows of a layer than 32-bit offsets of their weights reach: a sequence in the last pages, in the second layer."""
+    from paper_2502_09922_amd import paged_evict
+
+    hkv, page, n, keep = 8, 1024, 3000, 1000
+    pages = (1 << 29) // (hkv * page) + 3
+    c = plain.Pages((8, hkv, 2), torch.bfloat16, [1], page, seed=62, weighed=True)
+    own, g = 3, torch.Generator().manual_seed(62)
+    c.k, c.v = (torch.randn(1, own, hkv, page, 2, generator=g).bfloat16() for _ in range(2))
+    c.weights, c.places = torch.rand(1, own, hkv, page, generator=g), torch.randint(0, n, (1, own, hkv, page), generator=g).int()
+    c.table, c.lens, c.positions = torch.tensor([[2, 0, 1]], dtype=torch.int32), torch.tensor([n], dtype=torch.int32), torch.tensor([n], dtype=torch.int32)
+    big = [torch.zeros((2, pages) + t.shape[2:], dtype=t.dtype, device="cuda") for t in (c.k, c.v, c.weights, c.places)]
+    for t, x in zip((c.k, c.v, c.weights, c.places), big):
+        x[1, -own:] = t[0].cuda()
+        x[0, -own:] = t[0].cuda()
+    from paper_2502_09922_amd import PagedCache
+
+    table = (c.table + (pages - own)).int().cuda()
+    cache = PagedCache(big[0], big[1], table, c.lens.cuda(), c.positions.cuda(), big[2], big[3])
+    paged_evict(cache, keep=keep, recent=10, max_len=n)
+    plain.evict(c, keep, 0, 10, n)
+    for t, x in zip((c.k, c.v, c.weights, c.places), big):
+        for layer in (0, 1):
+            assert plain.same(x[layer, -own:].cpu(), t[0])
+    assert cache.lens.tolist() == [keep]
