@@ -114,7 +114,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 
   const int G = hq / hkv, blocks = (G + 15) / 16;
-  int b = blockIdx.x, unit = blockIdx.y, z = blockIdx.z, len_of_b;
+  int b = blockIdx.y, unit = blockIdx.x, z = blockIdx.z, len_of_b;
   Piece dealt{};
   if (p.share) {
     const bool any = batch <= 64 ? deal<1>(map, batch, hkv * blocks, p.share, blockIdx.x, most, TK, dealt)
@@ -129,7 +129,8 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   unit = __builtin_amdgcn_readfirstlane(unit);
   z = __builtin_amdgcn_readfirstlane(z);
   const int kh = unit / blocks, cb = unit % blocks, cols = min(16, G - cb * 16);
-  // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest
+  // by length: the longest first, and where all workgroups fit the chip at once, two to a CU, the shortest beside the longest (a sequence's
+  // heads are neighbours: the second half of the workgroups goes to the CUs where the first half is)
   if (half) {
     const int rank = b < half ? b : batch - 1 - (b - half);
     b = batch <= 64 ? row_by_length<1, true>(map.lens, batch, rank, 1 << 24, len_of_b) : row_by_length<ORDERED / 64, true>(map.lens, batch, rank, 1 << 24, len_of_b);
@@ -554,7 +555,7 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
   const int heads = a.hkv * ((a.hq / a.hkv + 15) / 16);
   int half = 0;
   if (p.n == 1 && !p.share && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = (long)heads * a.batch <= 2 * CUS ? std::max(1, CUS / heads) : a.batch;
-  kernel<<<p.share ? dim3(p.share) : dim3(a.batch, heads, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
+  kernel<<<p.share ? dim3(p.share) : dim3(heads, a.batch, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
                                                            a.batch, p, paged_joins_weights(a, p) ? a.weights : nullptr);
 }
 
