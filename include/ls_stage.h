@@ -453,7 +453,8 @@ ls_status ls_paged_attention(const ls_heads* heads, const ls_pages* layer, int b
  *   weights   optional fp32 [layers][from_batch][n_kv_heads][from_seq]: what the slots' weights become (where the pools have them); NULL:
  *             zeros.  Places are the positions.
  *   max_len   host-side upper bound of n; an understated one costs speed, never positions
- * Slots without a page are left out.  Caches on 4 bytes for bf16 too.
+ * Slots without a page are left out.  Caches on 4 bytes for bf16 too.  A page that several sequences of the call name gets the rows of one of them,
+ * which have to be the same; `from` and the pools do not overlap.
  */
 ls_status ls_paged_fill(const ls_heads* heads, int layers, const ls_kv* from, int from_batch, int from_seq, const int32_t* src, const float* weights,
                         int max_len, const ls_pages* pages, int batch, void* hip_stream);

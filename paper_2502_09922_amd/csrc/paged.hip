@@ -3,6 +3,7 @@
 #include "paged.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 
 namespace ls {
@@ -154,15 +155,18 @@ __device__ __forceinline__ void make_moves(const EvictArgs& a, const int32_t* en
 // Rows of all kv heads of a layer, whose bytes of weights and places 32-bit offsets reach.
 constexpr int64_t NARROW = 1 << 29;
 
-// The moves of a (layer, sequence, kv head) whose keys fit the registers of W wavefronts, V to a lane: wavefront w has the w-th part of the slots,
-// 64 neighbours to a register.  The largest key that `keep` slots or more reach is searched for between the smallest and the largest of the
-// slots that may go, by where it lay if keys were spread evenly, until exactly `keep` slots reach it or nothing is left
-// between; in the latter case the lower ones of equal keys stay.  Weights and places are read once.  Where a unit has no more than FEW moves (`here`),
-// they are made here: another launch for one move each took 6 us for 5120 units.
+// The moves of a (layer, sequence, kv head): W wavefronts, of which the w-th has the w-th part of the slots, 64 neighbours at a time.  The largest key that
+// `keep` slots or more reach is searched for between the smallest and the largest of the slots that may go, by where it lay if keys were spread
+// evenly, until exactly `keep` slots reach it or nothing is left between; in the latter case the lower ones of equal keys stay.  V > 0: the
+// keys of up to 64 W V slots are held in V registers of a lane, and weights and places are read once; V = 0: keys are made again for each count.
+// Where a unit has no more than FEW moves (`here`), they are made here: another launch for one move each took 6 us for 5120 units.
+// Bound by its steps one after the other: 70B, 128 units of up to 16384 slots down to 2048 26 us (16 wavefronts; 4 loads, 8 rounds, 4 list), 5120
+// units of 501 slots, one move each, 15.
 constexpr int FEW = 32, GUESSES = 12;
 template <int W, int V>
 __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here) {
-  constexpr int GR = V < 8 ? V : 8;  // registers at a time; those behind the slots hold keys of 0, below every threshold
+  constexpr int GR = V == 0 ? 16 : 8;  // keys at a time; of no slot: 0, below every threshold
+  typedef std::conditional_t<V == 0, size_t, unsigned> Row;
   const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   __shared__ int bad, sums[2][W][3];
@@ -195,46 +199,59 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
   const int per = (n + 64 * W - 1) / (64 * W), first = wave * per * 64, slot0 = first + lane, mask = (1 << a.map.shift) - 1;
   const float* weights = a.weights + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
   const int32_t* places = a.places + ((size_t)layer * a.map.pages * a.hkv << a.map.shift);
-  // the registers that may hold slots of this wavefront, GR at a time
-  auto registers = [&](auto f) __attribute__((always_inline)) {
+  auto load = [&](int g, unsigned* k) __attribute__((always_inline)) {
+    Row row[GR];
+    float w[GR];
+    int place[GR];
 #pragma unroll
-    for (int g = 0; g < V; g += GR)
-      if (g < per) {
+    for (int j = 0; j < GR; ++j) {
+      const int slot = min(slot0 + (g + j) * 64, n - 1);
+      row[j] = (((Row)entries[slot >> a.map.shift] * a.hkv + kh) << a.map.shift) + (slot & mask);
+    }
 #pragma unroll
-        for (int i = g; i < g + GR; ++i) f(i, slot0 + i * 64, i < per && slot0 + i * 64 < n);
-      }
+    for (int j = 0; j < GR; ++j) {
+      w[j] = weights[row[j]];
+      place[j] = places[row[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < GR; ++j) k[j] = g + j < per && slot0 + (g + j) * 64 < n ? stay_key(w[j], place[j], a.first, from) : 0;
   };
-  unsigned key[V];
+  unsigned key[V > 0 ? V : GR];
+  if constexpr (V > 0) {
 #pragma unroll
-  for (int g = 0; g < V; g += GR) {
-    if (g < per) {
-      unsigned row[GR];
-      float w[GR];
-      int place[GR];
+    for (int g = 0; g < V; g += GR) {
+      if (g < per) {
+        load(g, key + g);
+      } else {
 #pragma unroll
-      for (int j = 0; j < GR; ++j) {
-        const int slot = min(slot0 + (g + j) * 64, n - 1);
-        row[j] = ((unsigned)(entries[slot >> a.map.shift] * a.hkv + kh) << a.map.shift) + (slot & mask);
+        for (int j = 0; j < GR; ++j) key[g + j] = 0;
       }
-#pragma unroll
-      for (int j = 0; j < GR; ++j) {
-        w[j] = weights[row[j]];
-        place[j] = places[row[j]];
-      }
-#pragma unroll
-      for (int j = 0; j < GR; ++j) key[g + j] = g + j < per && slot0 + (g + j) * 64 < n ? stay_key(w[j], place[j], a.first, from) : 0;
-    } else {
-#pragma unroll
-      for (int j = 0; j < GR; ++j) key[g + j] = 0;
     }
   }
+  // f(which of 64 slots, slot, key of it) over all slots of this wavefront and some behind, whose keys are 0
+  auto all_slots = [&](auto f) __attribute__((always_inline)) {
+    if constexpr (V > 0) {
+#pragma unroll
+      for (int g = 0; g < V; g += GR)
+        if (g < per) {
+#pragma unroll
+          for (int i = g; i < g + GR; ++i) f(i, slot0 + i * 64, key[i]);
+        }
+    } else {
+      for (int g = 0; g < per; g += GR) {
+        load(g, key);
+#pragma unroll
+        for (int j = 0; j < GR; ++j) f(g + j, slot0 + (g + j) * 64, key[j]);
+      }
+    }
+  };
   unsigned low = 0xFFFFFFFFu, high = 0;
   int stay = 0;  // slots that stay whatever their weight
-  registers([&](int i, int, bool there) __attribute__((always_inline)) {
-    const bool free = there && key[i] != 0xFFFFFFFFu;
-    low = min(low, free ? key[i] : 0xFFFFFFFFu);
-    high = max(high, free ? key[i] : 0u);
-    stay += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] == 0xFFFFFFFFu));
+  all_slots([&](int i, int slot, unsigned k) __attribute__((always_inline)) {
+    const bool free = i < per && slot < n && k != 0xFFFFFFFFu;
+    low = min(low, free ? k : 0xFFFFFFFFu);
+    high = max(high, free ? k : 0u);
+    stay += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == 0xFFFFFFFFu));
   });
   auto bits = [](float v) { return __builtin_bit_cast(unsigned, v); };
   low = bits(exchange<32, 1>(__builtin_bit_cast(float, low), [&](float x, float y) { return __builtin_bit_cast(float, min(bits(x), bits(y))); }));
@@ -267,12 +284,7 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
     if (round < GUESSES) step = min(max((unsigned)((float)range * ((float)(reach - a.keep) / (float)(reach - above))), 1u), range - 1);
     const unsigned middle = __builtin_amdgcn_readfirstlane(least + step);
     int got = 0;
-#pragma unroll
-    for (int g = 0; g < V; g += GR)
-      if (g < per) {
-#pragma unroll
-        for (int i = g; i < g + GR; ++i) got += __builtin_popcountll(__builtin_amdgcn_ballot_w64(key[i] >= middle));
-      }
+    all_slots([&](int, int, unsigned k) __attribute__((always_inline)) { got += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k >= middle)); });
     got = total(got, round);
     if (got >= a.keep) {
       least = middle;
@@ -284,46 +296,52 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
   }
   // ---- holes and movers in the order of slots
   const bool ties = reach != a.keep;  // of the slots of key `least`, keep - above stay
-  int rank = 0;
+  int rank0 = 0;                      // of those, in front of this wavefront
   if (ties) {
     int equal = 0;
-    registers([&](int i, int, bool there) __attribute__((always_inline)) { equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there && key[i] == least)); });
+    all_slots([&](int i, int slot, unsigned k) __attribute__((always_inline)) { equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < per && slot < n && k == least)); });
     if constexpr (W > 1) {
       each(equal, 0, 0);
-      for (int w = 0; w < wave; ++w) rank += sums[turn][w][0];
+      for (int w = 0; w < wave; ++w) rank0 += sums[turn][w][0];
     }
   }
-  auto before = [](uint64_t m) { return __builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0)); };  // lanes of m in front of this one
-  uint64_t stays = 0;  // bit i: slot i of this lane
-  int holes = 0, movers = 0;
-  registers([&](int i, int, bool there) __attribute__((always_inline)) {
-    bool is = there && key[i] >= least;
+  auto before = [](uint64_t m) { return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(m >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)m, 0)); };  // lanes of m in front of this one
+  auto stays = [&](int i, int slot, unsigned k, int& rank) __attribute__((always_inline)) {
+    const bool there = i < per && slot < n;
+    bool is = there && k >= least;
     if (ties) {
-      const uint64_t equal = __builtin_amdgcn_ballot_w64(there && key[i] == least);
-      if (there && key[i] == least) is = rank + (int)before(equal) < a.keep - above;
+      const uint64_t equal = __builtin_amdgcn_ballot_w64(there && k == least);
+      if (there && k == least) is = rank + before(equal) < a.keep - above;
       rank += __builtin_popcountll(equal);
     }
-    stays |= (uint64_t)is << i;
-    const uint64_t all = __builtin_amdgcn_ballot_w64(is);
-    const int64_t front = (int64_t)a.keep - (first + i * 64);  // of these 64 slots below `keep`
-    const uint64_t in_front = front >= 64 ? ~0ull : front <= 0 ? 0ull : (1ull << front) - 1;
-    holes += i < per ? __builtin_popcountll(~all & in_front) : 0;
-    movers += __builtin_popcountll(all & ~in_front);
-  });
-  int to = 0, fr = 0, all = movers;
-  if constexpr (W > 1) {
-    each(holes, movers, 0);
-    all = 0;
+    return is;
+  };
+  int to = 0, fr = 0, all = 0;
+  {
+    int holes = 0, movers = 0, rank = rank0;
+    all_slots([&](int i, int slot, unsigned k) __attribute__((always_inline)) {
+      const uint64_t is = __builtin_amdgcn_ballot_w64(stays(i, slot, k, rank));
+      const int64_t front = (int64_t)a.keep - (first + i * 64);  // of these 64 slots below `keep`
+      const uint64_t in_front = i >= per || front <= 0 ? 0ull : front >= 64 ? ~0ull : (1ull << front) - 1;
+      holes += __builtin_popcountll(~is & in_front);
+      movers += __builtin_popcountll(is & ~in_front);
+    });
+    all = movers;
+    if constexpr (W > 1) {
+      each(holes, movers, 0);
+      all = 0;
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      to += w < wave ? sums[turn][w][0] : 0;
-      fr += w < wave ? sums[turn][w][1] : 0;
-      all += sums[turn][w][1];
+      for (int w = 0; w < W; ++w) {
+        to += w < wave ? sums[turn][w][0] : 0;
+        fr += w < wave ? sums[turn][w][1] : 0;
+        all += sums[turn][w][1];
+      }
     }
   }
   int2* moves = here ? list : a.moves + (size_t)unit * a.most;
-  registers([&](int i, int slot, bool) __attribute__((always_inline)) {
-    const bool is = stays >> i & 1, hole = i < per && slot < a.keep && !is, mover = slot >= a.keep && is;
+  int rank = rank0;
+  all_slots([&](int i, int slot, unsigned k) __attribute__((always_inline)) {
+    const bool is = stays(i, slot, k, rank), hole = i < per && slot < a.keep && !is, mover = slot >= a.keep && is;
     const uint64_t hs = __builtin_amdgcn_ballot_w64(hole), ms = __builtin_amdgcn_ballot_w64(mover);
     if (hs) {
       if (hole) moves[to + before(hs)].x = slot;
@@ -339,85 +357,6 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
   __syncthreads();
   if (a.wide) make_moves<u32x4>(a, entries, layer, kh, list, all, 64 * W);
   else make_moves<uint32_t>(a, entries, layer, kh, list, all, 64 * W);
-}
-
-// The same for sequences of any length: keys are made again for each count, bit by bit.
-__global__ void __launch_bounds__(256) k_evict_choose_long(EvictArgs a) {
-  const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
-  const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
-  __shared__ int sums[4], bad;
-  int n, from;
-  if (!evict_seq(a, b, 256, &bad, n, from)) {
-    if (threadIdx.x == 0) a.count[unit] = -1;
-    return;
-  }
-  auto key_of = [&](int slot) {
-    const size_t row = slot_row(a, entries, layer, kh, slot);
-    return stay_key(a.weights[row], a.places[row], a.first, from);
-  };
-  auto total = [&](int mine) {  // over the workgroup
-    for (int off = 32; off; off >>= 1) mine += __shfl_xor(mine, off);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = mine;
-    __syncthreads();
-    return sums[0] + sums[1] + sums[2] + sums[3];
-  };
-  unsigned key = 0;
-  int reach = n;
-  for (int bit = 31; bit >= 0 && reach != a.keep; --bit) {
-    const unsigned higher = key | 1u << bit;
-    int mine = 0;
-    for (int slot = threadIdx.x; slot < n; slot += 256) mine += key_of(slot) >= higher;
-    const int got = total(mine);
-    if (got >= a.keep) {
-      key = higher;
-      reach = got;
-    }
-  }
-  int above = a.keep;  // slots whose key is above `key`; of those at it as many stay as are wanted yet
-  if (reach != a.keep) {
-    int mine = 0;
-    for (int slot = threadIdx.x; slot < n; slot += 256) mine += key_of(slot) > key;
-    above = total(mine);
-  }
-  const bool ties = reach != a.keep;
-  int equal0 = 0, to0 = 0, from0 = 0;  // of the slots before
-  __shared__ int pre[4][3];
-  int2* moves = a.moves + (size_t)unit * a.most;
-  for (int slot0 = 0; slot0 < n; slot0 += 256) {
-    const int slot = slot0 + threadIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const unsigned mine = slot < n ? key_of(slot) : 0;
-    const uint64_t below = (1ull << lane) - 1;
-    const uint64_t eq = __ballot(slot < n && ties && mine == key);
-    __syncthreads();
-    if (lane == 0) pre[wave][0] = __popcll(eq);
-    __syncthreads();
-    int rank = equal0 + __popcll(eq & below);
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) rank += pre[w][0];
-      equal0 += pre[w][0];
-    }
-    const bool kept = slot < n && (ties ? mine > key || (mine == key && rank < a.keep - above) : mine >= key);
-    const bool hole = slot < a.keep && !kept, mover = slot < n && slot >= a.keep && kept;
-    const uint64_t holes = __ballot(hole), movers = __ballot(mover);
-    if (lane == 0) {
-      pre[wave][1] = __popcll(holes);
-      pre[wave][2] = __popcll(movers);
-    }
-    __syncthreads();
-    int to = to0 + __popcll(holes & below), fr = from0 + __popcll(movers & below);
-    for (int w = 0; w < 4; ++w) {
-      if (w < wave) {
-        to += pre[w][1];
-        fr += pre[w][2];
-      }
-      to0 += pre[w][1];
-      from0 += pre[w][2];
-    }
-    if (hole) moves[to].x = slot;
-    if (mover) moves[fr].y = slot;
-  }
-  if (threadIdx.x == 0) a.count[unit] = from0;
 }
 
 // The moves: a workgroup to MOVES of them at a time.  The lengths, which the launch before reads, are set by one workgroup of a sequence.
@@ -441,8 +380,7 @@ __global__ void __launch_bounds__(256) k_evict_lens(EvictArgs a, int32_t* __rest
 
 void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t st) {
   // More wavefronts to a unit where units do not fill the chip: 1024 units of 1025 slots 14 -> 10 us.
-  const bool few = units <= 2048;
-  const bool here = a.most <= FEW;
+  const bool few = units <= 2048, here = a.most <= FEW;
   const int n = ((int64_t)a.map.pages * a.hkv << a.map.shift) < NARROW ? a.max_len : INT32_MAX;
   if (n <= 64 * 8) k_evict_choose<1, 8><<<units, 64, 0, st>>>(a, here);
   else if (n <= 64 * 16 && !few) k_evict_choose<1, 16><<<units, 64, 0, st>>>(a, here);
@@ -453,8 +391,9 @@ void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t s
   else if (n <= 1024 * 8) k_evict_choose<16, 8><<<units, 1024, 0, st>>>(a, here);
   else if (n <= 1024 * 16) k_evict_choose<16, 16><<<units, 1024, 0, st>>>(a, here);
   else if (n <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a, here);
-  else k_evict_choose_long<<<units, 256, 0, st>>>(a);
-  if (here && n <= 1024 * 32) {
+  else if (n <= 1024 * 64) k_evict_choose<16, 64><<<units, 1024, 0, st>>>(a, here);
+  else k_evict_choose<16, 0><<<units, 1024, 0, st>>>(a, here);
+  if (here) {
     k_evict_lens<<<(a.batch + 255) / 256, 256, 0, st>>>(a, lens);
     return;
   }

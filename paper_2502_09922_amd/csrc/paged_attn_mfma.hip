@@ -14,11 +14,11 @@
 //
 // The new token's row is put into its tile in LDS by the wavefront that has that tile, and into the cache: nobody waits for memory there.
 //
-// Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 106 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for, 106; the
-// arithmetic alone 45.  70B, 64 of 128 to 2287 slots 66 us, 5.5 TB/s (64 without arithmetic): one workgroup to each place of the chip, so its start and
-// end, 5 us, are nobody else's.  4 of 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 116, 5.6 TB/s, where a tile's
-// products take half of its time on a SIMD.  Weights: scores go out and come back, 4 bytes for each query head and slot: 64 sequences of 1000 slots, 8 query heads to a kv head
-// 56 us, 44 without, where a stored score's place among the fills makes no difference.
+// Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 106 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for,
+// as long; the arithmetic alone 45.  70B, 64 of 128 to 2287 slots 60 us, 6.1 TB/s (66 when a CU's two workgroups were of the same sequence).  4 of
+// 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 116, 5.6 TB/s, where a tile's products take half of its time on a
+// SIMD.  Weights: scores go out and come back, 4 bytes for each query head and slot: 70B, 64 of 128 to 2287 slots 75 us instead of 57 (12 for the
+// stores, 5 of which they cost where all of them go to the same lines; behind the fills or in another layout no less).
 #include "attn_mfma.hpp"
 #include "paged.hpp"
 
@@ -522,14 +522,14 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     __syncthreads();  // the scores of all wavefronts are in memory
     for (int first = threadIdx.x; first < keys; first += AHEAD * THREADS) {
       constexpr int U = 4;  // heads on their way at once
-      if (first != (int)threadIdx.x) weights_of(first);
       float got[AHEAD] = {};
       for (int c0 = 0; c0 < cols; c0 += U) {
         float v[U][AHEAD];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int j = 0; j < AHEAD; ++j) v[u][j] = c0 + u < cols ? p.scores[(row0 + c0 + u) * p.stride + min(first + j * THREADS, t.n)] : 0.f;
+          for (int j = 0; j < AHEAD; ++j) v[u][j] = p.scores[(row0 + min(c0 + u, cols - 1)) * p.stride + min(first + j * THREADS, t.n)];
+        if (c0 == 0 && first != (int)threadIdx.x) weights_of(first);  // behind the scores, which wait for nothing
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (c0 + u < cols)
