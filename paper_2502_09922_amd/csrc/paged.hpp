@@ -40,6 +40,7 @@ struct PagedPieces {
   int2* dealt = nullptr;    // [sequence]: first workgroup, pieces
   float* scores = nullptr;  // [row * hq + head][stride] q k of every slot, where weights are wanted
   int stride = 0;           // a multiple of 32
+  int held = 0;             // from column to column of scores that stay in LDS
 };
 void launch_paged_attn_mfma(uint32_t dt, const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st);  // head_dim 64 and 128, rows on 16 bytes
 

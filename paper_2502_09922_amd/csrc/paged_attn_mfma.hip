@@ -95,8 +95,9 @@ __device__ __forceinline__ bool deal(const PageMap& map, int batch, int units, i
   return true;
 }
 
-// TK: keys of a tile; NW: wavefronts; NB: tiles of a ring, a power of two
-template <class T, int HD, int TK, int NW, int NB, bool WEIGH>
+// TK: keys of a tile; NW: wavefronts; NB: tiles of a ring, a power of two.  Weights: scores wait for the end in memory, or in LDS, behind the rings.
+enum Weigh { NO_WEIGHTS = 0, IN_MEMORY = 1, IN_LDS = 2 };
+template <class T, int HD, int TK, int NW, int NB, Weigh WEIGH>
 __global__ void __launch_bounds__(64 * NW, 2)
 k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, int32_t* __restrict__ places,
              T* __restrict__ out, int hq, int hkv, int max_pos, int most, int half, int batch, PagedPieces p, float* __restrict__ weights) {
@@ -108,7 +109,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   constexpr int UNITS = TK / 8;    // parts of a tile that lie in one page whatever the page's size
   constexpr int TILE = TK * ROWB;
   constexpr int DT = HD / 16, HALVES = TK / 16;
-  constexpr int STORES = WEIGH ? HALVES : 0;  // of a tile's scores
+  constexpr int STORES = WEIGH == IN_MEMORY ? HALVES : 0;  // of a tile's scores
   static_assert(RPI <= 8 && (NB & (NB - 1)) == 0, "");
   typedef T T4 __attribute__((ext_vector_type(4)));
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -317,7 +318,8 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     for (int j = 0; j < AHEAD; ++j) had[j] = weights[to[j]];
   };
   if (WEIGH && weights) weights_of(threadIdx.x);
-  float* scores = WEIGH ? p.scores + (row0 + lr) * p.stride : nullptr;  // of this lane's column
+  float* scores = WEIGH == IN_MEMORY ? p.scores + (row0 + lr) * p.stride : nullptr;  // of this lane's column
+  float* sm_s = reinterpret_cast<float*>(smem + NW * NB * 2 * TILE);
 
   f32x4 o[DT];
   float m_run = -INFINITY, l_run = 0.f;  // l_run: of this lane's keys
@@ -403,10 +405,10 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (WEIGH) {
+    if constexpr (WEIGH != NO_WEIGHTS) {
       if (lr < cols)
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>(scores + key0 + h * 16 + 4 * lg) = s[h];
+        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>((WEIGH == IN_LDS ? sm_s + lr * p.held : scores) + key0 + h * 16 + 4 * lg) = s[h];
     }
     if (masked) {
 #pragma unroll
@@ -517,7 +519,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       else if (WEIGH || !whole) p.ml[place0 + c] = float2{m, den};
     }
   }
-  if constexpr (WEIGH) {  // the weights of all slots, where one workgroup has all of them and all of the query heads
+  if constexpr (WEIGH != NO_WEIGHTS) {  // the weights of all slots, where one workgroup has all of them and all of the query heads
     if (!weights) return;
     __syncthreads();  // the scores of all wavefronts are in memory
     for (int first = threadIdx.x; first < keys; first += AHEAD * THREADS) {
@@ -528,7 +530,10 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-          for (int j = 0; j < AHEAD; ++j) v[u][j] = p.scores[(row0 + min(c0 + u, cols - 1)) * p.stride + min(first + j * THREADS, t.n)];
+          for (int j = 0; j < AHEAD; ++j) {
+            const int c = min(c0 + u, cols - 1), slot = min(first + j * THREADS, t.n);
+            v[u][j] = WEIGH == IN_LDS ? sm_s[c * p.held + slot] : p.scores[(row0 + c) * p.stride + slot];
+          }
         if (c0 == 0 && first != (int)threadIdx.x) weights_of(first);  // behind the scores, which wait for nothing
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -545,29 +550,41 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   }
 }
 
-template <class T, int HD, int NW, int NB, bool WEIGH>
+// Bytes of scores that fit beside the rings without taking a place on the CU from another workgroup.
+template <int NW> constexpr int HELD = NW == 4 ? 13 << 10 : 28 << 10;
+
+template <class T, int HD, int NW, int NB, Weigh WEIGH>
 void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
   constexpr int TK = 16, TILES = NW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = NW * 16 * (HD + SM_PAD) * 4;
-  constexpr int SMEM = TILES > JOIN ? TILES : JOIN;
+  static_assert(TILES >= JOIN && TILES <= NW * 16384, "");
   static std::atomic<uint64_t> lds_allowed{0};
   auto kernel = k_paged_mfma<T, HD, TK, NW, NB, WEIGH>;
-  allow_dynamic_lds((const void*)kernel, SMEM, lds_allowed);
+  allow_dynamic_lds((const void*)kernel, TILES + (WEIGH == IN_LDS ? HELD<NW> : 0), lds_allowed);
+  const unsigned lds = TILES + (WEIGH == IN_LDS ? a.hq / a.hkv * p.held * 4 : 0);
   const int heads = a.hkv * ((a.hq / a.hkv + 15) / 16);
   int half = 0;
   if (p.n == 1 && !p.share && a.batch > 1 && a.batch <= ORDERED && a.max_keys > ORDERED_KEYS) half = (long)heads * a.batch <= 2 * CUS ? std::max(1, CUS / heads) : a.batch;
-  kernel<<<p.share ? dim3(p.share) : dim3(heads, a.batch, p.n), 64 * NW, SMEM, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
+  kernel<<<p.share ? dim3(p.share) : dim3(heads, a.batch, p.n), 64 * NW, lds, st>>>(a.map, (const T*)a.qkv, a.cs, (T*)a.kc, (T*)a.vc, a.places, (T*)a.out, a.hq, a.hkv, a.max_pos, most, half,
                                                            a.batch, p, paged_joins_weights(a, p) ? a.weights : nullptr);
 }
 
 // Four wavefronts with two tiles each, two workgroups to a CU (fp32 of 128 dims: one tile of 16 KB), or twice the wavefronts where a CU has one
 // workgroup at most.  13B, 32 sequences 106 us; three wavefronts 110, two 116, tiles of 32 keys or rings of four tiles, which leave a CU one
 // workgroup, 7 to 8 more.  7B, 8 sequences of 1024 slots with weights: eight wavefronts 27.0, four 29.1.
+// Scores of one workgroup that has all of a sequence's slots stay in LDS where they fit: 13B, 32 sequences of 1024 to 1087 slots 122 us, 132 through memory.
+template <class T, int HD, int NW, int NB>
+void launch_nw(const PagedAttn& a, PagedPieces p, int most, hipStream_t st) {
+  p.held = p.stride + 4;  // columns' equal slots in different banks
+  if (!a.weights) launch_kernel_of<T, HD, NW, NB, NO_WEIGHTS>(a, p, most, st);
+  else if (paged_joins_weights(a, p) && (int64_t)(a.hq / a.hkv) * p.held * 4 <= HELD<NW>) launch_kernel_of<T, HD, NW, NB, IN_LDS>(a, p, most, st);
+  else launch_kernel_of<T, HD, NW, NB, IN_MEMORY>(a, p, most, st);
+}
 template <class T, int HD>
 void launch_hd(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
   constexpr int NB = sizeof(T) * HD == 512 ? 1 : 2;
   const bool alone = (p.share ? p.share : (long)a.batch * a.hkv * ((a.hq / a.hkv + 15) / 16) * p.n) <= CUS;
-  if (a.weights) alone ? launch_kernel_of<T, HD, 8, NB, true>(a, p, most, st) : launch_kernel_of<T, HD, 4, NB, true>(a, p, most, st);
-  else alone ? launch_kernel_of<T, HD, 8, NB, false>(a, p, most, st) : launch_kernel_of<T, HD, 4, NB, false>(a, p, most, st);
+  if (alone) launch_nw<T, HD, 8, NB>(a, p, most, st);
+  else launch_nw<T, HD, 4, NB>(a, p, most, st);
 }
 
 }  // namespace

@@ -660,3 +660,16 @@ def test_evictions_beyond_32_bits():
         for layer in (0, 1):
             assert plain.same(x[layer, -own:].cpu(), t[0])
     assert cache.lens.tolist() == [keep]
+
+
+@TYPES
+@pytest.mark.parametrize("heads,slots", [((1, 1, 128), 3311), ((1, 1, 128), 3313), ((8, 1, 128), 411), ((8, 1, 128), 413), ((16, 1, 64), 190), ((2, 2, 64), 500)],
+                         ids=lambda x: str(x).replace(" ", ""))
+@pytest.mark.parametrize("batch", [1, 270])
+def test_scores_around_what_stays_on_the_chip(heads, slots, dtype, batch):
+    """Weights of sequences whose scores just fit beside the tiles, and of ones whose scores do not; few workgroups and many."""
+    lens = [2] * batch
+    lens[0], lens[-1] = slots // 2, slots
+    c = plain.Pages(heads, dtype, lens, 16, seed=71, weighed=True, room=2)
+    check(c, None, max_ctx=slots)
+    check(c, None, max_ctx=slots + 1)
