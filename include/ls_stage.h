@@ -412,7 +412,7 @@ typedef struct {
   float* weights;           /* optional [layers][pages][n_kv_heads][page]: attention weight that a slot has got so far     */
   int32_t* places;          /* with weights: position of the slot's token                                                  */
   int32_t* lens;            /* [max_batch] slots that are filled, the first ones; below 0: the sequence takes no part      */
-  int32_t* positions;       /* optional [max_batch]: position of the sequence's next token; NULL: lens, for nothing is evicted */
+  int32_t* positions;       /* optional [max_batch]: position of the sequence's next token; NULL: lens, for nothing is evicted; not lens itself */
   const int32_t* table;     /* [max_batch][columns] pages; an entry outside [0, pages) names none                          */
   uint32_t pages;           /* pages of the pool                                                                           */
   uint32_t page;            /* slots of a page: a power of two from 8 to 1024                                              */
@@ -431,7 +431,7 @@ size_t ls_paged_attention_scratch_bytes(const ls_heads* heads, const ls_pages* l
  *   rope     fp32 [max_seq][head_dim/2][2], cos and sin (see ls_tree_attention), or NULL: rows come turned
  *   layer    one layer's pools.  With weights, every slot's weight grows by what the query heads of its kv head give it (the softmax's values,
  *            summed over those heads), the new slot's starts with that, and its place is the token's position.
- *   out      [batch, n_q_heads * head_dim]
+ *   out      [batch, n_q_heads * head_dim], not over qkv
  *   max_ctx  host-side upper bound of lens[b]; max_ctx + 1 beyond columns * page is LS_ERR_KV_OVERFLOW, and beyond max_seq too where
  *            rope is given and positions are not.  Without weights an understated bound costs speed, never slots; with
  *            weights a sequence of more slots counts as one without room.
@@ -454,7 +454,7 @@ ls_status ls_paged_attention(const ls_heads* heads, const ls_pages* layer, int b
  *             zeros.  Places are the positions.
  *   max_len   host-side upper bound of n; an understated one costs speed, never positions
  * Slots without a page are left out.  Caches on 4 bytes for bf16 too.  A page that several sequences of the call name gets the rows of one of them,
- * which have to be the same; `from` and the pools do not overlap.
+ * which have to be the same; `from` and the pages' buffers do not overlap.
  */
 ls_status ls_paged_fill(const ls_heads* heads, int layers, const ls_kv* from, int from_batch, int from_seq, const int32_t* src, const float* weights,
                         int max_len, const ls_pages* pages, int batch, void* hip_stream);
@@ -465,7 +465,7 @@ ls_status ls_paged_fill(const ls_heads* heads, int layers, const ls_kv* from, in
  * is no number is below all others.  (Where more than `keep` slots are of such positions, the lowest slots of them.)  Kept slots below `keep` stay
  * where they are; the kept ones behind, in order, go to the slots below `keep` that are not kept, in order: key, value, weight and
  * place.  lens[b] becomes keep; what lies behind is left as it is, so pages behind slot keep - 1 are the caller's again.
- *   pages    with weights and places; all layers.  positions NULL: lens, as far as nothing has been evicted.
+ *   pages    with weights, places and positions; all layers
  *   keep     at least 1;  first, recent: at least 0, first + recent at most keep
  *   max_len  host-side upper bound of lens[b]; a sequence with more is left alone
  *   scratch  of ls_paged_evict_scratch_bytes (0: invalid sizes), 16-byte aligned; nothing in it outlasts the call

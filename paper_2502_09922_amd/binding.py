@@ -365,7 +365,6 @@ class PagedCache:
             self._heads[(n_q_heads, max_seq)] = h
         return h
 
-
     def attention_call(self, columns: int, max_seq: int, max_ctx: int):
         """(n_q_heads, ls_heads, scratch bytes) of an attention call over rows of so many columns: of one size step after step."""
         if self._call is None or self._call[0] != (columns, max_seq, max_ctx):
@@ -423,7 +422,7 @@ def paged_fill(cache: PagedCache, k, v, seq_lens, src, max_len: int, weights=Non
 
 def paged_evict(cache: PagedCache, keep: int, recent: int, max_len: int, first: int = 0):
     """Cut sequences down to `keep` slots (ls_paged_evict): the first `first` positions and the newest `recent` stay, and of the others those
-    of the largest weights; max_len: a bound of lens."""
+    of the largest weights; the cache has positions; max_len: a bound of lens."""
     device = cache.device
     heads, layers = cache.heads(cache._t["k"].shape[2], 1 << 24), cache._t["k"].shape[0]
     nb = lib.ls_paged_evict_scratch_bytes(heads, layers, cache.batch, keep, max_len)

@@ -105,7 +105,7 @@ __device__ __forceinline__ size_t slot_row(const EvictArgs& a, const int32_t* en
 // Slots and positions of a unit's sequence; false if it is left alone, whose entries all threads of the workgroup look at.
 __device__ __forceinline__ bool evict_seq(const EvictArgs& a, int b, int threads, int* bad, int& n, int& from) {
   n = a.map.lens[b];
-  const int pos = a.map.positions ? a.map.positions[b] : n;
+  const int pos = a.map.positions[b];
   from = pos < a.recent ? 0 : pos - a.recent;
   if (n <= a.keep || n > a.max_len || (n - 1) >> a.map.shift >= a.map.columns) return false;
   const int32_t* entries = a.map.table + (size_t)b * a.map.columns;
@@ -403,6 +403,10 @@ void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t s
 }
 
 // ---- arguments ---------------------------------------------------------------------------------------------------------------
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
 const char* pages_error(const ls_heads* h, const ls_pages* p, int batch) {
   if (!p || !p->k || !p->v || !p->lens || !p->table) return "NULL ls_pages or pointer inside it";
   if (p->page < 8 || p->page > 1024 || (p->page & (p->page - 1))) return "page has to be a power of two from 8 to 1024";
@@ -413,7 +417,13 @@ const char* pages_error(const ls_heads* h, const ls_pages* p, int batch) {
   const uintptr_t size = h->dtype == LS_DTYPE_F32 ? 4 : 2;
   if (((uintptr_t)p->k | (uintptr_t)p->v) & (size - 1)) return "a pool is not aligned to its type";
   if (((uintptr_t)p->weights | (uintptr_t)p->places | (uintptr_t)p->lens | (uintptr_t)p->positions | (uintptr_t)p->table) & 3) return "a buffer is not aligned to its type";
+  if (overlap(p->lens, h->max_batch * 4ull, p->positions, h->max_batch * 4ull)) return "lens and positions are one buffer";
   return nullptr;
+}
+
+// Whether no launch takes the weights of so many slots.
+bool too_many_weights(const ls_heads* h, const ls_pages* p, int max_ctx) {
+  return p->weights && (int64_t)h->n_kv_heads * ((int64_t)max_ctx / 256 + 1) >= (1 << 24) - (1 << 16);
 }
 
 PageMap map_of(const ls_pages* p) {
@@ -455,6 +465,7 @@ ls_status paged_attention_args(const char* who, const ls_heads* h, const ls_page
   if (const char* e = pages_error(h, p, batch)) return bad(who, e);
   const ls_status rc = context_error(who, h, p, max_ctx, turns);
   if (rc != LS_OK) return rc;
+  if (too_many_weights(h, p, max_ctx)) return bad(who, "weights of more slots than a launch takes");
   *a = attn_of(h, p, batch, max_ctx);
   if (a->weights) {
     const size_t need = paged_attn_scratch_bytes(*a);
@@ -481,7 +492,7 @@ size_t evict_units(const ls_heads* h, int layers, int batch) { return (size_t)la
 const char* evict_error(const ls_heads* h, int layers, int batch, int keep, int max_len) {
   if (const char* e = ls::heads_error(h)) return e;
   if (batch < 1 || batch > (int)h->max_batch || batch > 65535) return "batch outside [1, max_batch], or beyond 65535";
-  if (layers < 1 || layers > (1 << 20) || evict_units(h, layers, batch) >= (1u << 24)) return "layers outside [1, what a launch takes]";
+  if (layers < 1 || layers > (1 << 20) || evict_units(h, layers, batch) >= (1u << 22)) return "layers outside [1, what a launch takes]";
   if (keep < 1) return "keep has to be at least 1";
   if (max_len < 0 || max_len > (1 << 24)) return "max_len outside [0, 2^24]";
   return nullptr;
@@ -492,7 +503,7 @@ const char* evict_error(const ls_heads* h, int layers, int batch, int keep, int 
 extern "C" {
 
 size_t ls_paged_attention_scratch_bytes(const ls_heads* h, const ls_pages* layer, int batch, int max_ctx) {
-  if (ls::heads_error(h) || ls::pages_error(h, layer, batch) || max_ctx < 0 || (uint64_t)max_ctx + 1 > (uint64_t)layer->columns * layer->page) return 0;
+  if (ls::heads_error(h) || ls::pages_error(h, layer, batch) || max_ctx < 0 || (uint64_t)max_ctx + 1 > (uint64_t)layer->columns * layer->page || ls::too_many_weights(h, layer, max_ctx)) return 0;
   return ls::paged_attn_scratch_bytes(ls::attn_of(h, layer, batch, max_ctx));
 }
 
@@ -506,6 +517,8 @@ ls_status ls_paged_attention(const ls_heads* h, const ls_pages* layer, int batch
   const uintptr_t size = h->dtype == LS_DTYPE_F32 ? 4 : 2;
   if (((uintptr_t)qkv | (uintptr_t)out) & (size - 1)) return bad(who, "a buffer is not aligned to its type");
   if ((uintptr_t)rope & 7) return bad(who, "rope is not aligned to 8 bytes");
+  const uint64_t row = (uint64_t)batch * h->head_dim * size;
+  if (ls::overlap(qkv, row * (h->n_q_heads + 2ull * h->n_kv_heads), out, row * h->n_q_heads)) return bad(who, "out overlaps qkv");
   a.qkv = qkv; a.cs = rope; a.out = out;
   ls::launch_paged_attn(h->dtype, a, (hipStream_t)hip_stream);
   return launched(who);
@@ -521,6 +534,8 @@ ls_status ls_paged_fill(const ls_heads* h, int layers, const ls_kv* from, int fr
   const uintptr_t at = (uintptr_t)from->k | (uintptr_t)from->v | (uintptr_t)pages->k | (uintptr_t)pages->v;
   if (at & 3) return bad(who, "a cache is not aligned to 4 bytes");
   if (((uintptr_t)src | (uintptr_t)from->seq_lens | (uintptr_t)weights) & 3) return bad(who, "a buffer is not aligned to its type");
+  if (ls::overlap(from->seq_lens, from_batch * 4ull, pages->lens, batch * 4ull) || ls::overlap(from->seq_lens, from_batch * 4ull, pages->positions, batch * 4ull))
+    return bad(who, "seq_lens overlaps lens or positions");
   if (max_len < 0) return bad(who, "max_len is negative");
   const size_t row = (size_t)h->head_dim * (h->dtype == LS_DTYPE_F32 ? 4 : 2);
   const bool wide = row % 16 == 0 && (at & 15) == 0;
@@ -554,6 +569,7 @@ ls_status ls_paged_evict(const ls_heads* h, int layers, const ls_pages* pages, i
   if (const char* e = evict_error(h, layers, batch, keep, max_len)) return bad(who, e);
   if (const char* e = ls::pages_error(h, pages, batch)) return bad(who, e);
   if (!pages->weights) return bad(who, "pages without weights and places");
+  if (!pages->positions) return bad(who, "pages without positions, which lens do not give any more");
   if (first < 0 || recent < 0 || (int64_t)first + recent > keep) return bad(who, "first and recent are at least 0 and together at most keep");
   const uintptr_t at = (uintptr_t)pages->k | (uintptr_t)pages->v;
   if (at & 3) return bad(who, "a pool is not aligned to 4 bytes");

@@ -316,7 +316,7 @@ PagedPieces pieces_for(const PagedAttn& a, size_t room) {
       if (p.share > base) return p;
       p.share = 0;
     }
-    const long fit = (long)std::min(room / (a.batch * a.hq * place_bytes(a)), (size_t)1 << 20);
+    const long fit = (long)std::min(room / ((size_t)a.batch * a.hq * place_bytes(a)), (size_t)1 << 20);
     const long want = std::min({std::max(CUS / base, 1l), (a.max_keys + 127l) / 128, std::max(fit, 1l)});
     p.keys = (int)((a.max_keys + want - 1) / want + 63) / 64 * 64;
     p.n = (a.max_keys + p.keys - 1) / p.keys;

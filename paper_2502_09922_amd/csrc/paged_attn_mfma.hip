@@ -17,8 +17,9 @@
 // Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 106 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for,
 // as long; the arithmetic alone 45.  70B, 64 of 128 to 2287 slots 60 us, 6.1 TB/s (66 when a CU's two workgroups were of the same sequence).  4 of
 // 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 116, 5.6 TB/s, where a tile's products take half of its time on a
-// SIMD.  Weights: scores go out and come back, 4 bytes for each query head and slot: 70B, 64 of 128 to 2287 slots 75 us instead of 57 (12 for the
-// stores, 5 of which they cost where all of them go to the same lines; behind the fills or in another layout no less).
+// SIMD.  Weights: where a workgroup has all of a sequence's slots, scores wait in LDS as far as there is room (13B, 32 sequences 120 us), otherwise they
+// go out and come back, 4 bytes for each query head and slot: 70B, 64 of 128 to 2287 slots 75 us instead of 57 (12 for the stores, 5 of which
+// they cost where all of them go to the same lines; behind the fills or in another layout no less).
 #include "attn_mfma.hpp"
 #include "paged.hpp"
 
@@ -571,7 +572,7 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
 // Four wavefronts with two tiles each, two workgroups to a CU (fp32 of 128 dims: one tile of 16 KB), or twice the wavefronts where a CU has one
 // workgroup at most.  13B, 32 sequences 106 us; three wavefronts 110, two 116, tiles of 32 keys or rings of four tiles, which leave a CU one
 // workgroup, 7 to 8 more.  7B, 8 sequences of 1024 slots with weights: eight wavefronts 27.0, four 29.1.
-// Scores of one workgroup that has all of a sequence's slots stay in LDS where they fit: 13B, 32 sequences of 1024 to 1087 slots 122 us, 132 through memory.
+// Scores of one workgroup that has all of a sequence's slots stay in LDS where they fit: 13B, 32 sequences of 1024 to 1087 slots 120 us, 132 through memory.
 template <class T, int HD, int NW, int NB>
 void launch_nw(const PagedAttn& a, PagedPieces p, int most, hipStream_t st) {
   p.held = p.stride + 4;  // columns' equal slots in different banks
