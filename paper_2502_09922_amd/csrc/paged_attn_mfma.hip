@@ -16,7 +16,7 @@
 //
 // Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 106 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for,
 // as long; the arithmetic alone 45.  70B, 64 of 128 to 2287 slots 60 us, 6.1 TB/s (66 when a CU's two workgroups were of the same sequence).  4 of
-// 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 116, 5.6 TB/s, where a tile's products take half of its time on a
+// 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 109, 6.0 TB/s, where a tile's products take half of its time on a
 // SIMD.  Weights: where a workgroup has all of a sequence's slots, scores wait in LDS as far as there is room (13B, 32 sequences 120 us), otherwise they
 // go out and come back, 4 bytes for each query head and slot: 70B, 64 of 128 to 2287 slots 75 us instead of 57 (12 for the stores, 5 of which
 // they cost where all of them go to the same lines; behind the fills or in another layout no less).
@@ -110,6 +110,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   constexpr int UNITS = TK / 8;    // parts of a tile that lie in one page whatever the page's size
   constexpr int TILE = TK * ROWB;
   constexpr int DT = HD / 16, HALVES = TK / 16;
+  constexpr bool APART = NB == 1;  // the next tile's keys are asked for as soon as this one's are read: fp32, 13B, 16 of 1000 slots 116 -> 109 us (bf16, two tiles, 106 -> 108)
   constexpr int STORES = WEIGH == IN_MEMORY ? HALVES : 0;  // of a tile's scores
   static_assert(RPI <= 8 && (NB & (NB - 1)) == 0, "");
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -192,17 +193,27 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   uint64_t gone = 0;            // whose parts have no page: UNITS bits for each of the last tiles asked for
   // Written in assembly: of the builtin the compiler knows that it writes LDS but not where, and would wait for the fills on their way
   // before it reads what has arrived.  (m0 is reserved, of which the compiler warns.)
-  auto fill = [&]() __attribute__((always_inline)) {
+  const T* vt_next[UNITS];  // values of the tile whose keys have been asked for last
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-    auto piece = [](auto once, const T* base, unsigned off, unsigned to) __attribute__((always_inline)) {
-      if constexpr (decltype(once)::value) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
-      else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
-    };
+  auto piece = [](auto once, const T* base, unsigned off, unsigned to) __attribute__((always_inline)) {
+    if constexpr (decltype(once)::value) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+  };
 #pragma clang diagnostic pop
+  // What one block of columns reads once does not stay in L2: 13B, 32 sequences 120 -> 106 us, 70B, 64 ragged 76 -> 66 (32 heads over one,
+  // 64 sequences of 2000 slots, which two blocks read: 21 and 24).
+  auto rows_of_tile = [&](const T* const* from, const unsigned* off, unsigned to) __attribute__((always_inline)) {
+    auto all = [&](auto once) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) piece(once, from[i * RPI / 8], off[i], to + i * 1024);
+    };
+    if (blocks == 1) all(std::true_type{});
+    else all(std::false_type{});
+  };
+  auto fill_keys = [&]() __attribute__((always_inline)) {
     const int key0 = (t_lo + wave + next * NW) * TK;
-    const unsigned to = lds0 + (next & (NB - 1)) * (2 * TILE);
-    const T *kt[UNITS], *vt[UNITS];
+    const T* kt[UNITS];
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int at = key0 + 8 * u;
@@ -210,25 +221,21 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       gone = gone << 1 | (at <= t.n && !there);
       const size_t row = page_row0(there ? page[u] : 0, hkv, kh, map.shift) + (at & mask);
       kt[u] = kc + row * HD;
-      vt[u] = vc + row * HD;
+      vt_next[u] = vc + row * HD;
     }
-    // What one block of columns reads once does not stay in L2: 13B, 32 sequences 120 -> 106 us, 70B, 64 ragged 76 -> 66 (32 heads over one,
-    // 64 sequences of 2000 slots, which two blocks read: 21 and 24).
-    auto all = [&](auto once) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        piece(once, kt[i * RPI / 8], koff[i], to + i * 1024);
-        piece(once, vt[i * RPI / 8], voff[i], to + TILE + i * 1024);
-      }
-    };
-    if (blocks == 1) all(std::true_type{});
-    else all(std::false_type{});
+    rows_of_tile(kt, koff, lds0 + (next & (NB - 1)) * (2 * TILE));
+  };
+  auto fill_values = [&]() __attribute__((always_inline)) {
+    rows_of_tile(vt_next, voff, lds0 + (next & (NB - 1)) * (2 * TILE) + TILE);
     ++next;
     look_up(next);
   };
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) asm volatile("" : "+v"(raw[kk]));  // waited for here, not behind the tiles
-  while (next < min(count, NB)) fill();
+  while (next < min(count, NB)) {
+    fill_keys();
+    fill_values();
+  }
 
   // ---- queries: this wavefront's 16 columns, turned
   const float* turn = cs + (size_t)t.pos * HD;
@@ -338,8 +345,11 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     const int key0 = (t_lo + wave + i * NW) * TK;
     unsigned char* ks = smem + wave * (NB * 2 * TILE) + (i & (NB - 1)) * (2 * TILE);
     unsigned char* vs = ks + TILE;
-    // Tile i has landed: behind its fills are those of the tiles asked for since, and the stores of the scores since then.
-    if (next - i == NB && i >= NB - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((NB - 1) * (2 * NL + STORES)));
+    // Tile i has landed: behind its fills are those of the tiles asked for since, and the stores of the scores since then.  In a ring of one tile
+    // its keys have, behind whose fills are its values'.
+    const bool more = next < count;
+    if constexpr (APART) wait_vm(NL + min(i, 1) * STORES);
+    else if (next - i == NB && i >= NB - 1) __builtin_amdgcn_s_waitcnt(waitcnt_vm((NB - 1) * (2 * NL + STORES)));
     else wait_vm((next - 1 - i) * 2 * NL + min(i, NB - 1) * STORES);
     asm volatile("" ::: "memory");
     const unsigned units = (unsigned)(gone >> ((next - 1 - i) * UNITS)) & ((1u << UNITS) - 1);  // the highest bit is the first part's
@@ -350,16 +360,12 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       for (int u = 0; u < UNITS; ++u)
         if (units >> (UNITS - 1 - u) & 1) seen &= ~(0xFFu << (8 * u));
       if (key0 + TK > keys) seen &= (1u << (keys - key0)) - 1;
-      // values that nobody sees may be anything: zero times that has to be zero
-#pragma unroll
-      for (int j = 0; j < NL; ++j)
-        if (!(seen >> (j * RPI + lrow) & 1)) *reinterpret_cast<u32x4*>(vs + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
     }
-    if (last && lane < 2 * CPR) {  // the new token's row
-      const int r = t.n - key0;
-      *reinterpret_cast<u32x4*>((nv ? vs : ks) + r * ROWB + ((nc ^ (nv ? value_swizzle<T, HD>(r) : key_swizzle<T, HD>(r))) << 4)) = fresh;
+    const int new_row = t.n - key0;
+    if (last) {
+      if (lane < CPR) *reinterpret_cast<u32x4*>(ks + new_row * ROWB + ((nc ^ key_swizzle<T, HD>(new_row)) << 4)) = fresh;
+      asm volatile("" ::: "memory");
     }
-    if (masked || last) asm volatile("" ::: "memory");
 
     // ---- scores: all of a tile's keys are asked for at once, and all of its values before the softmax
     f32x4 s[HALVES];
@@ -385,6 +391,22 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
 #pragma unroll
           for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][kk][e], qh[kk][e], s[h], 0, 0, 0);
       }
+    }
+    if constexpr (APART) {
+      if (more) {  // over this tile's keys, of which every read has its value by now
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        fill_keys();
+      }
+      wait_vm(more ? NL : 0);  // its values
+      asm volatile("" ::: "memory");
+    }
+    if (masked || last) {
+      // values that nobody sees may be anything: zero times that has to be zero
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+        if (!(seen >> (j * RPI + lrow) & 1)) *reinterpret_cast<u32x4*>(vs + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+      if (last && nv && lane < 2 * CPR) *reinterpret_cast<u32x4*>(vs + new_row * ROWB + ((nc ^ value_swizzle<T, HD>(new_row)) << 4)) = fresh;
+      asm volatile("" ::: "memory");
     }
     // bf16: the k index of the second product runs over keys {4g..4g+3} of each half, g = lane / 16, fp32: row 4g + e, dims 16-byte chunk by chunk
     s16x4 vt[HALVES][sizeof(T) == 2 ? DT : 1];
@@ -467,9 +489,10 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
 #pragma unroll
             for (int d = 0; d < 4; ++d) o[j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[h][j * 4 + e][d], s[h][e], o[j * 4 + d], 0, 0, 0);
     }
-    if (next < count) {  // over this tile, of which every read has its value by now
+    if (more) {  // over this tile, of which every read has its value by now
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      fill();
+      if constexpr (!APART) fill_keys();
+      fill_values();
     }
   }
 
