@@ -166,13 +166,22 @@ k_paged_attn(PageMap map, const T* __restrict__ qkv, const float2* __restrict__ 
   }
 }
 
-// Maximum and sum of a (sequence, query head) over its pieces, in their order.
+// Maximum and sum of a (sequence, query head) over its pieces, in their order, U of them on their way at once.
+template <int U>
 __device__ __forceinline__ float2 joined(const float2* __restrict__ ml, size_t step, int n, float scale) {
   float m = -INFINITY, den = 0.f;
-  for (int z = 0; z < n; ++z) m = fmaxf(m, ml[z * step].x);
-  for (int z = 0; z < n; ++z) {
-    const float2 v = ml[z * step];
-    den += v.y * (v.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((v.x - m) * scale));  // a sum without a maximum is 0, or no number
+  for (int z0 = 0; z0 < n; z0 += U) {
+    float2 v[U];
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = ml[min(z0 + u, n - 1) * step];
+#pragma unroll
+    for (int u = 0; u < U; ++u) top = fmaxf(top, v[u].x);
+    den *= m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale);  // a sum without a maximum is 0, or no number
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (z0 + u < n) den += v[u].y * (v[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((v[u].x - top) * scale));
+    m = top;
   }
   return float2{m, den};
 }
@@ -237,33 +246,34 @@ k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int 
     *reinterpret_cast<TD*>(out + row * hd + d) = w;
     return;
   }
+  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, first = item % blocks * 256, slot = first + threadIdx.x;
+  if (map.lens[b] < first) return;
+  // pages and scores are asked for before it is known whether the sequence takes part
+  const int page = map.table[(size_t)b * map.columns + min(slot >> map.shift, map.columns - 1)];
+  float s[U];
+  auto load = [&](int g0, int g) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) s[u] = p.scores[((size_t)b * hq + kh * G + min(g0 + g + u, G - 1)) * p.stride + min(slot, p.stride - 1)];
+  };
+  load(0, 0);
   if (!paged_seq(map, b, max_pos, turns, most, t)) return;
   const int keys = t.n + 1, n = p.share ? dealt.y : min((t.n + p.keys) / p.keys, p.n);
-  const int blocks = (most + 255) / 256, item = blockIdx.x - out_blocks, kh = item / blocks, first = item % blocks * 256, slot = first + threadIdx.x;
-  if (first >= keys) return;
-  const int page = slot < keys ? map.table[(size_t)b * map.columns + (slot >> map.shift)] : -1;
-  const bool there = (unsigned)page < (unsigned)map.pages;
+  const bool there = slot < keys && (unsigned)page < (unsigned)map.pages;
   const size_t at = page_row0(there ? page : 0, hkv, kh, map.shift) + (slot & ((1 << map.shift) - 1));
   const float had = there && slot != t.n ? weights[at] : 0.f;
   __shared__ float2 heads[64];  // maximum, 1 / sum
   float got = 0.f;
   for (int g0 = 0; g0 < G; g0 += 64) {
-    const size_t row = (size_t)b * hq + kh * G + g0;
     const int count = min(64, G - g0);
-    float s[U];
-    auto load = [&](int g) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) s[u] = p.scores[(row + min(g + u, count - 1)) * p.stride + min(slot, keys - 1)];
-    };
-    load(0);
+    if (g0) load(g0, 0);
     if (g0) __syncthreads();
     if ((int)threadIdx.x < count) {
-      const float2 all = joined(p.ml + place_of(kh * G + g0 + threadIdx.x), step, n, scale);
+      const float2 all = joined<U>(p.ml + place_of(kh * G + g0 + threadIdx.x), step, n, scale);
       heads[threadIdx.x] = float2{all.x == -INFINITY ? 0.f : all.x, 1.f / all.y};
     }
     __syncthreads();
     for (int g = 0; g < count; g += U) {
-      if (g) load(g);
+      if (g) load(g0, g);
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (g + u < count) got += __builtin_amdgcn_exp2f((s[u] - heads[g + u].x) * scale) * heads[g + u].y;
