@@ -467,7 +467,7 @@ ls_status ls_paged_fill(const ls_heads* heads, int layers, const ls_kv* from, in
  * place.  lens[b] becomes keep; what lies behind is left as it is, so pages behind slot keep - 1 are the caller's again.
  *   pages    with weights, places and positions; all layers
  *   keep     at least 1;  first, recent: at least 0, first + recent at most keep
- *   max_len  host-side upper bound of lens[b]; a sequence with more is left alone
+ *   max_len  host-side upper bound of lens[b]; a sequence with more is left alone.  Beyond 65536 scratch grows with it.
  *   scratch  of ls_paged_evict_scratch_bytes (0: invalid sizes), 16-byte aligned; nothing in it outlasts the call
  * A sequence with a page below lens[b] that the table does not name is left alone.  Pages of a sequence that is cut down are its own.
  */

@@ -424,7 +424,8 @@ def paged_evict(cache: PagedCache, keep: int, recent: int, max_len: int, first: 
     """Cut sequences down to `keep` slots (ls_paged_evict): the first `first` positions and the newest `recent` stay, and of the others those
     of the largest weights; the cache has positions; max_len: a bound of lens."""
     device = cache.device
-    heads, layers = cache.heads(cache._t["k"].shape[2], 1 << 24), cache._t["k"].shape[0]
+    k, table = cache._t["k"], cache._t["table"]
+    heads, layers, max_len = cache.heads(k.shape[2], 1 << 24), k.shape[0], min(max_len, table.shape[1] * k.shape[3])  # scratch goes by it
     nb = lib.ls_paged_evict_scratch_bytes(heads, layers, cache.batch, keep, max_len)
     scratch = _scratch(nb, device)
     _run(device, lib.ls_paged_evict, heads, layers, cache._all, cache.batch, keep, first, recent, max_len, scratch.data_ptr() if nb else None, nb)

@@ -86,6 +86,8 @@ struct EvictArgs {
   int32_t* places;
   int32_t* count;  // [units] moves that are to be made, -1 for a sequence that is left alone
   int2* moves;     // [units][most]: to slot x from slot y
+  u32x4* keys;     // [units][wavefronts][groups / 4][64], where registers do not hold them
+  int groups;      // of 64 slots to a wavefront, room for them
   void *kc, *vc;
   int pieces;      // of a row, 16 bytes each (wide) or 4
   bool wide;
@@ -152,21 +154,22 @@ __device__ __forceinline__ void make_moves(const EvictArgs& a, const int32_t* en
   }
 }
 
+constexpr int HELD = 1024 * 64;  // slots at most whose keys registers hold
 // Rows of all kv heads of a layer, whose bytes of weights and places 32-bit offsets reach.
 constexpr int64_t NARROW = 1 << 29;
 
 // The moves of a (layer, sequence, kv head): W wavefronts, of which the w-th has the w-th part of the slots, 64 neighbours at a time.  The largest key that
 // `keep` slots or more reach is searched for between the smallest and the largest of the slots that may go, by where it lay if keys were spread
-// evenly, until exactly `keep` slots reach it or nothing is left between; in the latter case the lower ones of equal keys stay.  V > 0: the
-// keys of up to 64 W V slots are held in V registers of a lane, and weights and places are read once; V = 0: keys are made again for each count.
+// evenly, until exactly `keep` slots reach it or nothing is left between; in the latter case the lower ones of equal keys stay.  Weights and places
+// are read once.  V > 0: the keys of up to 64 W V slots are held in V registers of a lane; V = 0: each lane leaves them in memory for itself, four of
+// its slots side by side (8 units of 131072 slots 248 us, 930 when keys were made again for each count).
 // Where a unit has no more than FEW moves (`here`), they are made here: another launch for one move each took 6 us for 5120 units.
 // Bound by its steps one after the other: 70B, 128 units of up to 16384 slots down to 2048 26 us (16 wavefronts; 4 loads, 8 rounds, 4 list), 5120
 // units of 501 slots, one move each, 15.
-constexpr int FEW = 32, GUESSES = 12;
-template <int W, int V>
+constexpr int FEW = 32, GUESSES = 12, GROUPS = 32;
+template <int W, int V, class Row = unsigned>
 __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here) {
-  constexpr int GR = V == 0 ? 16 : 8;  // keys at a time; of no slot: 0, below every threshold
-  typedef std::conditional_t<V == 0, size_t, unsigned> Row;
+  constexpr int GR = 8, READ = GROUPS;  // keys at a time that are made, and that are read again; of no slot: 0, below every threshold
   const int unit = blockIdx.x, kh = unit % a.hkv, b = unit / a.hkv % a.batch, layer = unit / a.hkv / a.batch;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   __shared__ int bad, sums[2][W][3];
@@ -216,7 +219,8 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
 #pragma unroll
     for (int j = 0; j < GR; ++j) k[j] = g + j < per && slot0 + (g + j) * 64 < n ? stay_key(w[j], place[j], a.first, from) : 0;
   };
-  unsigned key[V > 0 ? V : GR];
+  unsigned key[V > 0 ? V : READ];
+  u32x4* mine = V > 0 ? nullptr : a.keys + ((size_t)unit * W + wave) * (a.groups / 4) * 64 + lane;
   if constexpr (V > 0) {
 #pragma unroll
     for (int g = 0; g < V; g += GR) {
@@ -226,6 +230,13 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
 #pragma unroll
         for (int j = 0; j < GR; ++j) key[g + j] = 0;
       }
+    }
+  } else {
+    for (int g = 0; g < per; g += READ) {
+#pragma unroll
+      for (int j = 0; j < READ; j += GR) load(g + j, key + j);
+#pragma unroll
+      for (int j = 0; j < READ; j += 4) mine[(g + j) / 4 * 64] = u32x4{key[j], key[j + 1], key[j + 2], key[j + 3]};
     }
   }
   // f(which of 64 slots, slot, key of it) over all slots of this wavefront and some behind, whose keys are 0
@@ -238,10 +249,12 @@ __global__ void __launch_bounds__(64 * W) k_evict_choose(EvictArgs a, bool here)
           for (int i = g; i < g + GR; ++i) f(i, slot0 + i * 64, key[i]);
         }
     } else {
-      for (int g = 0; g < per; g += GR) {
-        load(g, key);
+      for (int g = 0; g < per; g += READ) {
+        u32x4 four[READ / 4];
 #pragma unroll
-        for (int j = 0; j < GR; ++j) f(g + j, slot0 + (g + j) * 64, key[j]);
+        for (int j = 0; j < READ / 4; ++j) four[j] = mine[(g / 4 + j) * 64];
+#pragma unroll
+        for (int j = 0; j < READ; ++j) f(g + j, slot0 + (g + j) * 64, four[j / 4][j % 4]);
       }
     }
   };
@@ -378,11 +391,16 @@ __global__ void __launch_bounds__(256) k_evict_lens(EvictArgs a, int32_t* __rest
   if (b < a.batch && a.count[b * a.hkv] >= 0) lens[b] = a.keep;
 }
 
+// Groups of 64 slots whose keys each of 16 wavefronts leaves in memory.
+int key_groups(int max_len) { return max_len > HELD ? ((max_len + 1023) / 1024 + GROUPS - 1) / GROUPS * GROUPS : 0; }
+
 void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t st) {
   // More wavefronts to a unit where units do not fill the chip: 1024 units of 1025 slots 14 -> 10 us.
   const bool few = units <= 2048, here = a.most <= FEW;
-  const int n = ((int64_t)a.map.pages * a.hkv << a.map.shift) < NARROW ? a.max_len : INT32_MAX;
-  if (n <= 64 * 8) k_evict_choose<1, 8><<<units, 64, 0, st>>>(a, here);
+  const int n = a.max_len;
+  if (n > HELD) k_evict_choose<16, 0, size_t><<<units, 1024, 0, st>>>(a, here);
+  else if (((int64_t)a.map.pages * a.hkv << a.map.shift) >= NARROW) k_evict_choose<16, 64, size_t><<<units, 1024, 0, st>>>(a, here);
+  else if (n <= 64 * 8) k_evict_choose<1, 8><<<units, 64, 0, st>>>(a, here);
   else if (n <= 64 * 16 && !few) k_evict_choose<1, 16><<<units, 64, 0, st>>>(a, here);
   else if (n <= 64 * 32 && !few) k_evict_choose<1, 32><<<units, 64, 0, st>>>(a, here);
   else if (n <= 256 * 8) k_evict_choose<4, 8><<<units, 256, 0, st>>>(a, here);
@@ -391,8 +409,7 @@ void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t s
   else if (n <= 1024 * 8) k_evict_choose<16, 8><<<units, 1024, 0, st>>>(a, here);
   else if (n <= 1024 * 16) k_evict_choose<16, 16><<<units, 1024, 0, st>>>(a, here);
   else if (n <= 1024 * 32) k_evict_choose<16, 32><<<units, 1024, 0, st>>>(a, here);
-  else if (n <= 1024 * 64) k_evict_choose<16, 64><<<units, 1024, 0, st>>>(a, here);
-  else k_evict_choose<16, 0><<<units, 1024, 0, st>>>(a, here);
+  else k_evict_choose<16, 64><<<units, 1024, 0, st>>>(a, here);
   if (here) {
     k_evict_lens<<<(a.batch + 255) / 256, 256, 0, st>>>(a, lens);
     return;
@@ -560,7 +577,7 @@ ls_status ls_paged_fill(const ls_heads* h, int layers, const ls_kv* from, int fr
 size_t ls_paged_evict_scratch_bytes(const ls_heads* h, int layers, int batch, int keep, int max_len) {
   if (evict_error(h, layers, batch, keep, max_len)) return 0;
   const size_t units = evict_units(h, layers, batch), most = std::max(0, std::min(keep, max_len - keep));
-  return (units * 4 + 15) / 16 * 16 + std::max(units * most * sizeof(int2), (size_t)16);
+  return (units * 4 + 15) / 16 * 16 + std::max((units * most * sizeof(int2) + 15) / 16 * 16, (size_t)16) + units * ls::key_groups(max_len) * 64 * 16 * 4;
 }
 
 ls_status ls_paged_evict(const ls_heads* h, int layers, const ls_pages* pages, int batch, int keep, int first, int recent, int max_len, void* scratch,
@@ -589,6 +606,8 @@ ls_status ls_paged_evict(const ls_heads* h, int layers, const ls_pages* pages, i
   a.weights = pages->weights; a.places = pages->places;
   a.count = (int32_t*)scratch;
   a.moves = (int2*)((char*)scratch + (units * 4 + 15) / 16 * 16);
+  a.keys = (ls::u32x4*)((char*)a.moves + (units * a.most * sizeof(int2) + 15) / 16 * 16);
+  a.groups = ls::key_groups(max_len);
   a.kc = pages->k; a.vc = pages->v; a.pieces = pieces; a.wide = wide;
   ls::launch_evict(a, units, pages->lens, (hipStream_t)hip_stream);
   return launched(who);

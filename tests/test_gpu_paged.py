@@ -635,6 +635,28 @@ def test_all_lengths_of_sequences_that_are_cut_down(batch, n, keep, recent):
     assert int(want.lens[batch // 2]) == keep
 
 
+@pytest.mark.parametrize("keep,recent,values", [(400, 30, 7), (70000, 0, 1 << 20), (65536, 65536, 3), (20, 20, 1 << 20)])
+def test_sequences_beyond_registers_beside_short_ones(keep, recent, values):
+    """Long and short ones of a call, equal weights or few, lengths of the bound and below, a sequence that is left alone."""
+    page, hkv, lens = 1024, 2, [70000, 500, 131073, 65537, 1, -1]
+    c = plain.Pages((2, hkv, 2), torch.float32, [1], page, seed=63, weighed=True)
+    need = [max(0, n + page - 1) // page for n in lens]
+    g, order = torch.Generator().manual_seed(keep), list(range(sum(need)))
+    random.Random(keep).shuffle(order)
+    c.table = torch.full((len(lens), max(need)), -1, dtype=torch.int32)
+    for b, n in enumerate(need):
+        for i in range(n):
+            c.table[b, i] = order.pop()
+    c.lens = torch.tensor(lens, dtype=torch.int32)
+    c.positions = c.lens.clone()
+    size = (1, sum(need), hkv, page)
+    c.k, c.v = (torch.randn(size + (2,), generator=g) for _ in range(2))
+    c.weights = torch.randint(0, values, size, generator=g).float()
+    c.places = torch.randint(0, 140000, size, generator=g).int()
+    want = cut(c, keep, 0, recent, 131073)
+    assert want.lens.tolist() == [min(n, keep) for n in lens]
+
+
 def test_evictions_beyond_32_bits():
     """More rows of a layer than 32-bit offsets of their weights reach: a sequence in the last pages, in the second layer."""
     from paper_2502_09922_amd import paged_evict
