@@ -366,16 +366,18 @@ class PagedCache:
         return h
 
     def attention_call(self, columns: int, max_seq: int, max_ctx: int):
-        """(n_q_heads, ls_heads, scratch bytes) of an attention call over rows of so many columns: of one size step after step."""
-        if self._call is None or self._call[0] != (columns, max_seq, max_ctx):
+        """(n_q_heads, ls_heads, scratch bytes) of an attention call over rows of so many columns: of one size step after step.  The last
+        call's plan is kept; threads may call at once, so it is read and stored as a whole, once each."""
+        key, call = (columns, max_seq, max_ctx), self._call
+        if call is None or call[0] != key:
             k = self._t["k"]
             hkv, hd = k.shape[2], k.shape[4]
             if columns % hd or columns // hd <= 2 * hkv:
                 raise ValueError("qkv: [%d, (n_q_heads + %d) * %d] is wanted" % (self.batch, 2 * hkv, hd))
             hq = columns // hd - 2 * hkv
             heads = self.heads(hq, max_seq)
-            self._call = ((columns, max_seq, max_ctx), (hq, heads, lib.ls_paged_attention_scratch_bytes(heads, self._all, self.batch, max_ctx)))
-        return self._call[1]
+            call = self._call = (key, (hq, heads, lib.ls_paged_attention_scratch_bytes(heads, self._all, self.batch, max_ctx)))
+        return call[1]
 
 
 def _scratch(nb, device):
