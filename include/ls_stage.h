@@ -477,8 +477,8 @@ ls_status ls_paged_evict(const ls_heads* heads, int layers, const ls_pages* page
 
 /*
  * The stage's generation step over a cache in pages: ls_stage_decode whose attention is ls_paged_attention in every layer, the pools those
- * of all of the stage's layers.  lens[b] and positions[b] of sequences with room grow by one behind the last layer.  max_seq of the stage is the
- * positions that tokens may have.  Rows of sequences without room are computed from zeros as attention; nobody else's depend on them.
+ * of all of the stage's layers.  lens[b] and positions[b] of sequences with room grow by one behind the last layer.  lens, positions and table have
+ * `batch` rows or more; max_seq of the stage is the positions that tokens may have.  Rows of sequences without room are computed from zeros as attention; nobody else's depend on them.
  * max_ctx and scratch as in ls_paged_attention (the query with the stage's heads), the rest as in ls_stage_decode.  The probe does not see it.
  */
 ls_status ls_stage_paged(ls_stage* stage, const void* in, int batch, int max_ctx, const ls_pages* pages, void* out, float* logits_out,

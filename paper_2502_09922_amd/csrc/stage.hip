@@ -1161,7 +1161,8 @@ ls_status ls_stage_paged(ls_stage* s, const void* in, int batch, int max_ctx, co
   if (!in || !out) return fail(LS_ERR_INVALID_ARG, "%s: NULL argument", who);
   if (logits_out && !s->last) return fail(LS_ERR_INVALID_ARG, "%s: logits_out given but the stage has no LM head", who);
   const ls_cfg& c = s->cfg;
-  const ls_heads heads{c.dtype, c.n_q_heads, c.n_kv_heads, c.head_dim, c.max_batch, c.max_seq};
+  // lens, positions and table have as many rows as the call has sequences, whatever the stage has room for
+  const ls_heads heads{c.dtype, c.n_q_heads, c.n_kv_heads, c.head_dim, (uint32_t)batch, c.max_seq};
   ls::PagedAttn a;
   rc = ls::paged_attention_args(who, &heads, pages, batch, max_ctx, true, scratch, scratch_bytes, &a);
   if (rc != LS_OK) return rc;
