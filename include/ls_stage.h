@@ -439,7 +439,8 @@ size_t ls_paged_attention_scratch_bytes(const ls_heads* heads, const ls_pages* l
  * Slots whose page the table does not name are not there: nobody attends to them.  A sequence without room (lens[b] negative, or beyond the
  * table, slot lens[b] without a page, or a position that is negative or that rope does not have) keeps its cache, and its output row is zeros.  Pages may be shared
  * by sequences (a common prompt) as long as no slot lens[b] lies in them and there are no weights: rows of one slot that several sequences
- * write, or weights that they add to, are not ordered.  Scores, softmax, sums and weights are fp32; products as in ls_tree_attention.
+ * write, or weights that they add to, are not ordered.  Scores, softmax, sums and weights are fp32; products as in ls_tree_attention, but for the scores
+ * of a call with weights, whose queries enter with all of their bits.
  */
 ls_status ls_paged_attention(const ls_heads* heads, const ls_pages* layer, int batch, int max_ctx, const void* qkv, const float* rope,
                              void* out, void* scratch, size_t scratch_bytes, void* hip_stream);

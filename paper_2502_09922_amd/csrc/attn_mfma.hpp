@@ -23,4 +23,17 @@ __device__ __forceinline__ void two_parts(float v, bf16& first, bf16& second) {
   second = (bf16)fmaf(v, 0x1.000002p0f, -__builtin_bit_cast(float, bits & 0xFFFF0000u));
 }
 
+// v as a sum of three bf16, exactly: v cut off, the rest cut off, what is left of its 24 bits.  None of them is zero unless v is, and all have
+// its sign: where nothing is left a part is halved.
+__device__ __forceinline__ void three_parts(float v, bf16* part) {
+  auto cut = [](float w) { return __builtin_bit_cast(float, __builtin_bit_cast(unsigned, w) & 0xFFFF0000u); };
+  float a = cut(v), rest = v - a;
+  if (rest == 0.f) rest = a *= 0.5f;
+  float b = cut(rest), c = rest - b;
+  if (c == 0.f) c = b *= 0.5f;
+  part[0] = (bf16)a;
+  part[1] = (bf16)b;
+  part[2] = (bf16)c;
+}
+
 }  // namespace ls

@@ -4,7 +4,10 @@
 //   S^T[key][column] = K Q^T        A = 16 key rows, B = 16 columns
 //   O^T[dim][column] += V^T P^T     A = V^T, B = P^T
 // with the operand layouts, the split of bf16 queries and weights into two parts and the softmax of the attention of draft trees
-// (tree_attn_mfma.hip): a lane of a result holds column lane % 16 and rows 4 (lane / 16) + e.
+// (tree_attn_mfma.hip): a lane of a result holds column lane % 16 and rows 4 (lane / 16) + e.  An output is rounded to bf16, of which two parts hold
+// more than enough; the weights that slots get are fp32 and go by the scores, and with them queries keep
+// all of their bits, in three parts (of two, 2^-16 of a score would be lost; 13B, 32 sequences of 500 slots, four layers 256.4 -> 257.8 us, 7B, 8 of 1024
+// 124.7 -> 127.4).
 //
 // A workgroup is a (sequence, kv head, block of 16 columns, piece of the slots); its wavefronts take the piece's tiles in turn, each through a ring of
 // LDS of its own that is filled straight from memory, so there are no barriers and what is on its way needs no registers: bound by memory, what
@@ -262,8 +265,10 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     return;
   }
 
+  // bf16: queries in two parts, in three where slots' weights go by the scores too
+  constexpr int PARTS = sizeof(T) == 4 ? 1 : WEIGH ? 3 : 2;
   typedef std::conditional_t<sizeof(T) == 2, bf16x8, f32x4> Q;
-  Q qh[KS], ql[sizeof(T) == 2 ? KS : 1];
+  Q qp[PARTS][KS];
 #pragma unroll
   for (int kk = 0; kk < KS; ++kk) {
     const Q u = __builtin_bit_cast(Q, raw[kk]);
@@ -281,12 +286,13 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
 #pragma unroll
     for (int e = 0; e < EPC; ++e) {
       if constexpr (sizeof(T) == 2) {
-        bf16 first, second;
-        two_parts(w[e], first, second);
-        qh[kk][e] = first;
-        ql[kk][e] = second;
+        bf16 part[PARTS];
+        if constexpr (WEIGH) three_parts(w[e], part);
+        else two_parts(w[e], part[0], part[1]);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) qp[p][kk][e] = part[p];
       } else {
-        qh[kk][e] = w[e];
+        qp[0][kk][e] = w[e];
       }
     }
   }
@@ -385,14 +391,14 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     for (int kk = 0; kk < KS; ++kk) {
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+        for (int part = PARTS - 1; part >= 0; --part)
 #pragma unroll
-          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], part ? qh[kk] : ql[kk], s[h], 0, 0, 0);
+          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], qp[part][kk], s[h], 0, 0, 0);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][kk][e], qh[kk][e], s[h], 0, 0, 0);
+          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][kk][e], qp[0][kk][e], s[h], 0, 0, 0);
       }
     }
     if constexpr (APART) {
