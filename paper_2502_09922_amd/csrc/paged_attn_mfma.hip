@@ -38,6 +38,7 @@ constexpr int ORDERED = 256;       // sequences at most that are taken by length
 constexpr int ORDERED_KEYS = 512;  // and only where some may be longer
 constexpr float FOLLOW = 8.f;
 constexpr int CUS = 256;
+constexpr int TILE_KEYS = 16;  // as many rows as a matrix product has
 
 __device__ __forceinline__ int wave_total(int v) {
   return __builtin_amdgcn_readfirstlane(
@@ -99,22 +100,22 @@ __device__ __forceinline__ bool deal(const PageMap& map, int batch, int units, i
   return true;
 }
 
-// TK: keys of a tile; NW: wavefronts; NB: tiles of a ring, a power of two.  Weights: scores wait for the end in memory, or in LDS, behind the rings.
+// NW: wavefronts; NB: tiles of a ring, a power of two.  Weights: scores wait for the end in memory, or in LDS, behind the rings.
 enum Weigh { NO_WEIGHTS = 0, IN_MEMORY = 1, IN_LDS = 2 };
-template <class T, int HD, int TK, int NW, int NB, Weigh WEIGH>
+template <class T, int HD, int NW, int NB, Weigh WEIGH>
 __global__ void __launch_bounds__(64 * NW, 2)
 k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ cs, T* __restrict__ kc, T* __restrict__ vc, int32_t* __restrict__ places,
              T* __restrict__ out, int hq, int hkv, int max_pos, int most, int half, int batch, PagedPieces p, float* __restrict__ weights) {
-  constexpr int THREADS = 64 * NW;
+  constexpr int THREADS = 64 * NW, TK = TILE_KEYS;
   constexpr int ROWB = HD * sizeof(T), EPC = 16 / sizeof(T);
   constexpr int CPR = HD / EPC;    // 16-byte chunks of a row
   constexpr int RPI = 64 / CPR;    // rows that a wavefront's load covers
   constexpr int NL = TK / RPI;     // loads of a tile's keys, as many of its values
   constexpr int UNITS = TK / 8;    // parts of a tile that lie in one page whatever the page's size
   constexpr int TILE = TK * ROWB;
-  constexpr int DT = HD / 16, HALVES = TK / 16;
+  constexpr int DT = HD / 16;
   constexpr bool APART = NB == 1;  // the next tile's keys are asked for as soon as this one's are read: fp32, 13B, 16 of 1000 slots 116 -> 109 us (bf16, two tiles, 106 -> 108)
-  constexpr int STORES = WEIGH == IN_MEMORY ? HALVES : 0;  // of a tile's scores
+  constexpr int STORES = WEIGH == IN_MEMORY ? 1 : 0;  // of a tile's scores
   static_assert(RPI <= 8 && (NB & (NB - 1)) == 0, "");
   typedef T T4 __attribute__((ext_vector_type(4)));
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -363,7 +364,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     asm volatile("" ::: "memory");
     const unsigned units = (unsigned)(gone >> ((next - 1 - i) * UNITS)) & ((1u << UNITS) - 1);  // the highest bit is the first part's
     const bool masked = units || key0 + TK > keys, last = mine && i == count - 1;
-    unsigned seen = 0xFFFFFFFFu;
+    unsigned seen = (1u << TK) - 1;
     if (masked) {
 #pragma unroll
       for (int u = 0; u < UNITS; ++u)
@@ -377,28 +378,19 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     }
 
     // ---- scores: all of a tile's keys are asked for at once, and all of its values before the softmax
-    f32x4 s[HALVES];
-    Q kf[HALVES][KS];
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+    Q kf[KS];
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
-      const int kl = h * 16 + lr;
-#pragma unroll
-      for (int kk = 0; kk < KS; ++kk) kf[h][kk] = *reinterpret_cast<const Q*>(ks + kl * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(kl)) << 4));
-      s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int kk = 0; kk < KS; ++kk) kf[kk] = *reinterpret_cast<const Q*>(ks + lr * ROWB + (((kk * 4 + lg) ^ key_swizzle<T, HD>(lr)) << 4));
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int part = PARTS - 1; part >= 0; --part)
-#pragma unroll
-          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h][kk], qp[part][kk], s[h], 0, 0, 0);
+        for (int part = PARTS - 1; part >= 0; --part) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk], qp[part][kk], s, 0, 0, 0);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int h = 0; h < HALVES; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[h][kk][e], qp[0][kk][e], s[h], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[kk][e], qp[0][kk][e], s, 0, 0, 0);
       }
     }
     if constexpr (APART) {
@@ -417,39 +409,34 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
       if (last && nv && lane < 2 * CPR) *reinterpret_cast<u32x4*>(vs + new_row * ROWB + ((nc ^ value_swizzle<T, HD>(new_row)) << 4)) = fresh;
       asm volatile("" ::: "memory");
     }
-    // bf16: the k index of the second product runs over keys {4g..4g+3} of each half, g = lane / 16, fp32: row 4g + e, dims 16-byte chunk by chunk
-    s16x4 vt[HALVES][sizeof(T) == 2 ? DT : 1];
-    Q vf[HALVES][sizeof(T) == 2 ? 1 : DT];
+    // bf16: the k index of the second product runs over keys {4g..4g+3}, g = lane / 16, fp32: row 4g + e, dims 16-byte chunk by chunk
+    s16x4 vt[sizeof(T) == 2 ? DT : 1];
+    Q vf[sizeof(T) == 2 ? 1 : DT];
+    if constexpr (sizeof(T) == 2) {
+      const int k0 = 4 * lg + (lr >> 2), within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h) {
-      if constexpr (sizeof(T) == 2) {
-        const int k0 = h * 16 + 4 * lg + (lr >> 2), within = (lr & 1) * 8;  // of the 16-byte chunk that holds dims 4 (lr % 4) of 16
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const int ch = d * 2 + ((lr & 3) >> 1);
-          vt[h][d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<T, HD>(k0)) << 4) + within));
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < HD / 64; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vf[h][j * 4 + e] = *reinterpret_cast<const Q*>(vs + (h * 16 + 4 * lg + e) * ROWB + (j * 16 + lr) * 16);
+      for (int d = 0; d < DT; ++d) {
+        const int ch = d * 2 + ((lr & 3) >> 1);
+        vt[d] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vs + k0 * ROWB + ((ch ^ value_swizzle<T, HD>(k0)) << 4) + within));
       }
+    } else {
+#pragma unroll
+      for (int j = 0; j < HD / 64; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vf[j * 4 + e] = *reinterpret_cast<const Q*>(vs + (4 * lg + e) * ROWB + (j * 16 + lr) * 16);
     }
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (WEIGH != NO_WEIGHTS) {
-      if (lr < cols)
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) *reinterpret_cast<f32x4*>((WEIGH == IN_LDS ? sm_s + lr * p.held : scores) + key0 + h * 16 + 4 * lg) = s[h];
+      if (lr < cols) *reinterpret_cast<f32x4*>((WEIGH == IN_LDS ? sm_s + lr * p.held : scores) + key0 + 4 * lg) = s;
     }
     if (masked) {
 #pragma unroll
-      for (int j = 0; j < 4 * HALVES; ++j) s[j >> 2][j & 3] = seen >> ((j >> 2) * 16 + 4 * lg + (j & 3)) & 1u ? s[j >> 2][j & 3] : -INFINITY;
+      for (int j = 0; j < 4; ++j) s[j] = seen >> (4 * lg + j) & 1u ? s[j] : -INFINITY;
     }
     // ---- softmax.  A NaN score makes its weight NaN, and the sums with it, whatever the maximum is.
-    float mx = s[0][0];
+    float mx = s[0];
 #pragma unroll
-    for (int j = 1; j < 4 * HALVES; ++j) mx = __builtin_elementwise_maximum(mx, s[j >> 2][j & 3]);
+    for (int j = 1; j < 4; ++j) mx = __builtin_elementwise_maximum(mx, s[j]);
     // The reference of the exponentials follows a maximum that has moved by more than 2^FOLLOW only: weights above one are as exact as below.
     auto far = [&] { return (mx - m_run) * scale > FOLLOW; };  // false for (-inf, -inf)
     if (__builtin_amdgcn_ballot_w64(far()) != 0) {             // lanes of a column exchange their maxima only then
@@ -468,39 +455,29 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     }
     const float mc = m_run == -INFINITY ? 0.f : m_run * scale;
 #pragma unroll
-    for (int j = 0; j < 4 * HALVES; ++j) s[j >> 2][j & 3] = __builtin_amdgcn_exp2f(fmaf(s[j >> 2][j & 3], scale, -mc));
-#pragma unroll
-    for (int h = 0; h < HALVES; ++h) l_run += (s[h][0] + s[h][1]) + (s[h][2] + s[h][3]);
+    for (int j = 0; j < 4; ++j) s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], scale, -mc));
+    l_run += (s[0] + s[1]) + (s[2] + s[3]);
     // ---- output
     if constexpr (sizeof(T) == 2) {
-      bf16x4 pf[2][HALVES];
+      bf16x4 pf[2];
 #pragma unroll
-      for (int j = 0; j < 4 * HALVES; ++j) {
+      for (int j = 0; j < 4; ++j) {
         bf16 first, second;
-        two_parts(s[j >> 2][j & 3], first, second);
-        pf[0][j >> 2][j & 3] = first;
-        pf[1][j >> 2][j & 3] = second;
+        two_parts(s[j], first, second);
+        pf[0][j] = first;
+        pf[1][j] = second;
       }
 #pragma unroll
       for (int part = 1; part >= 0; --part)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          if constexpr (HALVES == 1) {
-            o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt[0][d], __builtin_bit_cast(s16x4, pf[part][0]), o[d], 0, 0, 0);
-          } else {
-            const bf16x8 both = __builtin_bit_cast(bf16x8, __builtin_shufflevector(vt[0][d], vt[HALVES - 1][d], 0, 1, 2, 3, 4, 5, 6, 7));
-            o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(both, __builtin_shufflevector(pf[part][0], pf[part][HALVES - 1], 0, 1, 2, 3, 4, 5, 6, 7), o[d], 0, 0, 0);
-          }
-        }
+        for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt[d], __builtin_bit_cast(s16x4, pf[part]), o[d], 0, 0, 0);
     } else {
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h)
+      for (int j = 0; j < HD / 64; ++j)
 #pragma unroll
-        for (int j = 0; j < HD / 64; ++j)
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int d = 0; d < 4; ++d) o[j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[h][j * 4 + e][d], s[h][e], o[j * 4 + d], 0, 0, 0);
+          for (int d = 0; d < 4; ++d) o[j * 4 + d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[j * 4 + e][d], s[e], o[j * 4 + d], 0, 0, 0);
     }
     if (i % NEAR == NEAR - 1) {
       far_l += l_run;
@@ -603,10 +580,10 @@ template <int NW> constexpr int HELD = NW == 4 ? 13 << 10 : 28 << 10;
 
 template <class T, int HD, int NW, int NB, Weigh WEIGH>
 void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStream_t st) {
-  constexpr int TK = 16, TILES = NW * NB * 2 * TK * HD * (int)sizeof(T), JOIN = NW * 16 * (HD + SM_PAD) * 4;
+  constexpr int TILES = NW * NB * 2 * TILE_KEYS * HD * (int)sizeof(T), JOIN = NW * 16 * (HD + SM_PAD) * 4;
   static_assert(TILES >= JOIN && TILES <= NW * 16384, "");
   static std::atomic<uint64_t> lds_allowed{0};
-  auto kernel = k_paged_mfma<T, HD, TK, NW, NB, WEIGH>;
+  auto kernel = k_paged_mfma<T, HD, NW, NB, WEIGH>;
   allow_dynamic_lds((const void*)kernel, TILES + (WEIGH == IN_LDS ? HELD<NW> : 0), lds_allowed);
   const unsigned lds = TILES + (WEIGH == IN_LDS ? a.hq / a.hkv * p.held * 4 : 0);
   const int heads = a.hkv * ((a.hq / a.hkv + 15) / 16);
