@@ -166,24 +166,34 @@ k_paged_attn(PageMap map, const T* __restrict__ qkv, const float2* __restrict__ 
   }
 }
 
+// Sums over pieces: U of them at a time, NEAR times that, and those, so that equal ones next to a long sum are not all rounded the same way (4096 pieces,
+// fp32: outputs off by 6.5e-5 of themselves, so 1e-6).
+constexpr int NEAR = 16;
+
 // Maximum and sum of a (sequence, query head) over its pieces, in their order, U of them on their way at once.
 template <int U>
 __device__ __forceinline__ float2 joined(const float2* __restrict__ ml, size_t step, int n, float scale) {
-  float m = -INFINITY, den = 0.f;
-  for (int z0 = 0; z0 < n; z0 += U) {
+  float m = -INFINITY, den = 0.f, far = 0.f;
+  for (int z0 = 0, turns = 1; z0 < n; z0 += U, ++turns) {
     float2 v[U];
-    float top = m;
+    float top = m, sum = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) v[u] = ml[min(z0 + u, n - 1) * step];
 #pragma unroll
     for (int u = 0; u < U; ++u) top = fmaxf(top, v[u].x);
-    den *= m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale);  // a sum without a maximum is 0, or no number
+    const float corr = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale);  // a sum without a maximum is 0, or no number
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (z0 + u < n) den += v[u].y * (v[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((v[u].x - top) * scale));
+      if (z0 + u < n) sum += v[u].y * (v[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((v[u].x - top) * scale));
+    den = fmaf(den, corr, sum);
+    far *= corr;
+    if (turns % NEAR == 0) {
+      far += den;
+      den = 0.f;
+    }
     m = top;
   }
-  return float2{m, den};
+  return float2{m, far + den};
 }
 
 // The pieces' results, and the slots' weights.  Workgroups [0, out_blocks) of a sequence take its output, D dims to a thread, the others 256 slots
@@ -220,26 +230,38 @@ k_paged_join(PageMap map, T* __restrict__ out, float* __restrict__ weights, int 
     if (!paged_seq(map, b, max_pos, turns, most, t)) return;
     const int n = p.share ? dealt.y : min((t.n + p.keys) / p.keys, p.n);
     if (n == 1) return;  // one piece writes the output itself
-    float m = -INFINITY, den = 0.f;
-    FD num = 0.f;
-    for (int z0 = 0; z0 < n; z0 += U) {
+    float m = -INFINITY, den = 0.f, far_den = 0.f;
+    FD num = 0.f, far_num = 0.f;
+    for (int z0 = 0, times = 1; z0 < n; z0 += U, ++times) {
       if (z0) load(z0);
-      float top = m;
+      float top = m, sum = 0.f;
+      FD part = 0.f;
 #pragma unroll
       for (int u = 0; u < U; ++u) top = z0 + u < n ? fmaxf(top, ml[u].x) : top;
       const float corr = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * scale);  // sums without a maximum are zeros, or no numbers
-      den *= corr;
-      num *= corr;
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (z0 + u < n) {
           const float wt = ml[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml[u].x - top) * scale);
 #pragma unroll
-          for (int e = 0; e < D; ++e) num[e] += v[u][e] * wt;
-          den += ml[u].y * wt;
+          for (int e = 0; e < D; ++e) part[e] += v[u][e] * wt;
+          sum += ml[u].y * wt;
         }
+      den = fmaf(den, corr, sum);
+      far_den *= corr;
+#pragma unroll
+      for (int e = 0; e < D; ++e) num[e] = fmaf(num[e], corr, part[e]);
+      far_num *= corr;
+      if (times % NEAR == 0) {
+        far_den += den;
+        far_num += num;
+        den = 0.f;
+        num = 0.f;
+      }
       m = top;
     }
+    den += far_den;
+    num += far_num;
     TD w;
 #pragma unroll
     for (int e = 0; e < D; ++e) w[e] = from_f<T>(num[e] / den);

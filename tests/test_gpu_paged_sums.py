@@ -87,3 +87,43 @@ def test_weights_of_long_contexts(dtype):
     assert (err <= bound).all()
     u = 2.0**-8 if dtype == torch.bfloat16 else sum(roundings(n // 16 // 4 + 1, 4, 1)) * 2.0**-24 + 2.0**-23
     assert ((out - values).abs() <= 1.01 * u * values.abs()).all()
+
+
+def joined(pieces):
+    """Roundings of a sum over pieces, eight at a time, sixteen times that, and those; a factor for each piece and each time."""
+    return 9 / 2 + 1 + 17 / 2 + 1 + (-(-pieces // 128) + 1) / 2 + 1
+
+
+MANY = pytest.mark.parametrize("hd,n,pieces", [(96, 523000, 4096), (64, 1000000, 256)], ids=["any shape", "matrix cores"])
+
+
+def own_roundings(hd, n, pieces):
+    """Of a piece's sums of weights and of weighted values.  The kernel for every shape adds eight keys up, and 64 times that; the other one has eight
+    wavefronts in a piece."""
+    if hd == 96:
+        assert n / pieces <= 512
+        return (9 / 2 + 65 / 2 + 1,) * 2
+    return roundings(n // 16 // pieces // 8 + 1, 8, 0)
+
+
+@MANY
+def test_outputs_of_many_pieces(hd, n, pieces):
+    out, _, values, _, _ = call(1, hd, torch.float32, [n], n, False)
+    bound = (sum(own_roundings(hd, n, pieces)) + 2 * joined(pieces) + 2) * 2.0**-24
+    err = float(((out - values).abs() / values.abs()).max())
+    print("outputs off by %.2e of them, %.2e allowed" % (err, bound))
+    assert err <= bound
+
+
+@MANY
+@TYPES
+def test_weights_of_many_pieces(hd, n, pieces, dtype):
+    out, weights, values, below, table = call(1, hd, dtype, [n], n, True)
+    slot = torch.arange(n + 1)
+    got = weights[table[0].long()[slot // PAGE], :, slot % PAGE].double()
+    w = torch.where(((slot % 16 == 0) | (slot == n))[:, None], 1.0, below.exp()[None])
+    want = w / w.sum(0)
+    bound = (own_roundings(hd, n, pieces)[0] + joined(pieces) + 3 + 2 * (4 + 6 * below.abs())) * 2.0**-24
+    err = float(((got - want).abs() / want).max())
+    print("weights off by %.2e of them, %.2e allowed" % (err, float(bound.min())))
+    assert err <= float(bound.min())
