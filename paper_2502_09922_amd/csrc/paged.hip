@@ -162,7 +162,7 @@ constexpr int64_t NARROW = 1 << 29;
 // `keep` slots or more reach is searched for between the smallest and the largest of the slots that may go, by where it lay if keys were spread
 // evenly, until exactly `keep` slots reach it or nothing is left between; in the latter case the lower ones of equal keys stay.  Weights and places
 // are read once.  V > 0: the keys of up to 64 W V slots are held in V registers of a lane; V = 0: each lane leaves them in memory for itself, four of
-// its slots side by side (8 units of 131072 slots 248 us, 930 when keys were made again for each count).
+// its slots side by side (8 units of 131072 slots 270 us, 930 when keys were made again for each count).
 // Where a unit has no more than FEW moves (`here`), they are made here: another launch for one move each took 6 us for 5120 units.
 // Bound by its steps one after the other: 70B, 128 units of up to 16384 slots down to 2048 26 us (16 wavefronts; 4 loads, 8 rounds, 4 list), 5120
 // units of 501 slots, one move each, 15.
@@ -395,7 +395,14 @@ __global__ void __launch_bounds__(256) k_evict_lens(EvictArgs a, int32_t* __rest
 int key_groups(int max_len) { return max_len > HELD ? ((max_len + 1023) / 1024 + GROUPS - 1) / GROUPS * GROUPS : 0; }
 
 void launch_evict(const EvictArgs& a, size_t units, int32_t* lens, hipStream_t st) {
-  // More wavefronts to a unit where units do not fill the chip: 1024 units of 1025 slots 14 -> 10 us.
+  // As many registers as hold the keys, and more wavefronts to a unit where units do not fill the chip.  One slot to go, with the second launch, us:
+  //    501 slots, 8 / 512 / 4096 units    one wavefront 12 / 18 / 18   four 17 / 22 / 38
+  //   1025 slots, 64 / 2048 / 4096 units  one 25 / 26 / 31             four 16 / 27 / 36         sixteen 21 / 85 / 164
+  //   2049 slots, 8 / 512 / 4096 units                                 four 15 / 26 / 53         sixteen 15 / 39 / 153
+  //   4097 slots, 8 / 64 / 512 / 2048 units                            four 22 / 23 / 25 / 48    sixteen 18 / 20 / 29 / 82
+  //   8000 slots, 8 / 64 / 512 units                                   four 25 / 25 / 30         sixteen 18 / 17 / 33
+  // so that up to 512 slots one wavefront does, up to 4096 four; beyond, and below for one, it goes by the units.  (From 512 units on four would
+  // do for 4097 to 8192 slots, which `few` leaves to sixteen.)
   const bool few = units <= 2048, here = a.most <= FEW;
   const int n = a.max_len;
   if (n > HELD) k_evict_choose<16, 0, size_t><<<units, 1024, 0, st>>>(a, here);

@@ -5,9 +5,9 @@
 //
 // Here the kernel for every shape (the fast one: paged_attn_mfma.hip), which pieces a context is cut into, and the kernel that joins them
 // and adds the weights up.  One wavefront to a (sequence, query head, piece), a lane to one or two pairs of dims, eight keys and values on
-// their way at once; eight slots lie in one page, whose number is uniform.  Bound by a wavefront's instructions: of 128 dims, as before
-// the matrix cores had them, 13B, 32 sequences of 1024 to 1087 slots 140 us (106 there), 70B, 64 ragged ones 699 (66): each query head
-// reads the cache for itself.
+// their way at once; eight slots lie in one page, whose number is uniform.  Bound by a wavefront's instructions, as each query head reads the
+// cache for itself: 96 dims, bf16, 40 heads over 40, 32 sequences of 1024 to 1087 slots 121 us (4.3 TB/s), 64 heads over 8, 64 of 128 to 2287 slots
+// 697 (0.36 TB/s of what one reading takes).
 #include "paged.hpp"
 
 #include <algorithm>
@@ -329,10 +329,11 @@ size_t piece_bytes(const PagedAttn& a, const PagedPieces& p) {
 //   - Where a kv head's keys and values of a sequence are at most ONE bytes, one workgroup each and no second launch: 8 kv heads, bf16, 128 dims,
 //     600 slots 10.2 us, in pieces of 128 slots 11.7 (900 slots 12.1 and 11.7); 64 dims, 1200 slots 11.2 and 11.4; fp32, 128 dims, 300 slots 11.5
 //     and 11.8, 400 slots 13.7 and 11.8.
-//   - Where some may be longer than LONG bytes, workgroups get shares by the lengths that the device knows: of 32 sequences of 500 slots and one of 16000, 8
-//     kv heads, the long one's 8 workgroups took 153 us, shared out 30; 64 of 300 and two of 3500 73 and 29.  It costs a microsecond in
-//     front and the second launch: 64 of 5000 slots 199 us uncut, 205 shared out; 64 of 2287 93 and 103.
-//   - Otherwise in equal pieces until a CU each has one: 7B, one sequence of 3000 slots 15.3 us, 16.6 with two to a CU.
+//   - Where some may be longer than LONG bytes, workgroups get shares by the lengths that the device knows: of 32 sequences of 500 slots and one of 16000, 64
+//     heads over 8, the long one's 8 workgroups take 191 us, shared out 39; 64 of 300 and two of 3500 51 and 31.  It costs a microsecond in
+//     front and the second launch: 64 of 5000 slots 200 us uncut, 209 shared out; 64 of 2287 93 and 103.
+//   - Otherwise in equal pieces until a CU each has one: 7B, one sequence of 3000 slots 14.9 us, 16.6 with two to a CU.  Where lengths differ the longest
+//     one's pieces are what the launch waits for: 32 heads, fp32, 700, 596, 240 and 632 slots 24 tiles, of which an even share were 17.
 PagedPieces pieces_for(const PagedAttn& a, size_t room) {
   PagedPieces p;
   p.keys = (a.max_keys + 63) / 64 * 64;

@@ -17,12 +17,12 @@
 //
 // The new token's row is put into its tile in LDS by the wavefront that has that tile, and into the cache: nobody waits for memory there.
 //
-// Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 106 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for,
-// as long; the arithmetic alone 45.  70B, 64 of 128 to 2287 slots 60 us, 6.1 TB/s (66 when a CU's two workgroups were of the same sequence).  4 of
-// 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 109, 6.0 TB/s, where a tile's products take half of its time on a
-// SIMD.  Weights: where a workgroup has all of a sequence's slots, scores wait in LDS as far as there is room (13B, 32 sequences 120 us), otherwise they
-// go out and come back, 4 bytes for each query head and slot: 70B, 64 of 128 to 2287 slots 75 us instead of 57 (12 for the stores, 5 of which
-// they cost where all of them go to the same lines; behind the fills or in another layout no less).
+// Bound by memory: 13B, 32 sequences of 1024 to 1087 slots (694 MB of cache) 107 us, 6.5 TB/s; with no arithmetic at all, the tiles only waited for,
+// 106; the arithmetic alone 45.  70B, 64 of 128 to 2287 slots (366 MB) 60 us, 6.1 TB/s (66 when a CU's two workgroups were of the same sequence).  4 of
+// 20001 to 32768 80, of which 5 are the second launch.  fp32, 13B, 16 of 1000 108, 6.0 TB/s, where a tile's products take half of its time on a
+// SIMD.  Weights: where a workgroup has all of a sequence's slots, scores wait in LDS as far as there is room (13B, 32 sequences 121 us), otherwise they
+// go out and come back, 4 bytes for each query head and slot: 70B, 64 others of 128 to 2287 slots (337 MB) 75 us instead of 56 (12 for the stores, 5 of
+// which they cost where all of them go to the same lines; behind the fills or in another layout no less).
 #include "attn_mfma.hpp"
 #include "paged.hpp"
 
@@ -114,7 +114,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
   constexpr int UNITS = TK / 8;    // parts of a tile that lie in one page whatever the page's size
   constexpr int TILE = TK * ROWB;
   constexpr int DT = HD / 16;
-  constexpr bool APART = NB == 1;  // the next tile's keys are asked for as soon as this one's are read: fp32, 13B, 16 of 1000 slots 116 -> 109 us (bf16, two tiles, 106 -> 108)
+  constexpr bool APART = NB == 1;  // the next tile's keys are asked for as soon as this one's are read: fp32, 13B, 16 of 1000 slots 116 -> 108 us (bf16, two tiles, 106 -> 108)
   constexpr int STORES = WEIGH == IN_MEMORY ? 1 : 0;  // of a tile's scores
   static_assert(RPI <= 8 && (NB & (NB - 1)) == 0, "");
   typedef T T4 __attribute__((ext_vector_type(4)));
@@ -205,7 +205,7 @@ k_paged_mfma(PageMap map, const T* __restrict__ qkv, const float* __restrict__ c
     else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
   };
 #pragma clang diagnostic pop
-  // What one block of columns reads once does not stay in L2: 13B, 32 sequences 120 -> 106 us, 70B, 64 ragged 76 -> 66 (32 heads over one,
+  // What one block of columns reads once does not stay in L2: 13B, 32 sequences 120 -> 106 us, 70B, 64 ragged 76 -> 66, by now 60 (32 heads over one,
   // 64 sequences of 2000 slots, which two blocks read: 21 and 24).
   auto rows_of_tile = [&](const T* const* from, const unsigned* off, unsigned to) __attribute__((always_inline)) {
     auto all = [&](auto once) __attribute__((always_inline)) {
@@ -594,9 +594,9 @@ void launch_kernel_of(const PagedAttn& a, const PagedPieces& p, int most, hipStr
 }
 
 // Four wavefronts with two tiles each, two workgroups to a CU (fp32 of 128 dims: one tile of 16 KB), or twice the wavefronts where a CU has one
-// workgroup at most.  13B, 32 sequences 106 us; three wavefronts 110, two 116, tiles of 32 keys or rings of four tiles, which leave a CU one
-// workgroup, 7 to 8 more.  7B, 8 sequences of 1024 slots with weights: eight wavefronts 27.0, four 29.1.
-// Scores of one workgroup that has all of a sequence's slots stay in LDS where they fit: 13B, 32 sequences of 1024 to 1087 slots 120 us, 132 through memory.
+// workgroup at most.  13B, 32 sequences 106 us when these were compared; three wavefronts 110, two 116, tiles of 32 keys or rings of four tiles, which leave a CU one
+// workgroup, 7 to 8 more.  7B, 8 sequences of 1024 slots with weights: eight wavefronts 27.0, four 29.1 (28.1 since queries have three parts).
+// Scores of one workgroup that has all of a sequence's slots stay in LDS where they fit: 13B, 32 sequences of 1024 to 1087 slots 121 us, 132 through memory.
 template <class T, int HD, int NW, int NB>
 void launch_nw(const PagedAttn& a, PagedPieces p, int most, hipStream_t st) {
   p.held = p.stride + 4;  // columns' equal slots in different banks
